@@ -27,6 +27,12 @@ FUNCTIONS = ("sketchssm_update", "sketchssm_decode", "sketchssm_full_read_baseli
              "sketchssm_ring_bytes", "sketchssm_status_string", "sketchssm_last_error", "sketchssm_check_config")
 
 
+# include/sketchssm_mixer.h: the operators around the recurrence (ops.py takes tensors)
+MIXER_FUNCTIONS = ("sketchssm_conv", "sketchssm_conv_token", "sketchssm_scan", "sketchssm_scan_workspace", "sketchssm_norm",
+                   "sketchssm_matmul_fp8", "sketchssm_matmul_fp8_workspace")
+E4M3 = 2
+
+
 class SketchSSMError(RuntimeError):
     def __init__(self, status: int, message: str):
         super().__init__(f"{STATUS.get(status, status)}: {message}")
@@ -54,6 +60,22 @@ class Ring(ctypes.Structure):
 
 class Token(ctypes.Structure):
     _fields_ = [(name, ctypes.c_void_p) for name in ("k", "v", "beta", "log_decay")]
+
+
+class ConvConfig(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_int32) for name in ("channels", "width", "io_dtype", "silu")]
+
+
+class NormArgs(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64)] + [(name, ctypes.c_int32) for name in
+                ("columns", "group", "x_dtype", "io_dtype", "out_dtype", "skip_width")] + [
+                   ("eps", ctypes.c_float), ("x", ctypes.c_void_p), ("ldx", ctypes.c_int64),
+                   ("residual", ctypes.c_void_p), ("ld_residual", ctypes.c_int64),
+                   ("residual_out", ctypes.c_void_p), ("ld_residual_out", ctypes.c_int64),
+                   ("gate", ctypes.c_void_p), ("ld_gate", ctypes.c_int64),
+                   ("skip", ctypes.c_void_p), ("ld_skip", ctypes.c_int64), ("skip_head", ctypes.c_int64),
+                   ("D", ctypes.c_void_p), ("weight", ctypes.c_void_p), ("out", ctypes.c_void_p),
+                   ("ld_out", ctypes.c_int64), ("scales", ctypes.c_void_p), ("ld_scales", ctypes.c_int64)]
 
 
 _lib = None
@@ -90,6 +112,17 @@ def load(path: str | None = None):
     lib.sketchssm_status_string.restype = ctypes.c_char_p
     lib.sketchssm_last_error.argtypes = []
     lib.sketchssm_last_error.restype = ctypes.c_char_p
+    i32, i64, size = ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
+    lib.sketchssm_conv.argtypes = [ctypes.POINTER(ConvConfig), i32, i64, P, P, i64, P, P, P, P, P, i64, P]
+    lib.sketchssm_conv_token.argtypes = [cfgp, i32, i32, P, i64, P, P, P, P, i64, P, P, ringp, i32, P, P]
+    lib.sketchssm_scan.argtypes = [cfgp, i32, i64, P, P, i64, P, i64, P, i64, P, i64, P, P, P, P, P, P, i64, P, size, P]
+    lib.sketchssm_norm.argtypes = [ctypes.POINTER(NormArgs), P]
+    lib.sketchssm_matmul_fp8.argtypes = [i64, i32, i32, P, i64, P, i64, P, i64, P, i32, P, i64, P, size, P]
+    for f in ("sketchssm_conv", "sketchssm_conv_token", "sketchssm_scan", "sketchssm_norm", "sketchssm_matmul_fp8"):
+        getattr(lib, f).restype = ctypes.c_int
+    lib.sketchssm_scan_workspace.argtypes = [cfgp, i64]
+    lib.sketchssm_matmul_fp8_workspace.argtypes = [i64, i32, i32]
+    lib.sketchssm_scan_workspace.restype = lib.sketchssm_matmul_fp8_workspace.restype = size
     _lib = lib
     return lib
 

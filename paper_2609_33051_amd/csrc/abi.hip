@@ -9,10 +9,17 @@
 
 #include "../../include/sketchssm.h"
 #include "args.h"
+#include "host.h"
 
 namespace {
 
 thread_local char g_err[512] = "";
+
+constexpr int64_t kMaxItems = (int64_t)1 << 23;
+
+}  // namespace
+
+namespace skssm {
 
 int fail(int code, const char* fmt, ...) {
   va_list ap;
@@ -21,10 +28,6 @@ int fail(int code, const char* fmt, ...) {
   va_end(ap);
   return code;
 }
-
-constexpr int64_t kMaxItems = (int64_t)1 << 23;
-
-bool aligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 // Shape checks common to every entry point.
 int check_shape(const skssm_config* c, bool need_rank, bool allow_rank0) {
@@ -55,15 +58,6 @@ int check_shape(const skssm_config* c, bool need_rank, bool allow_rank0) {
   return SKSSM_OK;
 }
 
-// State-dependent maps: P = 4 pivots for ranks 8..32, the exact metric for
-// ranks 8 and 16 (the storage width with a rank table).
-int check_map_rank(const skssm_config* c) {
-  if (c->pivots == SKSSM_EXACT_MAP && c->rank != 8 && c->rank != 16)
-    return fail(SKSSM_EUNSUPPORTED, "the exact-metric map is compiled for rank 8 and 16");
-  if (c->rank < 8 || c->rank > 32) return fail(SKSSM_EUNSUPPORTED, "state-dependent maps need rank 8..32");
-  return SKSSM_OK;
-}
-
 // Ring fields read or written by a call: the raw inputs always, the derived
 // fields of the family, and f (`derived_f`, sketch read) or pi
 // (`derived_pi`, exact baseline).
@@ -80,6 +74,33 @@ int check_ring(const skssm_config* c, const skssm_ring* r, bool derived_f, bool 
     if (derived_pi && !r->pi) return fail(SKSSM_EINVAL, "ring pi is NULL (GDN/KDA baseline)");
     if (derived_pi && !aligned(r->pi)) return fail(SKSSM_EALIGN, "ring pi not aligned");
   }
+  return SKSSM_OK;
+}
+
+int launched(int rc, const char* what) {
+  if (rc == -2) return fail(SKSSM_EUNSUPPORTED, "%s: no kernel compiled for this shape", what);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return fail(SKSSM_EHIP, "%s: %s", what, hipGetErrorString(e));
+  g_err[0] = '\0';
+  return SKSSM_OK;
+}
+
+}  // namespace skssm
+
+namespace {
+
+using skssm::aligned;
+using skssm::check_ring;
+using skssm::check_shape;
+using skssm::fail;
+using skssm::launched;
+
+// State-dependent maps: P = 4 pivots for ranks 8..32, the exact metric for
+// ranks 8 and 16 (the storage width with a rank table).
+int check_map_rank(const skssm_config* c) {
+  if (c->pivots == SKSSM_EXACT_MAP && c->rank != 8 && c->rank != 16)
+    return fail(SKSSM_EUNSUPPORTED, "the exact-metric map is compiled for rank 8 and 16");
+  if (c->rank < 8 || c->rank > 32) return fail(SKSSM_EUNSUPPORTED, "state-dependent maps need rank 8..32");
   return SKSSM_OK;
 }
 
@@ -124,14 +145,6 @@ void put_order(skssm::DecodeArgs& a, const Ranks& rk) {
 template <class A> void put_ranks(A& a, const Ranks& rk) {
   a.ragged = rk.ragged;
   for (int h = 0; h < skssm::kMaxRaggedHeads; ++h) a.hrank[h] = rk.h[h];
-}
-
-int launched(int rc, const char* what) {
-  if (rc == -2) return fail(SKSSM_EUNSUPPORTED, "%s: no kernel compiled for this shape", what);
-  const hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return fail(SKSSM_EHIP, "%s: %s", what, hipGetErrorString(e));
-  g_err[0] = '\0';
-  return SKSSM_OK;
 }
 
 // The current token's own arrays (sketchssm_step): all required, aligned like

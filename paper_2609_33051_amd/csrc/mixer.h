@@ -1,0 +1,136 @@
+// Argument blocks and device helpers of the operators around the recurrence
+// (convolution, scan, norm, 8-bit products).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "args.h"
+#include "device.h"
+
+namespace skssm {
+
+// Packed sequences: sequence b is rows start(b) .. start(b + 1) - 1 of `tokens`.
+// Offsets come from device memory and are held to 0..tokens here, so that no
+// access leaves the arrays whatever they hold.
+struct Sequences {
+  const int32_t* offsets;  // [batch + 1], or NULL: equal lengths
+  int batch, tokens, each; // each = tokens / batch (offsets NULL)
+  __device__ __forceinline__ int start(int b) const {
+    if (!offsets) return b * each;
+    const int o = offsets[b];
+    return o < 0 ? 0 : o > tokens ? tokens : o;
+  }
+  // The sequence that holds row t: the last one that starts at or before it.
+  __device__ __forceinline__ int of(int t) const {
+    if (!offsets) return t / each;
+    int lo = 0, hi = batch;  // start(lo) <= t (or lo = 0), start(hi) > t (or hi = batch)
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (start(mid) <= t) lo = mid; else hi = mid;
+    }
+    return lo;
+  }
+};
+
+__device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + fast_exp(-z)); }
+// log(1 + e^r), exact to fp32 where e^r is small against 1 (the step sizes are 1e-3 and less)
+__device__ __forceinline__ float softplus(float r) { return fmaxf(r, 0.f) + log1pf(__expf(-fabsf(r))); }
+
+struct ConvArgs {
+  Sequences seq;
+  int C;                  // channels
+  const void* x;          // rows ldx elements apart
+  size_t ldx;
+  const float* taps;      // [C][w]
+  const float* bias;      // [C] or NULL
+  const void* state_in;   // [batch][w-1][C] or NULL
+  void* state_out;        // or NULL
+  void* y;
+  size_t ldy;
+};
+// `states_apart`: the new states are written by a launch of their own, after the outputs'
+int run_conv(const ConvArgs& a, int width, int io, int silu, bool states_apart, void* stream);
+
+struct ConvTokenArgs {
+  int B, H, G, W, n, K, V;
+  const void* x;          // [B][H V + 2 G K], rows ldx apart
+  size_t ldx;
+  const float* taps;
+  const float* bias;
+  void* state;            // [B][w-1][C]
+  const void* dt;         // [B][H], rows lddt apart
+  size_t lddt;
+  const float* dt_bias;
+  const float* A;
+  void* rk;               // ring fields [B][H][W][..], slot n
+  void* rv;
+  float* rbeta;
+  float* rla;
+  void* q;                // [B][H][K]
+};
+int run_conv_token(const ConvTokenArgs& a, int width, int io, void* stream);
+
+struct NormArgs {
+  int rows, columns, group;
+  int skip_width;
+  float eps;
+  const void* x;
+  size_t ldx;
+  const void* residual;
+  size_t ld_residual;
+  void* residual_out;
+  size_t ld_residual_out;
+  const void* gate;
+  size_t ld_gate;
+  const void* skip;
+  size_t ld_skip, skip_head;
+  const float* D;
+  const float* weight;
+  void* out;
+  size_t ld_out;
+  float* scales;
+  size_t ld_scales;
+};
+int run_norm(const NormArgs& a, int x_dtype, int io, int out, void* stream);
+
+struct MatmulArgs {
+  int M, N, K;
+  const uint8_t* a;
+  size_t lda;
+  const float* sa;
+  size_t ldsa;
+  const uint8_t* w;
+  size_t ldw;
+  const float* sw;
+  void* y;
+  size_t ldy;
+  float* part;            // split products, [splits][M][N]
+};
+int run_matmul_fp8(const MatmulArgs& a, int out, void* stream);
+size_t matmul_fp8_workspace(int M, int N, int K);
+
+struct ScanArgs {
+  Sequences seq;
+  int H, G;
+  const void* x;
+  size_t ldx;
+  const void* b;
+  size_t ldb;
+  const void* c;
+  size_t ldc;
+  const void* dt;
+  size_t lddt;
+  const float* dt_bias;
+  const float* A;
+  const float* D;
+  const float* S_in;
+  float* S_out;
+  void* y;
+  size_t ldy;
+  float* work;
+};
+int run_scan(const ScanArgs& a, int K, int V, int io, void* stream);
+size_t scan_workspace(int batch, int tokens, int H, int K, int V);
+
+}  // namespace skssm
