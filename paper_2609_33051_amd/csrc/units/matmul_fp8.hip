@@ -13,6 +13,8 @@
 // Under an output stored in bf16 (2^-8) that is nothing.  An fp32 output is computed
 // from the same values as bf16, which holds e4m3 exactly, by four 16x16x32_bf16
 // (7.5e-8 on the same blocks) at half the rate.
+#include <type_traits>
+
 #include "../mixer.h"
 
 namespace skssm {
@@ -128,86 +130,144 @@ __global__ __launch_bounds__(64 * WAVES) void matmul_few_kernel(MatmulArgs p) {
 __device__ __forceinline__ int key_a(int row) { return row & 7; }
 __device__ __forceinline__ int key_w(int row) { return (row & 3) | ((row >> 2) & 4); }
 
-typedef __attribute__((address_space(3))) void lds_void;
-typedef const __attribute__((address_space(1))) void global_void;
-__device__ __forceinline__ void to_lds16(const void* src, void* dst) {  // dst: the wave's first lane's
-  __builtin_amdgcn_global_load_lds((global_void*)src, (lds_void*)dst, 16, 0, 0);
+// 16 bytes a lane from base + at into LDS, the wave's 64 lanes one after the other
+// from `lds`.  In assembly, as the compiler would wait for every such load before the next
+// LDS read, whatever it reads; the caller waits (vmcnt) before the barrier that
+// publishes a stage.  No register is written.
+__device__ __forceinline__ void to_lds16(const uint8_t* base, uint32_t at, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(at), "s"(base) : "memory", "m0");
+}
+__device__ __forceinline__ uint32_t lds_address(const void* p) {
+  return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
 }
 
 template <typename OUT, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__(64 * WM * WN) void matmul_tile_kernel(MatmulArgs p) {
+__global__ __launch_bounds__(64 * WM * WN, 2) void matmul_tile_kernel(MatmulArgs p, int mt, int nt) {
   constexpr int WAVES = WM * WN, TM = BM / WM / 16, TN = BN / WN / 16;  // 16 x 16 tiles of a wave
+  constexpr int SA = BM / 8 / WAVES, SW = BN / 8 / WAVES;              // 8-row pieces a wave stages
   static_assert(TN % 4 == 0, "a lane's 16 consecutive columns come from 4 tiles");
   __shared__ __attribute__((aligned(16))) uint8_t la[2][BM * 128], lw[2][BN * 128];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = lane & 15, g = lane >> 4;
-  const int mt = (p.M + BM - 1) / BM;
-  const int m0 = (blockIdx.x % mt) * BM, n0 = (blockIdx.x / mt) * BN;
-  const int wm = wave % WM, wn = wave / WM, blocks = (p.K + 127) >> 7, last = p.K / 16 - 1;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, g = lane >> 4;
+  // Workgroups go round the eight XCDs: each XCD takes a run of tiles, in columns of 8
+  // tiles of rows, so that what runs at once on it shares rows of a and of w in its L2.
+  int tile = blockIdx.x;
+  {
+    const int n = mt * nt, per = n / 8, rest = n % 8, x = tile % 8, i = tile / 8;
+    tile = x * per + min(x, rest) + i;
+  }
+  constexpr int BAND = 8;
+  const int band = tile / (BAND * nt), rows = min(BAND, mt - band * BAND), in = tile - band * BAND * nt;
+  const int m0 = (band * BAND + in % rows) * BM, n0 = (in / rows) * BN;
+  const int wm = wave % WM, wn = wave / WM, blocks = (p.K + 127) >> 7, full = p.K >> 7;
   floatx4 acc[TN][TM];
 #pragma unroll
   for (int j = 0; j < TN; ++j)
 #pragma unroll
     for (int i = 0; i < TM; ++i) acc[j][i] = floatx4{0.f, 0.f, 0.f, 0.f};
 
-  auto stage = [&](int kb, int buf) {  // a wave moves 8 rows at a time
+  const uint8_t* const a0 = p.a + (size_t)m0 * p.lda;
+  const uint8_t* const w0 = p.w + (size_t)n0 * p.ldw;
+  const uint32_t lds_a = lds_address(la), lds_w = lds_address(lw);
+  // a wave moves 8 rows at a time; rows past the end repeat the last one, chunks past the end of K the last chunk
+  uint32_t va[SA], vw[SW];
+  auto places = [&](int chunks) {
 #pragma unroll
-    for (int s = 0; s < BM / 8 / WAVES; ++s) {
-      const int row = (s * WAVES + wave) * 8 + (lane >> 3);
-      const int c = min(kb * 8 + ((lane & 7) ^ key_a(row)), last);
-      to_lds16(p.a + (size_t)min(m0 + row, p.M - 1) * p.lda + (size_t)c * 16, &la[buf][(s * WAVES + wave) * 1024]);
+    for (int s = 0; s < SA; ++s) {
+      const int row = (s * WAVES + wave) * 8 + (lane >> 3), c = min((lane & 7) ^ key_a(row), chunks - 1);
+      va[s] = (uint32_t)(min(row, p.M - 1 - m0) * (uint32_t)p.lda) + c * 16;
     }
 #pragma unroll
-    for (int s = 0; s < BN / 8 / WAVES; ++s) {
-      const int row = (s * WAVES + wave) * 8 + (lane >> 3);
-      const int c = min(kb * 8 + ((lane & 7) ^ key_w(row)), last);
-      to_lds16(p.w + (size_t)min(n0 + row, p.N - 1) * p.ldw + (size_t)c * 16, &lw[buf][(s * WAVES + wave) * 1024]);
+    for (int s = 0; s < SW; ++s) {
+      const int row = (s * WAVES + wave) * 8 + (lane >> 3), c = min((lane & 7) ^ key_w(row), chunks - 1);
+      vw[s] = (uint32_t)(min(row, p.N - 1 - n0) * (uint32_t)p.ldw) + c * 16;
     }
   };
-  auto frag = [&](const uint8_t* tile, int row, int key) {
-    const uint8_t* at = tile + row * 128;
-    return join(*reinterpret_cast<const uint4*>(at + ((g ^ key) << 4)), *reinterpret_cast<const uint4*>(at + (((g + 4) ^ key) << 4)));
+  auto stage = [&](int kb, int buf) {
+    if (kb == full) places((p.K >> 4) & 7);
+#pragma unroll
+    for (int s = 0; s < SA; ++s) to_lds16(a0 + (size_t)kb * 128, va[s], lds_a + buf * BM * 128 + (s * WAVES + wave) * 1024);
+#pragma unroll
+    for (int s = 0; s < SW; ++s) to_lds16(w0 + (size_t)kb * 128, vw[s], lds_w + buf * BN * 128 + (s * WAVES + wave) * 1024);
   };
-  float sa[TM];
+  // the lane's two chunks of its row in the wave's first tile of a and of w; tile i of a lies
+  // 16 rows on, and tile j of w takes lane row 4 x + y from row 16 x + 4 (j % 4) + y of 64:
+  // neither changes the key
+  const uint32_t oa = (wm * TM * 16 + r) * 128, ow = (wn * TN * 16 + (r >> 2) * 16 + (r & 3)) * 128;
+  const int ka = key_a(r), kw = (r & 3) | (r & 4);
+  const uint32_t oa0 = oa + ((g ^ ka) << 4), oa1 = oa + (((g + 4) ^ ka) << 4);
+  const uint32_t ow0 = ow + ((g ^ kw) << 4), ow1 = ow + (((g + 4) ^ kw) << 4);
+  auto frag = [&](const uint8_t* t0, const uint8_t* t1, int at) {
+    return join(*reinterpret_cast<const uint4*>(t0 + at), *reinterpret_cast<const uint4*>(t1 + at));
+  };
+  // the block's factors: a_scale of the lane's rows, w_scale of the wave's 64-column parts
+  float sa[TM], sw[TN / 4], na[TM], nw[TN / 4];
   auto scales = [&](int kb) {
 #pragma unroll
-    for (int i = 0; i < TM; ++i) sa[i] = p.sa[(size_t)kb * p.ldsa + min(m0 + (wm * TM + i) * 16 + r, p.M - 1)];
+    for (int i = 0; i < TM; ++i) na[i] = p.sa[(size_t)kb * p.ldsa + min(m0 + (wm * TM + i) * 16 + r, p.M - 1)];
+#pragma unroll
+    for (int q = 0; q < TN / 4; ++q) nw[q] = p.sw[(size_t)min((n0 + wn * TN * 16 + q * 64) >> 7, (p.N - 1) >> 7) * blocks + kb];
   };
-  stage(0, 0);
-  for (int kb = 0; kb < blocks; ++kb) {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    if (kb + 1 < blocks) stage(kb + 1, (kb + 1) & 1);
-    scales(kb);
+  auto compute = [&](int kb, auto tail) {
     const uint8_t* ta = la[kb & 1];
     const uint8_t* tw = lw[kb & 1];
+    // w's fragments are read a tile ahead, and between the products of a tile the
+    // vector units scale the sums of the tile before: 4 FMA in the shadow of an
+    // instruction of 32 cycles (in a block of their own after the tile's products
+    // they cost 7 %: 654 us against 609 at 8192 x 18560 x 4096)
+    auto weights = [&](int j) { return frag(tw + ow0, tw + ow1, ((j >> 2) * 64 + (j & 3) * 4) * 128); };
+    intx8 ahead = weights(0);
     Operand<OUT> fa[TM];
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
-      const int row = (wm * TM + i) * 16 + r;
-      intx8 x = frag(ta, row, key_a(row));
-      if (kb * 8 + 7 > last) {  // chunks past the end of K add nothing
+      intx8 x = frag(ta + oa0, ta + oa1, i * 16 * 128);
+      if constexpr (decltype(tail)::value) {  // chunks past the end of K add nothing
+        const int chunks = (p.K >> 4) & 7;
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-          if (kb * 8 + g + (e & 4) > last) x[e] = 0;
+          if (g + (e & 4) >= chunks) x[e] = 0;
       }
       fa[i].set(x);
     }
+    floatx4 t[2][TM];
 #pragma unroll
-    for (int j = 0; j < TN; ++j) {
-      // rows of tile j: lane row 4 x + y is column 16 x + 4 (j % 4) + y of 64
-      const int row = wn * TN * 16 + (j >> 2) * 64 + (r >> 2) * 16 + (j & 3) * 4 + (r & 3);
+    for (int j = 0; j <= TN; ++j) {
       Operand<OUT> fw;
-      fw.set(frag(tw, row, key_w(row)));
-      const int nb = min((n0 + wn * TN * 16 + (j >> 2) * 64) >> 7, (p.N - 1) >> 7);
-      const float sw = p.sw[(size_t)nb * blocks + kb];
+      if (j < TN) fw.set(ahead);
+      if (j + 1 < TN) ahead = weights(j + 1);
 #pragma unroll
       for (int i = 0; i < TM; ++i) {
-        const floatx4 t = block_product(fw, fa[i]);
-        const float s = sa[i] * sw;
+        if (j < TN) t[j & 1][i] = block_product(fw, fa[i]);
+        if (j > 0) {
+          const float s = sa[i] * sw[(j - 1) >> 2];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc[j][i][e] = fmaf(s, t[e], acc[j][i][e]);
+          for (int e = 0; e < 4; ++e) acc[j - 1][i][e] = fmaf(s, t[(j - 1) & 1][i][e], acc[j - 1][i][e]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
+  };
+  auto next = [&](int kb) {  // block kb's stage has come; block kb + 1's starts
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < TM; ++i) sa[i] = na[i];
+#pragma unroll
+    for (int q = 0; q < TN / 4; ++q) sw[q] = nw[q];
+    if (kb + 1 < blocks) {
+      stage(kb + 1, (kb + 1) & 1);
+      scales(kb + 1);
+    }
+  };
+  places(8);
+  stage(0, 0);
+  scales(0);
+  for (int kb = 0; kb < full; ++kb) {
+    next(kb);
+    compute(kb, std::false_type{});
+  }
+  if (full < blocks) {
+    next(full);
+    compute(full, std::true_type{});
   }
   const bool wide = (p.ldy * sizeof(OUT)) % 16 == 0 && (p.N & 15) == 0;
 #pragma unroll
@@ -242,6 +302,12 @@ __global__ __launch_bounds__(64 * WM * WN) void matmul_tile_kernel(MatmulArgs p)
   }
 }
 
+template <typename OUT, int BM, int BN, int WM, int WN>
+void launch_tiles(const MatmulArgs& p, hipStream_t s) {
+  const int mt = (p.M + BM - 1) / BM, nt = (p.N + BN - 1) / BN;
+  hipLaunchKernelGGL((matmul_tile_kernel<OUT, BM, BN, WM, WN>), dim3((unsigned)mt * (unsigned)nt), dim3(64 * WM * WN), 0, s, p, mt, nt);
+}
+
 template <typename OUT>
 int launch_matmul(const MatmulArgs& p, hipStream_t s) {
   const int mt = (p.M + 15) / 16;
@@ -250,9 +316,8 @@ int launch_matmul(const MatmulArgs& p, hipStream_t s) {
   else if (mt <= 2) hipLaunchKernelGGL((matmul_few_kernel<OUT, 2, 8>), few, dim3(512), 0, s, p);
   else if (mt <= 4) hipLaunchKernelGGL((matmul_few_kernel<OUT, 4, 8>), few, dim3(512), 0, s, p);
   else if (mt <= 8) hipLaunchKernelGGL((matmul_few_kernel<OUT, 8, 8>), few, dim3(512), 0, s, p);
-  else
-    hipLaunchKernelGGL((matmul_tile_kernel<OUT, 128, 128, 2, 2>), dim3((unsigned)(((p.M + 127) / 128) * ((p.N + 127) / 128))),
-                       dim3(256), 0, s, p);
+  else if (sizeof(OUT) == 4 || (int64_t)((p.M + 255) / 256) * ((p.N + 255) / 256) < 256) launch_tiles<OUT, 128, 128, 2, 2>(p, s);
+  else launch_tiles<bf16_t, 256, 256, 4, 2>(p, s);
   return 0;
 }
 

@@ -310,6 +310,8 @@ int sketchssm_matmul_fp8(int64_t M, int32_t N, int32_t K, const void* a, int64_t
   if (out_dtype != SKSSM_F32 && out_dtype != SKSSM_BF16) return fail(SKSSM_EINVAL, "%s: unknown out_dtype %d", what, out_dtype);
   int rc;
   if ((rc = check_stride(what, "a", lda, K, 1)) || (rc = check_stride(what, "w", ldw, K, 1))) return rc;
+  // a tile's rows are stepped through in 32 bits
+  if (lda >= 1 << 24 || ldw >= 1 << 24) return fail(SKSSM_EUNSUPPORTED, "%s: row strides must be less than 2^24", what);
   if (ld_ascale < M) return fail(SKSSM_EINVAL, "%s: a_scale stride %lld is less than %lld rows", what, (long long)ld_ascale, (long long)M);
   if (ldy < N) return fail(SKSSM_EINVAL, "%s: y stride %lld is less than %d columns", what, (long long)ldy, N);
   if (!w || !w_scale || (M > 0 && (!a || !a_scale || !y))) return fail(SKSSM_EINVAL, "%s: a, w, their scales and y are required", what);

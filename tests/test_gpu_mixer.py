@@ -364,6 +364,25 @@ def test_matmul(M, N, K):
     R.close(ops.matmul_fp8(a, sa, w, sw), y, bound + top * 2.0 ** -11 + y.abs() * R.U16, "bf16")
 
 
+@pytest.mark.parametrize("M,N,K", [(4096, 4096, 256), (4000, 4600, 272), (130, 70000, 144), (5100, 3600, 128)])
+def test_matmul_many_tiles(M, N, K):
+    """Enough tiles for the widest kernel, with rows, columns and a block past
+    its tiles' ends; some rows of every tile of rows are checked over all columns."""
+    case("matmul many", M, N, K)
+    r = rnd(M)
+    kb, nb = -(-K // 128), -(-N // 128)
+    a, w = fp8(r, (M, K)), fp8(r, (N, K))
+    sa, sw = torch.exp(r((kb, M))), torch.exp(r((nb, kb)))
+    y = ops.matmul_fp8(a, sa, w, sw)
+    yf = ops.matmul_fp8(a, sa, w, sw, out_dtype=torch.float32)
+    rows = torch.tensor(sorted({m for t in range(0, M, 256) for m in (t, t + 77, t + 255)} & set(range(M)) | {M - 1}), device="cuda")
+    want, mag, top = R.matmul(a.float()[rows].to(ops.F8), sa[:, rows], w, sw)
+    bound = (128 + K / 128 + 4) * R.U32 * mag
+    R.close(yf[rows], want, bound, "f32")
+    R.close(y[rows], want, bound + top * 2.0 ** -11 + want.abs() * R.U16, "bf16")
+    assert bool(torch.isfinite(y).all())
+
+
 @pytest.mark.parametrize("M,N,K", [(5, 96, 256), (140, 272, 320), (600, 400, 272)])
 def test_matmul_strides_and_neighbours(M, N, K):
     """Strided rows of every matrix; what lies between them is neither read (NaN) nor written."""
