@@ -94,7 +94,7 @@ int sketchssm_scan(const skssm_config* cfg, int32_t groups, int64_t tokens, cons
                    int64_t ldx, const void* b, int64_t ldb, const void* c, int64_t ldc, const void* dt, int64_t lddt,
                    const float* dt_bias, const float* A, const float* D, const float* S_in, float* S_out, void* y,
                    int64_t ldy, void* workspace, size_t workspace_bytes, void* stream);
-size_t sketchssm_scan_workspace(const skssm_config* cfg, int64_t tokens);
+size_t sketchssm_scan_workspace(const skssm_config* cfg, int32_t groups, int64_t tokens);
 
 /*
  * sketchssm_norm -- root-mean-square norm over groups of columns:

@@ -120,7 +120,7 @@ def load(path: str | None = None):
     lib.sketchssm_matmul_fp8.argtypes = [i64, i32, i32, P, i64, P, i64, P, i64, P, i32, P, i64, P, size, P]
     for f in ("sketchssm_conv", "sketchssm_conv_token", "sketchssm_scan", "sketchssm_norm", "sketchssm_matmul_fp8"):
         getattr(lib, f).restype = ctypes.c_int
-    lib.sketchssm_scan_workspace.argtypes = [cfgp, i64]
+    lib.sketchssm_scan_workspace.argtypes = [cfgp, i32, i64]
     lib.sketchssm_matmul_fp8_workspace.argtypes = [i64, i32, i32]
     lib.sketchssm_scan_workspace.restype = lib.sketchssm_matmul_fp8_workspace.restype = size
     _lib = lib

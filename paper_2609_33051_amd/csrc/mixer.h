@@ -131,6 +131,6 @@ struct ScanArgs {
   float* work;
 };
 int run_scan(const ScanArgs& a, int K, int V, int io, void* stream);
-size_t scan_workspace(int batch, int tokens, int H, int K, int V);
+size_t scan_workspace(int batch, int tokens, int H, int G, int K, int V);
 
 }  // namespace skssm

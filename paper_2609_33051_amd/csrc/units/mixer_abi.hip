@@ -146,9 +146,9 @@ int sketchssm_conv_token(const skssm_config* cfg, int32_t groups, int32_t width,
   return launched(skssm::run_conv_token(a, width, cfg->io_dtype, stream), what);
 }
 
-size_t sketchssm_scan_workspace(const skssm_config* cfg, int64_t tokens) {
-  if (skssm::check_shape(cfg, false, true) || tokens < 0 || tokens > kMaxTokens) return 0;
-  return skssm::scan_workspace(cfg->batch, (int)tokens, cfg->heads, cfg->dk, cfg->dv);
+size_t sketchssm_scan_workspace(const skssm_config* cfg, int32_t groups, int64_t tokens) {
+  if (check_groups("sketchssm_scan_workspace", cfg, groups) || tokens < 0 || tokens > kMaxTokens) return 0;
+  return skssm::scan_workspace(cfg->batch, (int)tokens, cfg->heads, groups, cfg->dk, cfg->dv);
 }
 
 int sketchssm_scan(const skssm_config* cfg, int32_t groups, int64_t tokens, const int32_t* offsets, const void* x,
@@ -172,7 +172,7 @@ int sketchssm_scan(const skssm_config* cfg, int32_t groups, int64_t tokens, cons
       (rc = check_stride(what, "c", ldc, GK, e)) || (rc = check_stride(what, "y", ldy, HV, e)))
     return rc;
   if (lddt < H) return fail(SKSSM_EINVAL, "%s: dt stride %lld is less than %lld heads", what, (long long)lddt, (long long)H);
-  const size_t need = skssm::scan_workspace(cfg->batch, (int)tokens, cfg->heads, cfg->dk, cfg->dv);
+  const size_t need = skssm::scan_workspace(cfg->batch, (int)tokens, cfg->heads, groups, cfg->dk, cfg->dv);
   if (need && (!workspace || workspace_bytes < need))
     return fail(SKSSM_EINVAL, "%s: workspace of %zu bytes, %zu needed", what, workspace ? workspace_bytes : (size_t)0, need);
   const size_t states = (size_t)cfg->batch * HV * cfg->dk * 4;

@@ -3,9 +3,10 @@
 // S the state before it,
 //     y_t = e^{g_t} S C_t + sum_{s <= t} e^{g_t - g_s} dt_s <B_s, C_t> x_s + D x_t,
 //     S' = e^{g_L} S + sum_s (e^{g_L - g_s} dt_s x_s) B_s^T,
-// every exponent <= 0.  A workgroup of four waves owns a head and a run of tokens
-// and goes through it chunk by chunk; the state stays in its registers (V / 4
-// value channels a wave) and each input is read once.
+// every exponent <= 0.  A workgroup of four waves owns 128 value channels (one
+// head, or two of a group: the scores <B_s, C_t> are theirs together) and a run of
+// tokens, and goes through it chunk by chunk; the state stays in registers (32 value
+// channels a wave) and each input is read once, a chunk ahead.
 //
 // Fragments.  Both operands of a product hold, per lane, 8 consecutive indices of
 // a 32-deep reduction (lane group g = lane / 16: 8 g .. 8 g + 7) of the row or
@@ -13,16 +14,21 @@
 // that two of them are such a fragment as they lie: tile kt, row m is channel
 // 32 (kt / 2) + 8 (m / 4) + 4 (kt % 2) + m % 4.
 //
-// Few sequences: a sequence is split into segments of `seg` tokens.  A first
-// launch runs the state part of every segment but a sequence's last, from zero
-// (the first: from S_in), and keeps its end state and total decay; the second
-// begins each segment from the states before it, joined.
+// Long sequences: a sequence is split into segments of `seg` tokens, a fair
+// share of the card.  A first launch runs the state part of every segment but a
+// sequence's last, from zero (the first: from S_in), and keeps its end state and
+// total decay; the second begins each segment from the states before it, joined.
+#include <type_traits>
+
 #include "../mixer.h"
 
 namespace skssm {
 
 constexpr int kChunk = 64;
+constexpr int kValues = 128;        // value channels of a workgroup
 constexpr int kGates = 4 * kChunk;  // tokens whose gates are computed together, a chunk per wave
+// places in a chunk's record of gates (floats)
+constexpr int kLeft = 0, kEnd = 64, kLocalRecord = 68, kLocal = 68, kStep = 196, kGate = 260, kPass = 324, kRecord = 420;
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short shortx4 __attribute__((ext_vector_type(4)));
@@ -45,18 +51,23 @@ struct FragF32 { float e[8]; };
 template <typename IO> struct Frags;
 template <> struct Frags<bf16_t> {
   using F = bf16x8;
-  // 8 consecutive columns of one row
-  template <int COLS> static __device__ __forceinline__ F row(const char* t, int row, int col) {
-    return __builtin_bit_cast(F, *reinterpret_cast<const uint4*>(t + Tile<bf16_t, COLS>::at(row, col)));
+  // 8 consecutive columns of one row, from the places of its 16-byte chunks
+  static __device__ __forceinline__ F row(const char* t, const uint32_t* at, int off) {
+    return __builtin_bit_cast(F, *reinterpret_cast<const uint4*>(t + at[0] + off));
   }
-  // 8 consecutive rows (row0 ..) of the column that the lane's place i = lane % 16 stands
-  // for, where places 4 p .. 4 p + 3 are columns col(p) .. col(p) + 3: a transposed read takes,
-  // from the lanes of a group, four rows of four 8-byte pieces
-  template <int COLS, class Col> static __device__ __forceinline__ F cols(const char* t, int row0, int i, Col col) {
+  // 8 consecutive rows of the column that the lane's place i = lane % 16 stands for, where
+  // places 4 p .. 4 p + 3 are four consecutive columns: a transposed read takes, from
+  // the 16 lanes of a group, four rows (i / 4) of four 8-byte pieces (i % 4)
+  static constexpr int kCols = 2;  // places a lane holds: of row i / 4 and of row 4 + i / 4
+  template <int COLS> static __device__ __forceinline__ void cols_at(uint32_t* at, int row0, int i, int col0, int step) {
+#pragma unroll
+    for (int q = 0; q < 2; ++q) at[q] = Tile<bf16_t, COLS>::at(row0 + 4 * q + (i >> 2), col0 + step * (i & 3));
+  }
+  // (odd: the same places four columns on, the other half of their chunks)
+  static __device__ __forceinline__ F cols(const char* t, const uint32_t* at, int off, int odd) {
     typedef __attribute__((address_space(3))) shortx4* lds4;
-    const int r = row0 + (i >> 2), c = col(i & 3);
-    const shortx4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(t + Tile<bf16_t, COLS>::at(r, c)));
-    const shortx4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(t + Tile<bf16_t, COLS>::at(r + 4, c)));
+    const shortx4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(t + at[0] + off + 8 * odd));
+    const shortx4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(t + at[1] + off + 8 * odd));
     return __builtin_bit_cast(F, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
   }
   static __device__ __forceinline__ floatx4 mma(F a, F b, floatx4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
@@ -69,18 +80,23 @@ template <> struct Frags<bf16_t> {
 };
 template <> struct Frags<float> {
   using F = FragF32;
-  template <int COLS> static __device__ __forceinline__ F row(const char* t, int row, int col) {
+  static __device__ __forceinline__ F row(const char* t, const uint32_t* at, int off) {
     F f;
-    const float4 a = *reinterpret_cast<const float4*>(t + Tile<float, COLS>::at(row, col));
-    const float4 b = *reinterpret_cast<const float4*>(t + Tile<float, COLS>::at(row, col + 4));
+    const float4 a = *reinterpret_cast<const float4*>(t + at[0] + off), b = *reinterpret_cast<const float4*>(t + at[1] + off);
     f.e[0] = a.x; f.e[1] = a.y; f.e[2] = a.z; f.e[3] = a.w;
     f.e[4] = b.x; f.e[5] = b.y; f.e[6] = b.z; f.e[7] = b.w;
     return f;
   }
-  template <int COLS, class Col> static __device__ __forceinline__ F cols(const char* t, int row0, int i, Col col) {
+  static constexpr int kCols = 8;
+  template <int COLS> static __device__ __forceinline__ void cols_at(uint32_t* at, int row0, int i, int col0, int step) {
+#pragma unroll
+    for (int q = 0; q < 8; ++q) at[q] = Tile<float, COLS>::at(row0 + q, col0 + step * (i >> 2) + (i & 3));
+  }
+  // (odd: the same places four columns on, the other chunk of a pair)
+  static __device__ __forceinline__ F cols(const char* t, const uint32_t* at, int off, int odd) {
     F f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) f.e[e] = *reinterpret_cast<const float*>(t + Tile<float, COLS>::at(row0 + e, col(i >> 2) + (i & 3)));
+    for (int e = 0; e < 8; ++e) f.e[e] = *reinterpret_cast<const float*>(t + (at[e] ^ (16 * odd)) + off);
     return f;
   }
   static __device__ __forceinline__ floatx4 mma(const F& a, const F& b, floatx4 c) {
@@ -99,35 +115,40 @@ template <> struct Frags<float> {
   }
 };
 
-// x weighted per token, as the state's update takes it: fp32, or two bf16 parts that
-// hold 16 bits of the product (what enters the state is not rounded to one bf16).
+// x weighted per token, as the state's update takes it: fp32, or three bf16 parts that
+// hold the product's 24 bits (two leave the state 2e-6 off, six times what fp32
+// sums do).
 template <typename IO> struct Weighted;
 template <> struct Weighted<float> {
+  static constexpr int kParts = 1;
   FragF32 f;
   __device__ __forceinline__ void set(const FragF32& x, const float* w) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) f.e[e] = x.e[e] * w[e];
   }
-  __device__ __forceinline__ floatx4 mma(const FragF32& a, floatx4 c) const { return Frags<float>::mma(a, f, c); }
+  __device__ __forceinline__ const FragF32& part(int) const { return f; }
 };
 template <> struct Weighted<bf16_t> {
-  bf16x8 hi, lo;
+  static constexpr int kParts = 3;
+  uint4 p[kParts];
   __device__ __forceinline__ void set(bf16x8 x, const float* w) {
     const uint4 u = __builtin_bit_cast(uint4, x);
     const uint32_t in[4] = {u.x, u.y, u.z, u.w};
-    uint32_t h[4], l[4];
+    uint32_t h[kParts][4];
 #pragma unroll
-    for (int p = 0; p < 4; ++p) {
-      const float a = bf16_lo(in[p]) * w[2 * p], b = bf16_hi(in[p]) * w[2 * p + 1];
-      h[p] = bf16_pack2(a, b);
-      l[p] = bf16_pack2(a - bf16_lo(h[p]), b - bf16_hi(h[p]));
+    for (int q = 0; q < 4; ++q) {
+      float a = bf16_lo(in[q]) * w[2 * q], b = bf16_hi(in[q]) * w[2 * q + 1];
+#pragma unroll
+      for (int k = 0; k < kParts; ++k) {
+        h[k][q] = bf16_pack2(a, b);
+        a -= bf16_lo(h[k][q]);
+        b -= bf16_hi(h[k][q]);
+      }
     }
-    hi = __builtin_bit_cast(bf16x8, make_uint4(h[0], h[1], h[2], h[3]));
-    lo = __builtin_bit_cast(bf16x8, make_uint4(l[0], l[1], l[2], l[3]));
+#pragma unroll
+    for (int k = 0; k < kParts; ++k) p[k] = make_uint4(h[k][0], h[k][1], h[k][2], h[k][3]);
   }
-  __device__ __forceinline__ floatx4 mma(bf16x8 a, floatx4 c) const {
-    return Frags<bf16_t>::mma(a, lo, Frags<bf16_t>::mma(a, hi, c));
-  }
+  __device__ __forceinline__ bf16x8 part(int k) const { return __builtin_bit_cast(bf16x8, p[k]); }
 };
 
 // A segment of a sequence.  Slots 0 .. batch-1 are the sequences' first segments;
@@ -163,15 +184,24 @@ struct Segment {
 
 // LOCAL: the state part alone, over the segment before the slot's (first launch).
 template <typename IO, int K, int V, bool LOCAL>
-__global__ __launch_bounds__(256) void scan_kernel(ScanArgs a, int seg, bool apart) {
+__global__ __launch_bounds__(256, sizeof(IO) == 2 ? 2 : 1) void scan_kernel(ScanArgs a, int seg, bool apart) {
   using FR = Frags<IO>;
   using F = typename FR::F;
   using TB = Tile<IO, K>;
-  using TX = Tile<IO, V>;
+  using TX = Tile<IO, kValues>;
   using TM = Tile<IO, kChunk>;
-  constexpr int KT = K / 16, KF = K / 32, VT = V / 64, PER = TB::kPer;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, i = lane & 15, g = lane >> 4;
-  const int h = blockIdx.x % a.H, slot = blockIdx.x / a.H, grp = h / (a.H / a.G);
+  constexpr int KT = K / 16, KF = K / 32, HEADS = kValues / V, PER = TB::kPer, ROW = (int)sizeof(IO) * 16;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, g = lane >> 4;
+  // workgroups go round the eight XCDs: each takes a run of heads, whose groups' B and C stay in its L2
+  const int per_group = a.H / a.G, parts = a.G * ((per_group + HEADS - 1) / HEADS);
+  const int slot = blockIdx.x / parts;
+  int part = blockIdx.x % parts;
+  if (parts % 8 == 0) part = (part % 8) * (parts / 8) + part / 8;
+  const int grp = part / ((per_group + HEADS - 1) / HEADS), first = (part % ((per_group + HEADS - 1) / HEADS)) * HEADS;
+  const int h0 = grp * per_group + first, heads = min(HEADS, per_group - first);
+  const int hl = HEADS == 2 ? wave >> 1 : 0;             // the wave's head among the workgroup's
+  const bool mine = hl < heads;                          // (an odd group's last workgroup has one head)
+  const int h = h0 + (mine ? hl : 0), vbase = HEADS == 2 ? 32 * (wave & 1) : 32 * wave;
 
   Segment s;
   if (LOCAL) {
@@ -190,290 +220,340 @@ __global__ __launch_bounds__(256) void scan_kernel(ScanArgs a, int seg, bool apa
   char* const lx = lb + TB::kBytes;
   char* const lc = lx + TX::kBytes;
   char* const lm = lc + TB::kBytes;
-  float* const gates = reinterpret_cast<float*>(LOCAL ? lc : lm + TM::kBytes);
-  float* const ghi = gates;             // g of the chunk in two parts, log2
-  float* const glo = gates + kGates;
-  float* const gdt = gates + 2 * kGates;
-  float* const get = gates + 3 * kGates;  // 2^{g_t}
-  float* const gws = gates + 4 * kGates;  // dt_s 2^{g_L - g_s}
-  float* const gend = gates + 5 * kGates; // g_L of the four chunks
+  float* const gates = reinterpret_cast<float*>(LOCAL ? lc : lm + HEADS * TM::kBytes);
 
-  // channels of the lane's pieces: value channels of place 4 p, key channels of tile kt
-  auto vcol = [&](int u, int p) { return VT == 2 ? 32 * wave + 8 * p + 4 * u : 16 * wave + 4 * p; };
-  auto kcol = [&](int kt, int p) { return 32 * (kt >> 1) + 8 * p + 4 * (kt & 1); };
-  // the lane's four values (v = place i, channels of group g) of tile (u, kt) in a tile-major state
+  // channels: the lane's four state values (v of place i, k of group g) of tile (u, kt) in a tile-major state
   auto state_at = [&](int u, int kt) {
-    const int v = vcol(u, i >> 2) + (i & 3), k = kcol(kt, g);
+    const int v = vbase + 8 * (i >> 2) + 4 * u + (i & 3), k = 32 * (kt >> 1) + 8 * g + 4 * (kt & 1);
     return ((v >> 4) * (K / 16) + (k >> 4)) * 256 + 4 * ((v & 15) + 16 * ((k & 15) >> 2));
   };
   auto work_at = [&](int j) { return a.work + ((size_t)(j - 1) * a.H + h) * (V * K); };  // before segment start j
   float* const decays = a.work ? a.work + (size_t)(a.seq.tokens / seg) * a.H * (V * K) : nullptr;
-  auto own_at = [&](int u, int kt) { return (((wave * VT + u) * KT + kt) * 64 + lane) * 4; };
 
-  floatx4 S[VT][KT];
+  floatx4 S[2][KT];
+#pragma unroll
+  for (int u = 0; u < 2; ++u)
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt) S[u][kt] = floatx4{0.f, 0.f, 0.f, 0.f};
   if (s.k == 0) {
-    const float* in = a.S_in ? a.S_in + ((size_t)s.b * a.H + h) * (V * K) : nullptr;
+    if (a.S_in) {
+      const float* in = a.S_in + ((size_t)s.b * a.H + h) * (V * K);
 #pragma unroll
-    for (int u = 0; u < VT; ++u)
+      for (int u = 0; u < 2; ++u)
 #pragma unroll
-      for (int kt = 0; kt < KT; ++kt) S[u][kt] = in ? *reinterpret_cast<const floatx4*>(in + state_at(u, kt)) : floatx4{0.f, 0.f, 0.f, 0.f};
-  } else {
+        for (int kt = 0; kt < KT; ++kt) S[u][kt] = *reinterpret_cast<const floatx4*>(in + state_at(u, kt));
+    }
+  } else if (!LOCAL) {
+    for (int k = 0; k < s.k; ++k) {  // the segments before this one, in order
+      const int j = (int)(((int64_t)s.lo + (int64_t)(k + 1) * seg) / seg);
+      const float* w = work_at(j);
+      const float d = k ? __builtin_amdgcn_exp2f(decays[(size_t)(j - 1) * a.H + h]) : 0.f;
 #pragma unroll
-    for (int u = 0; u < VT; ++u)
+      for (int u = 0; u < 2; ++u)
 #pragma unroll
-      for (int kt = 0; kt < KT; ++kt) S[u][kt] = floatx4{0.f, 0.f, 0.f, 0.f};
-    if (!LOCAL) {
-      for (int k = 0; k < s.k; ++k) {  // the segments before this one, in order
-        const int j = (int)(((int64_t)s.lo + (int64_t)(k + 1) * seg) / seg);
-        const float* w = work_at(j);
-        const float d = k ? __builtin_amdgcn_exp2f(decays[(size_t)(j - 1) * a.H + h]) : 0.f;
+        for (int kt = 0; kt < KT; ++kt) {
+          const floatx4 t = *reinterpret_cast<const floatx4*>(w + state_at(u, kt));
 #pragma unroll
-        for (int u = 0; u < VT; ++u)
-#pragma unroll
-          for (int kt = 0; kt < KT; ++kt) {
-            const floatx4 t = *reinterpret_cast<const floatx4*>(w + own_at(u, kt));
-#pragma unroll
-            for (int e = 0; e < 4; ++e) S[u][kt][e] = k ? fmaf(S[u][kt][e], d, t[e]) : t[e];
-          }
-      }
+          for (int e = 0; e < 4; ++e) S[u][kt][e] = k ? fmaf(S[u][kt][e], d, t[e]) : t[e];
+        }
     }
   }
 
-  // a chunk's rows in registers on their way to LDS: 16-byte pieces, zero past the segment
-  constexpr int NB = kChunk * TB::kChunks / 256, NX = kChunk * TX::kChunks / 256;
+  // A chunk's rows in registers on their way to LDS, 16-byte pieces, zero past the
+  // segment: 256 threads take 256 / kChunks rows at a time.
+  constexpr int RB = 256 / TB::kChunks, RX = 256 / TX::kChunks, NB = kChunk / RB, NX = kChunk / RX;
+  const int rb = tid / TB::kChunks, cb = (tid % TB::kChunks) * PER, rx = tid / TX::kChunks, cx = (tid % TX::kChunks) * PER;
+  const int xload = cx < heads * V ? cx : 0;  // (a missing head's columns: any values, its results are not stored)
+  const uint32_t ob = (uint32_t)((rb * a.ldb + cb) * sizeof(IO)), oc = (uint32_t)((rb * a.ldc + cb) * sizeof(IO)),
+                 ox = (uint32_t)((rx * a.ldx + xload) * sizeof(IO));
+  const char* const b0 = static_cast<const char*>(a.b) + (size_t)grp * K * sizeof(IO);
+  const char* const c0 = static_cast<const char*>(a.c) + (size_t)grp * K * sizeof(IO);
+  const char* const x0 = static_cast<const char*>(a.x) + (size_t)h0 * V * sizeof(IO);
   uint4 pb[NB], pc[NB], px[NX];
   auto fetch = [&](int p) {
     const int n = s.p1 - p;
+    auto rows = [&](auto all) {
+      constexpr bool ALL = decltype(all)::value;
 #pragma unroll
-    for (int q = 0; q < NB; ++q) {
-      const int at = q * 256 + tid, row = at / TB::kChunks, c = (at % TB::kChunks) * PER;
-      pb[q] = make_uint4(0, 0, 0, 0);
-      if (!LOCAL) pc[q] = make_uint4(0, 0, 0, 0);
-      if (row < n) {
-        pb[q] = *reinterpret_cast<const uint4*>(static_cast<const IO*>(a.b) + (size_t)(p + row) * a.ldb + grp * K + c);
-        if (!LOCAL) pc[q] = *reinterpret_cast<const uint4*>(static_cast<const IO*>(a.c) + (size_t)(p + row) * a.ldc + grp * K + c);
+      for (int q = 0; q < NB; ++q) {
+        const size_t row = (size_t)(p + q * RB) * sizeof(IO);
+        if (!ALL) pb[q] = pc[q] = make_uint4(0, 0, 0, 0);
+        if (ALL || q * RB + rb < n) {
+          pb[q] = *reinterpret_cast<const uint4*>(b0 + row * a.ldb + ob);
+          if (!LOCAL) pc[q] = *reinterpret_cast<const uint4*>(c0 + row * a.ldc + oc);
+        }
       }
-    }
 #pragma unroll
-    for (int q = 0; q < NX; ++q) {
-      const int at = q * 256 + tid, row = at / TX::kChunks, c = (at % TX::kChunks) * PER;
-      px[q] = make_uint4(0, 0, 0, 0);
-      if (row < n) px[q] = *reinterpret_cast<const uint4*>(static_cast<const IO*>(a.x) + (size_t)(p + row) * a.ldx + (size_t)h * V + c);
-    }
+      for (int q = 0; q < NX; ++q) {
+        if (!ALL) px[q] = make_uint4(0, 0, 0, 0);
+        if (ALL || q * RX + rx < n) px[q] = *reinterpret_cast<const uint4*>(x0 + (size_t)(p + q * RX) * sizeof(IO) * a.ldx + ox);
+      }
+    };
+    if (n >= kChunk) rows(std::true_type{});
+    else rows(std::false_type{});
   };
   auto put = [&]() {
 #pragma unroll
     for (int q = 0; q < NB; ++q) {
-      const int at = q * 256 + tid, row = at / TB::kChunks, c = (at % TB::kChunks) * PER;
-      *reinterpret_cast<uint4*>(lb + TB::at(row, c)) = pb[q];
-      if (!LOCAL) *reinterpret_cast<uint4*>(lc + TB::at(row, c)) = pc[q];
+      *reinterpret_cast<uint4*>(lb + TB::at(q * RB + rb, cb)) = pb[q];
+      if (!LOCAL) *reinterpret_cast<uint4*>(lc + TB::at(q * RB + rb, cb)) = pc[q];
     }
 #pragma unroll
-    for (int q = 0; q < NX; ++q) {
-      const int at = q * 256 + tid, row = at / TX::kChunks, c = (at % TX::kChunks) * PER;
-      *reinterpret_cast<uint4*>(lx + TX::at(row, c)) = px[q];
-    }
+    for (int q = 0; q < NX; ++q) *reinterpret_cast<uint4*>(lx + TX::at(q * RX + rx, cx)) = px[q];
   };
-  // step sizes and decays of four chunks.  Sums of log decays run in 64 bits: a token that
-  // forgets everything (held to 2^-150, which is 0 in fp32) must not blur the differences
-  // of those after it.
-  const float A2 = a.A[h] * 1.44269504f, bias = a.dt_bias ? a.dt_bias[h] : 0.f;
+
+  // Step sizes and decays of four chunks, a chunk per wave.  Sums of log decays run in
+  // 64 bits: a token that forgets everything (held to 2^-150, which is 0 in fp32)
+  // must not blur the differences of those after it.  A chunk's record, in LDS, with
+  // the tile of 16 tokens t / 16 = w and G(w) the sum before it, base 2:
+  //   kLocal  g_t - G(w) in two parts       kStep  dt_t            kGate  2^{g_t}
+  //   kPass   dt_s 2^{G(w) - g_s} of the tokens s before tile w = 1, 2, 3
+  //   kLeft   dt_s 2^{g_L - g_s}            kEnd   g_L
+  // LOCAL keeps kLeft and kEnd.
+  auto record = [&](int head, int chunk) { return gates + (head * 4 + chunk) * (LOCAL ? kLocalRecord : kRecord); };
   auto gate = [&](int p) {
-    const int t = p + tid;
-    float dt = 0.f, la = 0.f;
-    if (t < s.p1) {
-      dt = softplus(ld_elem(static_cast<const IO*>(a.dt) + (size_t)t * a.lddt + h) + bias);
-      la = fmaxf(dt * A2, -150.f);
-    }
-    double sum = (double)la;
+    for (int q = 0; q < heads; ++q) {
+      const int t = p + tid, hh = h0 + q;
+      float dt = 0.f, la = 0.f;
+      if (t < s.p1) {
+        dt = softplus(ld_elem(static_cast<const IO*>(a.dt) + (size_t)t * a.lddt + hh) + (a.dt_bias ? a.dt_bias[hh] : 0.f));
+        la = fmaxf(dt * a.A[hh] * 1.44269504f, -150.f);
+      }
+      double sum = (double)la;
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const double up = __shfl_up(sum, o);
-      if (lane >= o) sum += up;
-    }
-    const double end = __shfl(sum, 63);
-    const float hi = (float)sum;
-    ghi[tid] = hi;
-    glo[tid] = (float)(sum - (double)hi);
-    gdt[tid] = dt;
-    get[tid] = __builtin_amdgcn_exp2f(hi);
-    gws[tid] = dt * __builtin_amdgcn_exp2f((float)(end - sum));
-    if (lane == 0) gend[wave] = (float)end;
-  };
-
-  float total = 0.f;
-  if (s.p0 < s.p1) fetch(s.p0);
-  int part = 0;
-  for (int p = s.p0; p < s.p1; p += kChunk, part = (part + 1) & 3) {
-    __syncthreads();
-    put();
-    if (part == 0) gate(p);
-    __syncthreads();
-    if (p + kChunk < s.p1) fetch(p + kChunk);
-    const int go = part * kChunk, n = s.p1 - p;
-
-    if constexpr (!LOCAL) {
-      // scores of the wave's 16 tokens t (place i) against s <= t, with decay and step: rows of M
-      const int t = 16 * wave + i;
-      F ct[KF];
-#pragma unroll
-      for (int kf = 0; kf < KF; ++kf) ct[kf] = FR::template row<K>(lc, t, 32 * kf + 8 * g);
-      const float th = ghi[go + t], tl = glo[go + t];
-#pragma unroll
-      for (int st = 0; st < 4; ++st) {
-        if (st > (wave | 1)) continue;  // (pairs of tiles: a fragment of M is 32 tokens deep)
-        floatx4 m = {0.f, 0.f, 0.f, 0.f};
-        if (st <= wave) {
-#pragma unroll
-          for (int kf = 0; kf < KF; ++kf) m = FR::mma(FR::template row<K>(lb, 16 * st + i, 32 * kf + 8 * g), ct[kf], m);
-          const int s0 = 16 * st + 4 * g;
-          const float4 sh = *reinterpret_cast<const float4*>(ghi + go + s0), sl = *reinterpret_cast<const float4*>(glo + go + s0),
-                       sd = *reinterpret_cast<const float4*>(gdt + go + s0);
-          const float h4[4] = {sh.x, sh.y, sh.z, sh.w}, l4[4] = {sl.x, sl.y, sl.z, sl.w}, d4[4] = {sd.x, sd.y, sd.z, sd.w};
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            m[e] = s0 + e <= t ? m[e] * d4[e] * __builtin_amdgcn_exp2f((th - h4[e]) + (tl - l4[e])) : 0.f;
-        }
-        FR::store4(lm, TM::at(t, 16 * st + 4 * g), m[0], m[1], m[2], m[3]);
+      for (int o = 1; o < 64; o <<= 1) {
+        const double up = __shfl_up(sum, o);
+        if (lane >= o) sum += up;
+      }
+      const double end = __shfl(sum, 63);
+      float* r = record(q, wave);
+      r[kLeft + lane] = dt * __builtin_amdgcn_exp2f((float)(end - sum));
+      if (lane == 0) r[kEnd] = (float)end;
+      if (!LOCAL) {
+        const double g1 = __shfl(sum, 15), g2 = __shfl(sum, 31), g3 = __shfl(sum, 47);
+        const double loc = sum - (lane < 16 ? 0.0 : lane < 32 ? g1 : lane < 48 ? g2 : g3);
+        const float hi = (float)loc;
+        r[kLocal + lane] = hi;
+        r[kLocal + 64 + lane] = (float)(loc - (double)hi);
+        r[kStep + lane] = dt;
+        r[kGate + lane] = __builtin_amdgcn_exp2f((float)sum);
+        if (lane < 16) r[kPass + lane] = dt * __builtin_amdgcn_exp2f((float)(g1 - sum));
+        if (lane < 32) r[kPass + 16 + lane] = dt * __builtin_amdgcn_exp2f((float)(g2 - sum));
+        if (lane < 48) r[kPass + 48 + lane] = dt * __builtin_amdgcn_exp2f((float)(g3 - sum));
       }
     }
-    F xt[VT][2];
+  };
+
+  // the lane's places in the tiles: rows i (+ 16 per 16 ROW COLS bytes) of B, C and M, columns of B and x
+  constexpr int NR = (int)sizeof(IO) / 2;  // 16-byte chunks of a fragment's row
+  uint32_t rowat[KF][NR], mrow[2][NR], bcol[KF][FR::kCols], xcol[FR::kCols];
 #pragma unroll
-    for (int u = 0; u < VT; ++u)
+  for (int q = 0; q < NR; ++q) {
 #pragma unroll
-      for (int sf = 0; sf < 2; ++sf) xt[u][sf] = FR::template cols<V>(lx, 32 * sf + 8 * g, i, [&](int q) { return vcol(u, q); });
+    for (int kf = 0; kf < KF; ++kf) rowat[kf][q] = TB::at(i, 32 * kf + 8 * g + 4 * q);
+#pragma unroll
+    for (int sf = 0; sf < 2; ++sf) mrow[sf][q] = hl * TM::kBytes + TM::at(i, 32 * sf + 8 * g + 4 * q);
+  }
+#pragma unroll
+  for (int kf = 0; kf < KF; ++kf) FR::template cols_at<K>(bcol[kf], 8 * g, i, 32 * kf, 8);
+  FR::template cols_at<kValues>(xcol, 8 * g, i, 32 * wave, 8);
+  const uint32_t oy = (uint32_t)((i * a.ldy + vbase + 8 * g) * sizeof(IO));
+  char* const y0 = static_cast<char*>(a.y) + (size_t)h * V * sizeof(IO);
+
+  if (!LOCAL) {  // scores of tokens after t in the 32 that a fragment spans: zero throughout
+    for (int q = tid; q < HEADS * TM::kBytes / 16; q += 256) reinterpret_cast<uint4*>(lm)[q] = make_uint4(0, 0, 0, 0);
+  }
+  float total = 0.f;
+  if (s.p0 < s.p1) fetch(s.p0);
+  int chunk = 0;
+  for (int p = s.p0; p < s.p1; p += kChunk, chunk = (chunk + 1) & 3) {
+    __syncthreads();
+    put();
+    if (chunk == 0) gate(p);
+    __syncthreads();
+    if (p + kChunk < s.p1) fetch(p + kChunk);
+    const float* const rec = record(mine ? hl : 0, chunk);
+
     if constexpr (!LOCAL) {
-      __syncthreads();
-      F sk[VT][KF];
+      // scores of tiles (w, st): tokens t (place i) of tile w against s of tile st <= w, with
+      // decay and step, as rows of M; D on the diagonal.  The ten tiles by wave:
+      // its diagonal one, then 0: (1,0) (2,0)  1: (2,1) (3,0)  2: (3,1)  3: (3,2).
+      const int count = wave < 2 ? 3 : 2;
+      for (int q = 0; q < count; ++q) {
+        const int tw = q == 0 ? wave : wave == 0 ? q : wave == 1 ? q + 1 : 3;
+        const int ts = q == 0 ? wave : wave == 1 ? (q == 1 ? 1 : 0) : wave < 1 ? 0 : wave - 1;
+        floatx4 m = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int u = 0; u < VT; ++u)
+        for (int kf = 0; kf < KF; ++kf)
+          m = FR::mma(FR::row(lb, rowat[kf], ts * ROW * K), FR::row(lc, rowat[kf], tw * ROW * K), m);
+        const int to = TM::at(16 * tw + i, 16 * ts + 4 * g);
+        for (int hh = 0; hh < heads; ++hh) {
+          const float* r = record(hh, chunk);
+          float f[4];
+          if (q == 0) {
+            const float th = r[kLocal + 16 * tw + i], tl = r[kLocal + 64 + 16 * tw + i], D = a.D ? a.D[h0 + hh] : 0.f;
+            const float4 sh = *reinterpret_cast<const float4*>(r + kLocal + 16 * ts + 4 * g),
+                         sl = *reinterpret_cast<const float4*>(r + kLocal + 64 + 16 * ts + 4 * g),
+                         sd = *reinterpret_cast<const float4*>(r + kStep + 16 * ts + 4 * g);
+            const float h4[4] = {sh.x, sh.y, sh.z, sh.w}, l4[4] = {sl.x, sl.y, sl.z, sl.w}, d4[4] = {sd.x, sd.y, sd.z, sd.w};
 #pragma unroll
-        for (int kf = 0; kf < KF; ++kf) sk[u][kf] = FR::of(S[u][2 * kf], S[u][2 * kf + 1]);
-      const float D = a.D ? a.D[h] : 0.f;
+            for (int e = 0; e < 4; ++e) {
+              const int o = 4 * g + e - i;  // s - t
+              f[e] = m[e] * d4[e] * __builtin_amdgcn_exp2f(fminf((th - h4[e]) + (tl - l4[e]), 0.f));
+              f[e] = o > 0 ? 0.f : o == 0 ? f[e] + D : f[e];
+            }
+          } else {
+            const float et = __builtin_amdgcn_exp2f(r[kLocal + 16 * tw + i]);
+            const float4 w4 = *reinterpret_cast<const float4*>(r + kPass + (tw == 1 ? 0 : tw == 2 ? 16 : 48) + 16 * ts + 4 * g);
+            f[0] = m[0] * et * w4.x; f[1] = m[1] * et * w4.y; f[2] = m[2] * et * w4.z; f[3] = m[3] * et * w4.w;
+          }
+          FR::store4(lm + hh * TM::kBytes, to, f[0], f[1], f[2], f[3]);
+        }
+      }
+    }
+    F xt[2][2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int sf = 0; sf < 2; ++sf) xt[u][sf] = FR::cols(lx, xcol, sf * 2 * ROW * kValues, u);
+    if constexpr (!LOCAL) {
+      // y: the state's part first, so that its products run while the scores settle
+      floatx4 y[4][2];
+#pragma unroll
+      for (int tt = 0; tt < 4; ++tt)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) y[tt][u] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int kf = 0; kf < KF; ++kf) {
+        const F s0 = FR::of(S[0][2 * kf], S[0][2 * kf + 1]), s1 = FR::of(S[1][2 * kf], S[1][2 * kf + 1]);
+#pragma unroll
+        for (int tt = 0; tt < 4; ++tt) {
+          const F ct = FR::row(lc, rowat[kf], tt * ROW * K);
+          y[tt][0] = FR::mma(s0, ct, y[tt][0]);
+          y[tt][1] = FR::mma(s1, ct, y[tt][1]);
+        }
+      }
 #pragma unroll
       for (int tt = 0; tt < 4; ++tt) {
-        const int t = 16 * tt + i;
-        floatx4 off[VT], y[VT];
+        const float et = rec[kGate + 16 * tt + i];
 #pragma unroll
-        for (int u = 0; u < VT; ++u) off[u] = y[u] = floatx4{0.f, 0.f, 0.f, 0.f};
+        for (int e = 0; e < 4; ++e) { y[tt][0][e] *= et; y[tt][1][e] *= et; }
+      }
+      __syncthreads();
+      const int n = mine ? s.p1 - p : 0;
 #pragma unroll
-        for (int kf = 0; kf < KF; ++kf) {
-          const F ct = FR::template row<K>(lc, t, 32 * kf + 8 * g);
-#pragma unroll
-          for (int u = 0; u < VT; ++u) off[u] = FR::mma(sk[u][kf], ct, off[u]);
-        }
+      for (int tt = 0; tt < 4; ++tt) {
 #pragma unroll
         for (int sf = 0; sf <= tt / 2; ++sf) {
-          const F mt = FR::template row<kChunk>(lm, t, 32 * sf + 8 * g);
-#pragma unroll
-          for (int u = 0; u < VT; ++u) y[u] = FR::mma(xt[u][sf], mt, y[u]);
+          const F mt = FR::row(lm, mrow[sf], tt * ROW * kChunk);
+          y[tt][0] = FR::mma(xt[0][sf], mt, y[tt][0]);
+          y[tt][1] = FR::mma(xt[1][sf], mt, y[tt][1]);
         }
-        const float et = get[go + t];
-        if (t < n) {
-          IO* dst = static_cast<IO*>(a.y) + (size_t)(p + t) * a.ldy + (size_t)h * V;
+        if (16 * tt + i < n) {
+          IO* dst = reinterpret_cast<IO*>(y0 + (size_t)(p + 16 * tt) * sizeof(IO) * a.ldy + oy);
+          Raw<IO, 8> o;
 #pragma unroll
-          for (int u = 0; u < VT; ++u) {
-            const int v = vcol(u, g);
-            Raw<IO, 4> x;
-            x.load(reinterpret_cast<const IO*>(lx + TX::at(t, v)));
+          for (int u = 0; u < 2; ++u)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) y[u][e] = fmaf(off[u][e], et, y[u][e]) + D * x.get(e);
-            st_elem4(dst + v, y[u][0], y[u][1], y[u][2], y[u][3]);
-          }
+            for (int e = 0; e < 4; e += 2) {
+              if constexpr (sizeof(IO) == 2) o.w[2 * u + e / 2] = bf16_pack2(y[tt][u][e], y[tt][u][e + 1]);
+              else { o.e[4 * u + e] = y[tt][u][e]; o.e[4 * u + e + 1] = y[tt][u][e + 1]; }
+            }
+          o.store(dst);
         }
       }
     }
     // the state: decay, then the chunk's tokens
-    const float end = gend[part], d = __builtin_amdgcn_exp2f(end);
+    const float end = rec[kEnd], d = __builtin_amdgcn_exp2f(end);
     total += end;
 #pragma unroll
-    for (int u = 0; u < VT; ++u)
+    for (int u = 0; u < 2; ++u)
 #pragma unroll
       for (int kt = 0; kt < KT; ++kt) S[u][kt] *= d;
 #pragma unroll
     for (int sf = 0; sf < 2; ++sf) {
-      Weighted<IO> w[VT];
+      Weighted<IO> w[2];
       Vec<8> ws;
-      ws.load(gws + go + 32 * sf + 8 * g);
+      ws.load(rec + kLeft + 32 * sf + 8 * g);
+      w[0].set(xt[0][sf], ws.e);
+      w[1].set(xt[1][sf], ws.e);
 #pragma unroll
-      for (int u = 0; u < VT; ++u) w[u].set(xt[u][sf], ws.e);
+      for (int kt = 0; kt < KT; kt += 2) {
+        const F b0t = FR::cols(lb, bcol[kt / 2], sf * 2 * ROW * K, 0), b1t = FR::cols(lb, bcol[kt / 2], sf * 2 * ROW * K, 1);
 #pragma unroll
-      for (int kt = 0; kt < KT; ++kt) {
-        const F bt = FR::template cols<K>(lb, 32 * sf + 8 * g, i, [&](int q) { return kcol(kt, q); });
-#pragma unroll
-        for (int u = 0; u < VT; ++u) S[u][kt] = w[u].mma(bt, S[u][kt]);
+        for (int k = 0; k < Weighted<IO>::kParts; ++k) {
+          S[0][kt] = FR::mma(b0t, w[0].part(k), S[0][kt]);
+          S[1][kt] = FR::mma(b0t, w[1].part(k), S[1][kt]);
+          S[0][kt + 1] = FR::mma(b1t, w[0].part(k), S[0][kt + 1]);
+          S[1][kt + 1] = FR::mma(b1t, w[1].part(k), S[1][kt + 1]);
+        }
       }
     }
   }
 
+  if (!mine) return;
   if (LOCAL) {
     float* w = work_at(slot + 1);
 #pragma unroll
-    for (int u = 0; u < VT; ++u)
+    for (int u = 0; u < 2; ++u)
 #pragma unroll
-      for (int kt = 0; kt < KT; ++kt) *reinterpret_cast<floatx4*>(w + own_at(u, kt)) = S[u][kt];
-    if (tid == 0) decays[(size_t)slot * a.H + h] = total;
-  } else if (s.p1 == s.hi && a.S_out) {
+      for (int kt = 0; kt < KT; ++kt) *reinterpret_cast<floatx4*>(w + state_at(u, kt)) = S[u][kt];
+    if (vbase == 0 && lane == 0) decays[(size_t)slot * a.H + h] = total;
+  } else if (s.p1 == s.hi) {
     // S_out in place of S_in: other segments' workgroups may still read it, so that a later
     // segment leaves its state where only this workgroup reads, for a copy after the launch
-    const bool keep = apart && s.k > 0;
-    float* out = keep ? work_at(slot - a.seq.batch + 1) : a.S_out + ((size_t)s.b * a.H + h) * (V * K);
+    float* out = apart && s.k > 0 ? work_at(slot - a.seq.batch + 1) : a.S_out + ((size_t)s.b * a.H + h) * (V * K);
 #pragma unroll
-    for (int u = 0; u < VT; ++u)
+    for (int u = 0; u < 2; ++u)
 #pragma unroll
-      for (int kt = 0; kt < KT; ++kt) *reinterpret_cast<floatx4*>(out + (keep ? own_at(u, kt) : state_at(u, kt))) = S[u][kt];
+      for (int kt = 0; kt < KT; ++kt) *reinterpret_cast<floatx4*>(out + state_at(u, kt)) = S[u][kt];
   }
 }
 
 // The end states that a launch in place left in the workspace, into S_out.
-template <int K, int V>
-__global__ __launch_bounds__(256) void scan_states_kernel(ScanArgs a, int seg) {
-  constexpr int KT = K / 16, VT = V / 64;
-  const int h = blockIdx.x % a.H, j = blockIdx.x / a.H + 1, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int i = lane & 15, g = lane >> 4;
+__global__ __launch_bounds__(256) void scan_states_kernel(ScanArgs a, int seg, int size) {
+  const int h = blockIdx.x % a.H, j = blockIdx.x / a.H + 1;
   Segment s;
   if (!s.later(a.seq, j, seg) || s.p1 != s.hi) return;
-  const float* w = a.work + ((size_t)(j - 1) * a.H + h) * (V * K);
-  float* out = a.S_out + ((size_t)s.b * a.H + h) * (V * K);
-  for (int u = 0; u < VT; ++u)
-    for (int kt = 0; kt < KT; ++kt) {
-      const int v = (VT == 2 ? 32 * wave + 8 * (i >> 2) + 4 * u : 16 * wave + 4 * (i >> 2)) + (i & 3);
-      const int k = 32 * (kt >> 1) + 8 * g + 4 * (kt & 1);
-      const int at = ((v >> 4) * (K / 16) + (k >> 4)) * 256 + 4 * ((v & 15) + 16 * ((k & 15) >> 2));
-      *reinterpret_cast<floatx4*>(out + at) = *reinterpret_cast<const floatx4*>(w + (((wave * VT + u) * KT + kt) * 64 + lane) * 4);
-    }
+  const float4* w = reinterpret_cast<const float4*>(a.work + ((size_t)(j - 1) * a.H + h) * size);
+  float4* out = reinterpret_cast<float4*>(a.S_out + ((size_t)s.b * a.H + h) * size);
+  for (int q = threadIdx.x; q < size / 4; q += 256) out[q] = w[q];
 }
 
-// Tokens of a segment: long enough to leave about `kWant` workgroups where one
-// per sequence and head would be fewer, and a multiple of the gates' 256 tokens.
-constexpr int kWant = 1024;
-int scan_segment(int batch, int tokens, int H) {
-  const int64_t items = (int64_t)batch * H;
-  if (items >= kWant) return tokens > 0 ? tokens : 1;
-  int64_t seg = ((int64_t)tokens * H + kWant - 1) / kWant;
+// Tokens of a segment: a fair share of all tokens for each of the two workgroups that a
+// CU holds, in whole gates; sequences no longer than that are not split.
+int scan_parts(int H, int G, int V) { return G * ((H / G + kValues / V - 1) / (kValues / V)); }
+int scan_segment(const Sequences& q, int parts) {
+  constexpr int64_t want = 512;
+  int64_t seg = ((int64_t)q.tokens * parts + want - 1) / want;
   seg = (seg + kGates - 1) / kGates * kGates;
-  return seg < kGates ? kGates : seg > tokens ? (tokens > 0 ? tokens : 1) : (int)seg;
+  const int longest = q.offsets ? q.tokens : q.each;
+  return seg < kGates ? kGates : seg >= longest ? (longest > 0 ? longest : 1) : (int)seg;
 }
+int scan_windows(const Sequences& q, int seg) { return seg < (q.offsets ? q.tokens : q.each) ? q.tokens / seg : 0; }
 
-size_t scan_workspace(int batch, int tokens, int H, int K, int V) {
-  const int seg = scan_segment(batch, tokens, H);
-  if (seg >= tokens) return 0;
-  return (size_t)(tokens / seg) * H * ((size_t)V * K + 1) * sizeof(float);
+size_t scan_workspace(int batch, int tokens, int H, int G, int K, int V) {
+  Sequences q{};
+  q.offsets = reinterpret_cast<const int32_t*>(4);  // lengths unknown: the most that any take
+  q.batch = batch;
+  q.tokens = tokens;
+  const int seg = scan_segment(q, scan_parts(H, G, V));
+  return (size_t)scan_windows(q, seg) * H * ((size_t)V * K + 1) * sizeof(float);
 }
 
 template <typename IO, int K, int V>
 int launch_scan(const ScanArgs& a, hipStream_t s) {
-  const int seg = scan_segment(a.seq.batch, a.seq.tokens, a.H);
-  const int windows = seg < a.seq.tokens ? a.seq.tokens / seg : 0;
+  const int parts = scan_parts(a.H, a.G, V), seg = scan_segment(a.seq, parts), windows = scan_windows(a.seq, seg);
   const bool apart = windows && a.S_in && a.S_in == a.S_out;
-  constexpr size_t gates = (5 * kGates + 4) * sizeof(float);
-  constexpr size_t local = Tile<IO, K>::kBytes + Tile<IO, V>::kBytes + gates;
-  constexpr size_t full = local + Tile<IO, K>::kBytes + Tile<IO, kChunk>::kBytes;
+  constexpr int heads = kValues / V;
+  constexpr size_t local = Tile<IO, K>::kBytes + Tile<IO, kValues>::kBytes;
+  constexpr size_t full = local + Tile<IO, K>::kBytes + heads * Tile<IO, kChunk>::kBytes;
   if (windows)
-    hipLaunchKernelGGL((scan_kernel<IO, K, V, true>), dim3((unsigned)windows * (unsigned)a.H), dim3(256), local, s, a, seg, false);
-  hipLaunchKernelGGL((scan_kernel<IO, K, V, false>), dim3((unsigned)(a.seq.batch + windows) * (unsigned)a.H), dim3(256), full, s, a,
-                     seg, apart);
-  if (apart) hipLaunchKernelGGL((scan_states_kernel<K, V>), dim3((unsigned)windows * (unsigned)a.H), dim3(256), 0, s, a, seg);
+    hipLaunchKernelGGL((scan_kernel<IO, K, V, true>), dim3((unsigned)windows * (unsigned)parts), dim3(256),
+                       local + heads * 4 * kLocalRecord * sizeof(float), s, a, seg, false);
+  hipLaunchKernelGGL((scan_kernel<IO, K, V, false>), dim3((unsigned)(a.seq.batch + windows) * (unsigned)parts), dim3(256),
+                     full + heads * 4 * kRecord * sizeof(float), s, a, seg, apart);
+  if (apart) hipLaunchKernelGGL(scan_states_kernel, dim3((unsigned)windows * (unsigned)a.H), dim3(256), 0, s, a, seg, V * K);
   return 0;
 }
 

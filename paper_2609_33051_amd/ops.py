@@ -151,7 +151,7 @@ def scan(cfg: B.Config, groups: int, x: Tensor, b: Tensor, c: Tensor, dt: Tensor
     if S_out is None:
         S_out = torch.empty(shape, dtype=_F32, device=x.device)
     lib = B.load()
-    need = lib.sketchssm_scan_workspace(cfg, T)
+    need = lib.sketchssm_scan_workspace(cfg, groups, T)
     if workspace is None and need:
         workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
     rc = lib.sketchssm_scan(cfg, groups, T, off, x.data_ptr(), ldx, b.data_ptr(), _matrix("b", b, T, GK, t, dev), c.data_ptr(),

@@ -176,7 +176,7 @@ def test_scan_split_over_workgroups(io, lengths):
     """Few items and long sequences: segments of 256 tokens, some of them of one sequence, states in place and apart."""
     case("scan split", io, lengths)
     H, G, K, V = 2, 1, 128, 64
-    assert B.load().sketchssm_scan_workspace(B.make_config("mamba2", len(lengths), H, K, V, 16, 16, io), sum(lengths)) > 0
+    assert B.load().sketchssm_scan_workspace(B.make_config("mamba2", len(lengths), H, K, V, 16, 16, io), G, sum(lengths)) > 0
     a, S = scan_case(sum(lengths), lengths, H, G, K, V, io)
     y1, S1 = scan_check(a, S, lengths, H, G, K, V, io)
     y2, S2 = scan_check(a, S, lengths, H, G, K, V, io, in_place=True)

@@ -97,12 +97,12 @@ def test_scan_refusals(lib):
     assert scan(lib, y=at(2)) == -1 and scan(lib, s_out=at(3)) == -1 and scan(lib, y=at(7)) == -1
     assert scan(lib, s_in=at(7) + 1024) == -1 and "overlap" in B.sketchssm_last_error()
     # one long sequence is split over workgroups: its workspace is required
-    need = lib.sketchssm_scan_workspace(cfg(batch=1), 1 << 16)
+    need = lib.sketchssm_scan_workspace(cfg(batch=1), 4, 1 << 16)
     assert need > 0
     assert scan(lib, c=cfg(batch=1), T=1 << 16) == -1 and "workspace" in B.sketchssm_last_error()
     assert scan(lib, c=cfg(batch=1), T=1 << 16, ws=at(20), nws=need - 1) == -1
     assert scan(lib, c=cfg(batch=1), T=1 << 16, ws=at(8), nws=need) == -1
-    assert lib.sketchssm_scan_workspace(cfg(batch=1), 64) == 0
+    assert lib.sketchssm_scan_workspace(cfg(batch=1), 4, 64) == 0
 
 
 def norm_args(**kw):
