@@ -34,8 +34,16 @@ struct Sequences {
 };
 
 __device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + fast_exp(-z)); }
-// log(1 + e^r), exact to fp32 where e^r is small against 1 (the step sizes are 1e-3 and less)
-__device__ __forceinline__ float softplus(float r) { return fmaxf(r, 0.f) + log1pf(__expf(-fabsf(r))); }
+// log(1 + e^r) = max(r, 0) + log(1 + e), e = e^{-|r|}, to a few units of fp32 also where e is
+// small (the step sizes are 1e-3 and less): log(1 + e) = 2 artanh(z), z = e / (2 + e) <= 1/3,
+// by its series 2 z (1 + z^2 / 3 + z^4 / 5 + ..), whose ninth term is below 2^-28.
+__device__ __forceinline__ float softplus(float r) {
+  const float e = fast_exp(-fabsf(r)), z = e * __builtin_amdgcn_rcpf(2.f + e), q = z * z;
+  float t = 1.f / 15.f;
+#pragma unroll
+  for (int k = 13; k >= 1; k -= 2) t = fmaf(t, q, 1.f / (float)k);
+  return fmaf(2.f * z, t, fmaxf(r, 0.f));
+}
 
 struct ConvArgs {
   Sequences seq;
