@@ -26,8 +26,17 @@ _F32 = torch.float32
 _IO = {torch.float32: B.F32, torch.bfloat16: B.BF16}
 
 
-def _stream() -> int:
-    return torch.cuda.current_stream().cuda_stream
+# The current device and its current stream's handle: as torch.cuda.current_device()
+# and current_stream(), of which the latter takes 2.9 us (a whole call here, launch
+# included, takes 6 to 10).
+try:
+    from torch._C import _cuda_getCurrentRawStream as _stream
+    from torch._C import _cuda_getDevice as _current
+except ImportError:  # a build of torch without these
+    _current = torch.cuda.current_device
+
+    def _stream(dev: int) -> int:
+        return torch.cuda.current_stream(dev).cuda_stream
 
 
 def _io(x: Tensor) -> int:
@@ -37,23 +46,29 @@ def _io(x: Tensor) -> int:
     return io
 
 
-def _matrix(name: str, x: Tensor, rows: int, columns: int, dtype, dev: int) -> int:
-    """The row stride of a rows x columns matrix whose rows are contiguous."""
-    if x.dim() != 2 or x.shape[0] != rows or x.shape[1] != columns or x.dtype is not dtype or x.get_device() != dev:
-        raise ValueError(f"{name}: a {dtype} tensor [{rows}][{columns}] on cuda:{dev} is needed, not {_said(x)}")
+def _matrix(name: str, x: Tensor, shape: tuple, dtype, dev: int) -> int:
+    """The row stride of a matrix whose rows are contiguous."""
     s = x.stride()
-    if s[1] != 1 and columns > 1:
-        raise ValueError(f"{name}: its rows are not contiguous")
-    return s[0] if rows > 1 and s[0] else max(s[0], columns + -columns * x.element_size() % 16 // x.element_size())
+    if x.shape == shape and x.dtype is dtype and x.get_device() == dev and s[1] == 1 and s[0] >= shape[1] and shape[0] > 1:
+        return s[0]
+    if x.shape != shape or x.dtype is not dtype or x.get_device() != dev:
+        raise ValueError(f"{name}: a {dtype} tensor {list(shape)} on cuda:{dev} is needed, not {_said(x)}")
+    if s[1] != 1 and shape[1] > 1:
+        raise ValueError(f"{name}: its rows are not contiguous ({_said(x)})")
+    if shape[0] > 1 and shape[1] == 1 and s[0] > 0:
+        return s[0]
+    if shape[0] > 1:
+        raise ValueError(f"{name}: its rows overlap ({_said(x)})")
+    return -(-shape[1] // 16) * 16  # at most one row: any stride
 
 
 def _flat(name: str, x: Tensor | None, shape: tuple, dtype, dev: int) -> int | None:
     """The address of a contiguous tensor (None passes)."""
     if x is None:
         return None
-    if x.shape != shape or x.dtype is not dtype or x.get_device() != dev or not x.is_contiguous():
-        raise ValueError(f"{name}: a contiguous {dtype} tensor {list(shape)} on cuda:{dev} is needed, not {_said(x)}")
-    return x.data_ptr()
+    if x.shape == shape and x.dtype is dtype and x.is_contiguous() and x.get_device() == dev:
+        return x.data_ptr()
+    raise ValueError(f"{name}: a contiguous {dtype} tensor {list(shape)} on cuda:{dev} is needed, not {_said(x)}")
 
 
 def _said(x: Tensor) -> str:
@@ -62,7 +77,7 @@ def _said(x: Tensor) -> str:
 
 def _device(x: Tensor) -> int:
     dev = x.get_device()
-    if dev < 0 or dev != torch.cuda.current_device():
+    if dev < 0 or dev != _current():
         raise ValueError(f"{x.device}: tensors on the current GPU are read")
     return dev
 
@@ -92,16 +107,16 @@ def conv(x: Tensor, taps: Tensor, bias: Tensor | None = None, *, offsets: Tensor
     T, C = x.shape
     w = taps.shape[1]
     n, off = _offsets(offsets, batch, dev)
-    ldx = _matrix("x", x, T, C, x.dtype, dev)
+    ldx = _matrix("x", x, (T, C), x.dtype, dev)
     shape = (n, w - 1, C)
     if out is None:
-        out = torch.empty((T, C), dtype=x.dtype, device=x.device)
+        out = x.new_empty((T, C))
     if state_out is None:
-        state_out = torch.empty(shape, dtype=x.dtype, device=x.device)
-    rc = B.load().sketchssm_conv(B.ConvConfig(C, w, io, 1 if silu else 0), n, T, off, x.data_ptr(), ldx,
+        state_out = x.new_empty(shape)
+    rc = (B._lib or B.load()).sketchssm_conv(B.ConvConfig(C, w, io, 1 if silu else 0), n, T, off, x.data_ptr(), ldx,
                                  _flat("taps", taps, (C, w), _F32, dev), _flat("bias", bias, (C,), _F32, dev),
                                  _flat("state", state, shape, x.dtype, dev), _flat("state_out", state_out, shape, x.dtype, dev),
-                                 out.data_ptr(), _matrix("out", out, T, C, x.dtype, dev), _stream())
+                                 out.data_ptr(), _matrix("out", out, (T, C), x.dtype, dev), _stream(dev))
     if rc:
         B._check(rc)
     return out, state_out
@@ -119,12 +134,12 @@ def conv_token(cfg: B.Config, groups: int, x: Tensor, taps: Tensor, bias: Tensor
     C, w, t = H * V + 2 * groups * K, taps.shape[-1], x.dtype
     if _IO[t] != cfg.io_dtype:
         raise ValueError(f"x is {t}: not the io type of the configuration")
-    ldx, lddt = _matrix("x", x, Bt, C, t, dev), _matrix("dt", dt, Bt, H, t, dev)
-    rc = B.load().sketchssm_conv_token(cfg, groups, w, x.data_ptr(), ldx, _flat("taps", taps, (C, w), _F32, dev),
+    ldx, lddt = _matrix("x", x, (Bt, C), t, dev), _matrix("dt", dt, (Bt, H), t, dev)
+    rc = (B._lib or B.load()).sketchssm_conv_token(cfg, groups, w, x.data_ptr(), ldx, _flat("taps", taps, (C, w), _F32, dev),
                                        _flat("bias", bias, (C,), _F32, dev), _flat("state", state, (Bt, w - 1, C), t, dev),
                                        dt.data_ptr(), lddt, _flat("dt_bias", dt_bias, (H,), _F32, dev),
                                        _flat("A", A, (H,), _F32, dev), ring, n_buffered,
-                                       _flat("q", q, (Bt, H, K), t, dev), _stream())
+                                       _flat("q", q, (Bt, H, K), t, dev), _stream(dev))
     if rc:
         B._check(rc)
 
@@ -144,22 +159,22 @@ def scan(cfg: B.Config, groups: int, x: Tensor, b: Tensor, c: Tensor, dt: Tensor
     if _IO[t] != cfg.io_dtype:
         raise ValueError(f"x is {t}: not the io type of the configuration")
     n, off = _offsets(offsets, Bt, dev)
-    ldx = _matrix("x", x, T, H * V, t, dev)
+    ldx = _matrix("x", x, (T, H * V), t, dev)
     shape = (Bt, H, V * K)
     if out is None:
-        out = torch.empty((T, H * V), dtype=t, device=x.device)
+        out = x.new_empty((T, H * V))
     if S_out is None:
-        S_out = torch.empty(shape, dtype=_F32, device=x.device)
-    lib = B.load()
+        S_out = x.new_empty(shape, dtype=_F32)
+    lib = B._lib or B.load()
     need = lib.sketchssm_scan_workspace(cfg, groups, T)
     if workspace is None and need:
-        workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
-    rc = lib.sketchssm_scan(cfg, groups, T, off, x.data_ptr(), ldx, b.data_ptr(), _matrix("b", b, T, GK, t, dev), c.data_ptr(),
-                            _matrix("c", c, T, GK, t, dev), dt.data_ptr(), _matrix("dt", dt, T, H, t, dev),
+        workspace = x.new_empty(need, dtype=torch.uint8)
+    rc = lib.sketchssm_scan(cfg, groups, T, off, x.data_ptr(), ldx, b.data_ptr(), _matrix("b", b, (T, GK), t, dev), c.data_ptr(),
+                            _matrix("c", c, (T, GK), t, dev), dt.data_ptr(), _matrix("dt", dt, (T, H), t, dev),
                             _flat("dt_bias", dt_bias, (H,), _F32, dev), _flat("A", A, (H,), _F32, dev),
                             _flat("D", D, (H,), _F32, dev), _flat("S", S, shape, _F32, dev),
-                            _flat("S_out", S_out, shape, _F32, dev), out.data_ptr(), _matrix("out", out, T, H * V, t, dev),
-                            *_space(workspace, dev), _stream())
+                            _flat("S_out", S_out, shape, _F32, dev), out.data_ptr(), _matrix("out", out, (T, H * V), t, dev),
+                            *_space(workspace, dev), _stream(dev))
     if rc:
         B._check(rc)
     return out, S_out
@@ -193,24 +208,21 @@ def norm(x: Tensor, weight: Tensor, eps: float, *, group: int | None = None, res
     M, N = x.shape
     other = gate if gate is not None else residual
     t = x.dtype if other is None else other.dtype
-    a = B.NormArgs()
-    a.x_dtype = _IO.get(x.dtype, -1)
-    a.io_dtype = _IO.get(t, -1)
     if out_dtype is None:
         out_dtype = t
     f8 = out_dtype is F8
-    a.out_dtype = B.E4M3 if f8 else _IO.get(out_dtype, -1)
-    a.rows, a.columns, a.group, a.eps = M, N, group or N, eps
-    a.x, a.ldx = x.data_ptr(), _matrix("x", x, M, N, x.dtype, dev)
+    io = _IO.get
+    a = B.NormArgs(M, N, group or N, io(x.dtype, -1), io(t, -1), B.E4M3 if f8 else io(out_dtype, -1), 0, eps, x.data_ptr(),
+                   _matrix("x", x, (M, N), x.dtype, dev))
     a.weight = _flat("weight", weight, (N,), _F32, dev)
     if residual is not None:
-        a.residual, a.ld_residual = residual.data_ptr(), _matrix("residual", residual, M, N, t, dev)
+        a.residual, a.ld_residual = residual.data_ptr(), _matrix("residual", residual, (M, N), t, dev)
         if residual_out is None:
-            residual_out = torch.empty((M, N), dtype=t, device=x.device)
+            residual_out = residual.new_empty((M, N))
     if residual_out is not None:
-        a.residual_out, a.ld_residual_out = residual_out.data_ptr(), _matrix("residual_out", residual_out, M, N, t, dev)
+        a.residual_out, a.ld_residual_out = residual_out.data_ptr(), _matrix("residual_out", residual_out, (M, N), t, dev)
     if gate is not None:
-        a.gate, a.ld_gate = gate.data_ptr(), _matrix("gate", gate, M, N, t, dev)
+        a.gate, a.ld_gate = gate.data_ptr(), _matrix("gate", gate, (M, N), t, dev)
     if skip is not None:
         if (skip.dim() != 3 or skip.dtype is not t or skip.get_device() != dev or skip.shape[0] != M
                 or skip.shape[1] * skip.shape[2] != N or skip.stride(2) != 1):
@@ -221,15 +233,19 @@ def norm(x: Tensor, weight: Tensor, eps: float, *, group: int | None = None, res
     elif D is not None:
         raise ValueError("D without skip")
     if out is None:
-        out = torch.empty((M, N), dtype=out_dtype, device=x.device)
-    a.out, a.ld_out = out.data_ptr(), _matrix("out", out, M, N, out_dtype, dev)
+        out, a.ld_out = x.new_empty((M, N), dtype=out_dtype), N
+    else:
+        a.ld_out = _matrix("out", out, (M, N), out_dtype, dev)
+    a.out = out.data_ptr()
     if f8:
         if scales is None:
-            scales = torch.empty((-(-N // 128), M), dtype=_F32, device=x.device)
-        a.scales, a.ld_scales = scales.data_ptr(), max(M, _rows("scales", scales, -(-N // 128), M, dev))
+            scales, a.ld_scales = x.new_empty((-(-N // 128), M), dtype=_F32), M
+        else:
+            a.ld_scales = max(M, _rows("scales", scales, -(-N // 128), M, dev))
+        a.scales = scales.data_ptr()
     elif scales is not None:
         raise ValueError("scales without an 8-bit output")
-    rc = B.load().sketchssm_norm(a, _stream())
+    rc = (B._lib or B.load()).sketchssm_norm(a, _stream(dev))
     if rc:
         B._check(rc)
     return out, scales, residual_out
@@ -255,18 +271,18 @@ def matmul_fp8(a: Tensor, a_scale: Tensor, w: Tensor, w_scale: Tensor, *, out_dt
     N = w.shape[0]
     kb = -(-K // 128)
     if out is None:
-        out = torch.empty((M, N), dtype=out_dtype, device=a.device)
+        out = a.new_empty((M, N), dtype=out_dtype)
     t = out.dtype
     if out.shape != (M, N) or t not in _IO or out.get_device() != dev or out.stride(1) != 1 and N > 1:
         raise ValueError(f"out: a bfloat16 or float32 tensor [{M}][{N}] with contiguous rows is needed, not {_said(out)}")
-    lib = B.load()
+    lib = B._lib or B.load()
     need = lib.sketchssm_matmul_fp8_workspace(M, N, K)
     if workspace is None and need:
-        workspace = torch.empty(need, dtype=torch.uint8, device=a.device)
-    rc = lib.sketchssm_matmul_fp8(M, N, K, a.data_ptr(), _matrix("a", a, M, K, F8, dev), a_scale.data_ptr(),
-                                  max(M, _rows("a_scale", a_scale, kb, M, dev)), w.data_ptr(), _matrix("w", w, N, K, F8, dev),
+        workspace = a.new_empty(need, dtype=torch.uint8)
+    rc = lib.sketchssm_matmul_fp8(M, N, K, a.data_ptr(), _matrix("a", a, (M, K), F8, dev), a_scale.data_ptr(),
+                                  max(M, _rows("a_scale", a_scale, kb, M, dev)), w.data_ptr(), _matrix("w", w, (N, K), F8, dev),
                                   _flat("w_scale", w_scale, (-(-N // 128), kb), _F32, dev), _IO[t], out.data_ptr(),
-                                  out.stride(0) if M > 1 else N, *_space(workspace, dev), _stream())
+                                  out.stride(0) if M > 1 else N, *_space(workspace, dev), _stream(dev))
     if rc:
         B._check(rc)
     return out
