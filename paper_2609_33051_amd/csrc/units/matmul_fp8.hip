@@ -328,7 +328,7 @@ void launch_tiles(const MatmulArgs& p, int splits, hipStream_t s) {
 // round of all CUs has to be full -- what is left over goes to smaller ones.
 // K split (not / by 2 / by 4): 77 x 4096 x 8192, 64x64: 23.7 / 17.5 / 15.5; 16 x 4096 x 8192 23.1 / 16.0 / 11.4; 16 x
 // 4096 x 4096 12.1 / 10.4 / 9.6; 200 x 2048 x 4096 13.8 / 13.2 / 13.6; 100 x 2048 x 2048 8.1 / 8.7 / 8.7: over what fills the
-// CUs, in parts of 8 blocks at least.
+// CUs in parts of 8 blocks at least, or twice that in parts of 16.
 struct MatmulPlan { int wide, rest, splits; };
 MatmulPlan matmul_plan(int M, int N, int K, bool narrow) {
 
@@ -347,7 +347,8 @@ MatmulPlan matmul_plan(int M, int N, int K, bool narrow) {
   const int rest = M > 64 && tiles(128, 64, N) >= cus ? 2 : M > 32 ? 3 : 4;
   const int64_t t = rest == 2 ? tiles(128, 64, N) : rest == 3 ? tiles(64, 64, N) : tiles(32, 64, N);
   const int blocks = (K + 127) / 128;
-  return {0, rest, (int)std::max<int64_t>(1, std::min<int64_t>(blocks / 8, cus / t))};
+  const int64_t once = std::min<int64_t>(blocks / 8, cus / t), twice = std::min<int64_t>(blocks / 16, 2 * cus / t);
+  return {0, rest, (int)std::max<int64_t>({1, once, twice})};
 }
 
 template <typename OUT>
