@@ -51,8 +51,17 @@ __device__ __forceinline__ Raw<IO, 16 / sizeof(IO)> conv_row(const Taps<IO, W>& 
   return y;
 }
 
-constexpr int kConvRows = 32;   // tokens of a workgroup
-constexpr int kConvBatch = 8;   // rows loaded together
+// Tokens of a workgroup, loaded together: 16, or 8 where 16 would leave less than
+// four workgroups a CU.  16384 x 10240 bf16 (four taps): 127.7 us, 5.26 TB/s, what a copy
+// of its size reaches (5.1 to 5.4); two loads of 8 133, 32 tokens as four loads of 8 139,
+// 64 154, and 32 with ordinary loads and stores 150 (nothing here is read twice but
+// the w - 1 tokens before a workgroup's).  777 x 1792 fp32: 6.5 us with 16, 5.4 with 8.
+constexpr int kConvRows = 16, kConvFew = 8;
+
+template <typename IO, int CH> __device__ __forceinline__ void store_nt(const Raw<IO, CH>& r, IO* p) {
+  static_assert(sizeof(r) == 16, "one store");
+  __builtin_nontemporal_store(__builtin_bit_cast(uintx4, r), reinterpret_cast<uintx4*>(p));
+}
 
 // The new state of one sequence and 16 bytes of channels: rows of the old one
 // where the sequence is shorter than w - 1 (row j comes from row j + length, so
@@ -74,7 +83,7 @@ __device__ __forceinline__ void conv_state(const ConvArgs& a, int b, int c) {
   }
 }
 
-template <typename IO, int W, bool SILU>
+template <typename IO, int W, bool SILU, int ROWS>
 __global__ __launch_bounds__(256) void conv_kernel(ConvArgs a, int cols, int tiles) {
   constexpr int CH = 16 / sizeof(IO);
   const int c = ((blockIdx.x % cols) * 256 + threadIdx.x) * CH;
@@ -84,7 +93,7 @@ __global__ __launch_bounds__(256) void conv_kernel(ConvArgs a, int cols, int til
     conv_state<IO, W>(a, part - tiles, c);
     return;
   }
-  const int T = a.seq.tokens, t0 = part * kConvRows, t1 = min(T, t0 + kConvRows);
+  const int T = a.seq.tokens, t0 = part * ROWS, t1 = min(T, t0 + ROWS);
   Taps<IO, W> k;
   k.load(a.taps, a.bias, c);
   const IO* x = static_cast<const IO*>(a.x) + c;
@@ -93,7 +102,7 @@ __global__ __launch_bounds__(256) void conv_kernel(ConvArgs a, int cols, int til
 
   // lo is held to the row (offsets that do not start at 0), so that a state's row index stays in 0..W-2
   int b = a.seq.of(t0), lo = min(t0, a.seq.start(b)), hi = a.seq.start(b + 1);
-  Raw<IO, CH> win[W - 1 + kConvBatch];  // the window, then the batch's rows
+  Raw<IO, CH> win[W - 1 + ROWS];  // the window, then the rows
   // the W - 1 inputs before row t of sequence b
   auto before = [&](int t) {
 #pragma unroll
@@ -104,9 +113,16 @@ __global__ __launch_bounds__(256) void conv_kernel(ConvArgs a, int cols, int til
       else win[j].zero();
     }
   };
+  if (t0 + ROWS <= min(T, hi)) {  // all of one sequence
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) win[W - 1 + i].load_nt(x + (size_t)(t0 + i) * a.ldx);
+    before(t0);
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) store_nt<IO, CH>(conv_row<IO, W, SILU>(k, win + i), y + (size_t)(t0 + i) * a.ldy);
+    return;
+  }
   before(t0);
-  int t = t0;
-  while (t < t1) {
+  for (int t = t0; t < t1;) {
     if (t >= hi && b + 1 < a.seq.batch) {  // the next sequence that has tokens (or the last one)
       do {
         ++b;
@@ -116,36 +132,34 @@ __global__ __launch_bounds__(256) void conv_kernel(ConvArgs a, int cols, int til
       lo = min(t, lo);
       before(t);
     }
-    const int run = (t >= hi ? t1 : min(t1, hi)) - t;  // rows of this sequence here
-    if (run >= kConvBatch) {
+    const int end = t >= hi ? t1 : min(t1, hi);  // of this sequence here
+    for (; t < end; ++t) {
+      win[W - 1].load(x + (size_t)t * a.ldx);
+      store_nt<IO, CH>(conv_row<IO, W, SILU>(k, win), y + (size_t)t * a.ldy);
 #pragma unroll
-      for (int i = 0; i < kConvBatch; ++i) win[W - 1 + i].load(x + (size_t)(t + i) * a.ldx);
-#pragma unroll
-      for (int i = 0; i < kConvBatch; ++i) conv_row<IO, W, SILU>(k, win + i).store(y + (size_t)(t + i) * a.ldy);
-#pragma unroll
-      for (int j = 0; j < W - 1; ++j) win[j] = win[kConvBatch + j];
-      t += kConvBatch;
-    } else {
-      for (int i = 0; i < run; ++i, ++t) {
-        win[W - 1].load(x + (size_t)t * a.ldx);
-        conv_row<IO, W, SILU>(k, win).store(y + (size_t)t * a.ldy);
-#pragma unroll
-        for (int j = 0; j < W - 1; ++j) win[j] = win[j + 1];
-      }
+      for (int j = 0; j < W - 1; ++j) win[j] = win[j + 1];
     }
   }
 }
 
-template <typename IO, int W, bool SILU>
-int launch_conv(const ConvArgs& a, bool apart, hipStream_t s) {
+template <typename IO, int W, bool SILU, int ROWS>
+int launch_conv_rows(const ConvArgs& a, bool apart, hipStream_t s) {
   constexpr int CH = 16 / sizeof(IO);
-  const int cols = (a.C / CH + 255) / 256, tiles = (a.seq.tokens + kConvRows - 1) / kConvRows;
+  const int cols = (a.C / CH + 255) / 256, tiles = (a.seq.tokens + ROWS - 1) / ROWS;
   const int states = a.state_out ? a.seq.batch : 0;
   const unsigned first = (unsigned)cols * (unsigned)(tiles + (apart ? 0 : states));
-  if (first) hipLaunchKernelGGL((conv_kernel<IO, W, SILU>), dim3(first), dim3(256), 0, s, a, cols, tiles);
+  if (first) hipLaunchKernelGGL((conv_kernel<IO, W, SILU, ROWS>), dim3(first), dim3(256), 0, s, a, cols, tiles);
+  // the new states in place of the old ones: after the outputs, which read those
   if (apart && states)
-    hipLaunchKernelGGL((conv_kernel<IO, W, SILU>), dim3((unsigned)cols * (unsigned)states), dim3(256), 0, s, a, cols, 0);
+    hipLaunchKernelGGL((conv_kernel<IO, W, SILU, ROWS>), dim3((unsigned)cols * (unsigned)states), dim3(256), 0, s, a, cols, 0);
   return 0;
+}
+
+template <typename IO, int W, bool SILU>
+int launch_conv(const ConvArgs& a, bool apart, hipStream_t s) {
+  const int64_t cols = (a.C / (16 / (int)sizeof(IO)) + 255) / 256;
+  return cols * a.seq.tokens >= 4 * 256 * kConvRows ? launch_conv_rows<IO, W, SILU, kConvRows>(a, apart, s)
+                                                    : launch_conv_rows<IO, W, SILU, kConvFew>(a, apart, s);
 }
 
 template <typename IO, int W>
@@ -168,37 +182,46 @@ int run_conv(const ConvArgs& a, int width, int io, int silu, bool states_apart, 
   return io == 1 ? launch_conv<bf16_t>(a, width, silu, states_apart, s) : launch_conv<float>(a, width, silu, states_apart, s);
 }
 
-// One token of every request.  Workgroups of request b: first those of the x
+// One token of every request.  Workgroups of RB requests: first those of the x
 // channels (256 threads of 16 bytes each, into ring.v), which also do the
 // gates; then one per group, which convolves the group's B and C once, leaves
 // them in LDS and writes them to every head of the group (ring.k and q): those
 // writes, H (V + 2 K) values a request against the H V + 2 G K that are read, are
-// what the call moves.
-template <typename IO, int W>
+// half of what the call moves.  A thread's taps and bias, 10 bytes for each byte of x,
+// serve RB requests.
+template <typename IO, int W, int RB>
 __global__ __launch_bounds__(256) void conv_token_kernel(ConvTokenArgs a, int xparts) {
   constexpr int CH = 16 / sizeof(IO);
-  const int parts = xparts + a.G, b = blockIdx.x / parts, part = blockIdx.x % parts, tid = threadIdx.x;
+  const int parts = xparts + a.G, b0 = blockIdx.x / parts * RB, part = blockIdx.x % parts, tid = threadIdx.x;
   const int HV = a.H * a.V, GK = a.G * a.K, C = HV + 2 * GK;
-  const IO* x = static_cast<const IO*>(a.x) + (size_t)b * a.ldx;
-  IO* state = static_cast<IO*>(a.state) + (size_t)b * (W - 1) * C;
-  auto conv = [&](int c) {
-    Taps<IO, W> k;
-    Raw<IO, CH> win[W];
-#pragma unroll
-    for (int j = 0; j < W - 1; ++j) win[j].load(state + (size_t)j * C + c);
-    win[W - 1].load(x + c);
-    k.load(a.taps, a.bias, c);
-#pragma unroll
-    for (int j = 0; j < W - 1; ++j) win[j + 1].store(state + (size_t)j * C + c);
-    return conv_row<IO, W, true>(k, win);
-  };
+  auto x = [&](int b) { return static_cast<const IO*>(a.x) + (size_t)b * a.ldx; };
+  auto state = [&](int b) { return static_cast<IO*>(a.state) + (size_t)b * (W - 1) * C; };
   if (part < xparts) {
     const int c = (part * 256 + tid) * CH;
     if (c < HV) {
+      Taps<IO, W> k;
+      Raw<IO, CH> win[RB][W];
+#pragma unroll
+      for (int q = 0; q < RB; ++q) {
+        const int b = min(b0 + q, a.B - 1);
+#pragma unroll
+        for (int j = 0; j < W - 1; ++j) win[q][j].load(state(b) + (size_t)j * C + c);
+        win[q][W - 1].load(x(b) + c);
+      }
+      k.load(a.taps, a.bias, c);
       const int h = c / a.V;
-      conv(c).store(static_cast<IO*>(a.rv) + (((size_t)b * a.H + h) * a.W + a.n) * a.V + (c - h * a.V));
+#pragma unroll
+      for (int q = 0; q < RB; ++q) {
+        const int b = b0 + q;
+        if (b >= a.B) break;
+#pragma unroll
+        for (int j = 0; j < W - 1; ++j) win[q][j + 1].store(state(b) + (size_t)j * C + c);
+        conv_row<IO, W, true>(k, win[q]).store(static_cast<IO*>(a.rv) + (((size_t)b * a.H + h) * a.W + a.n) * a.V + (c - h * a.V));
+      }
     }
-    for (int h = part * 256 + tid; h < a.H; h += xparts * 256) {
+    for (int i = part * 256 + tid; i < RB * a.H; i += xparts * 256) {
+      const int b = b0 + i / a.H, h = i % a.H;
+      if (b >= a.B) break;
       const float r = ld_elem(static_cast<const IO*>(a.dt) + (size_t)b * a.lddt + h) + (a.dt_bias ? a.dt_bias[h] : 0.f);
       const float beta = softplus(r);
       const size_t at = ((size_t)b * a.H + h) * a.W + a.n;
@@ -207,30 +230,48 @@ __global__ __launch_bounds__(256) void conv_token_kernel(ConvTokenArgs a, int xp
     }
     return;
   }
-  __shared__ uint4 row[2 * 128 / CH];
-  const int g = part - xparts, chunks = a.K / CH, rep = a.H / a.G;
-  if (tid < 2 * chunks) {
-    const int side = tid / chunks, c = HV + side * GK + g * a.K + (tid - side * chunks) * CH;
-    conv(c).store(reinterpret_cast<IO*>(&row[tid]));
+  __shared__ uint4 row[RB][2 * 128 / CH];
+  const int g = part - xparts, chunks = a.K / CH, rep = a.H / a.G, count = min(RB, a.B - b0);
+  for (int i = tid; i < count * 2 * chunks; i += 256) {
+    const int q = i / (2 * chunks), j = i % (2 * chunks), side = j / chunks, c = HV + side * GK + g * a.K + (j - side * chunks) * CH;
+    Taps<IO, W> k;
+    Raw<IO, CH> win[W];
+#pragma unroll
+    for (int t = 0; t < W - 1; ++t) win[t].load(state(b0 + q) + (size_t)t * C + c);
+    win[W - 1].load(x(b0 + q) + c);
+    k.load(a.taps, a.bias, c);
+#pragma unroll
+    for (int t = 0; t < W - 1; ++t) win[t + 1].store(state(b0 + q) + (size_t)t * C + c);
+    conv_row<IO, W, true>(k, win).store(reinterpret_cast<IO*>(&row[q][j]));
   }
   __syncthreads();
-  for (int i = tid; i < 2 * rep * chunks; i += 256) {
-    const int side = i / (rep * chunks), j = i - side * rep * chunks, hh = j / chunks, at = j - hh * chunks;
-    const size_t item = (size_t)b * a.H + g * rep + hh;
+  for (int i = tid; i < count * 2 * rep * chunks; i += 256) {
+    const int at = i % chunks, hh = i / chunks % rep, qs = i / chunks / rep, side = qs & 1, q = qs >> 1;
+    const size_t item = (size_t)(b0 + q) * a.H + g * rep + hh;
     IO* dst = side ? static_cast<IO*>(a.q) + item * a.K : static_cast<IO*>(a.rk) + (item * a.W + a.n) * a.K;
-    reinterpret_cast<uint4*>(dst)[at] = row[side * chunks + at];
+    reinterpret_cast<uint4*>(dst)[at] = row[q][side * chunks + at];
   }
+}
+
+template <typename IO, int W>
+int launch_conv_token(const ConvTokenArgs& a, hipStream_t s) {
+  constexpr int CH = 16 / sizeof(IO);
+  const int xparts = (a.H * a.V / CH + 255) / 256;
+  const unsigned parts = (unsigned)(xparts + a.G);
+  // four requests a workgroup where that leaves two workgroups a CU
+  if ((int64_t)parts * a.B >= 4 * 512)
+    hipLaunchKernelGGL((conv_token_kernel<IO, W, 4>), dim3(parts * (unsigned)((a.B + 3) / 4)), dim3(256), 0, s, a, xparts);
+  else
+    hipLaunchKernelGGL((conv_token_kernel<IO, W, 1>), dim3(parts * (unsigned)a.B), dim3(256), 0, s, a, xparts);
+  return 0;
 }
 
 template <typename IO>
 int launch_conv_token(const ConvTokenArgs& a, int width, hipStream_t s) {
-  constexpr int CH = 16 / sizeof(IO);
-  const int xparts = (a.H * a.V / CH + 255) / 256;
-  const dim3 grid((unsigned)a.B * (unsigned)(xparts + a.G));
   switch (width) {
-    case 2: hipLaunchKernelGGL((conv_token_kernel<IO, 2>), grid, dim3(256), 0, s, a, xparts); return 0;
-    case 3: hipLaunchKernelGGL((conv_token_kernel<IO, 3>), grid, dim3(256), 0, s, a, xparts); return 0;
-    case 4: hipLaunchKernelGGL((conv_token_kernel<IO, 4>), grid, dim3(256), 0, s, a, xparts); return 0;
+    case 2: return launch_conv_token<IO, 2>(a, s);
+    case 3: return launch_conv_token<IO, 3>(a, s);
+    case 4: return launch_conv_token<IO, 4>(a, s);
     default: return -2;
   }
 }

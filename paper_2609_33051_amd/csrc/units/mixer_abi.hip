@@ -80,7 +80,7 @@ int sketchssm_conv(const skssm_conv_config* cfg, int32_t batch, int64_t tokens, 
   if (state_in != state_out && overlap(state_in, ns, state_out, ns))
     return fail(SKSSM_EINVAL, "%s: the states overlap without being the same", what);
   const int64_t cols = ((int64_t)C * e / 16 + 255) / 256;
-  if (cols * (tokens / 16 + batch + 1) > kMaxGrid) return fail(SKSSM_EUNSUPPORTED, "%s: too many channels times tokens for one launch", what);
+  if (cols * (tokens / 8 + batch + 1) > kMaxGrid) return fail(SKSSM_EUNSUPPORTED, "%s: too many channels times tokens for one launch", what);
   skssm::ConvArgs a{};
   a.seq = sequences(batch, tokens, offsets);
   a.C = C;

@@ -60,6 +60,19 @@ def test_conv(io, w, lengths):
     assert torch.equal(y1, y2) and torch.equal(new1, new2)
 
 
+@pytest.mark.parametrize("io,C", [("bf16", 64), ("f32", 1032)])
+def test_conv_many_tokens(io, C):
+    """Enough tokens for the wide kernel; boundaries inside its workgroups and at their edges."""
+    case("conv many", io, C)
+    lengths = [16, 0, 5000, 15, 17, 4000, 1, 7999, 33] if C == 64 else [3000, 1, 31, 6000, 0, 16]
+    dt, r, T = DT[io], rnd(C), sum(lengths)
+    x, taps, bias, state = r((T, C), dt), r((C, 4)), r((C,)), r((len(lengths), 3, C), dt)
+    y, new = ops.conv(x, taps, bias, offsets=R.offsets(lengths), state=state)
+    want, mag, s, states = R.conv(x, taps, bias, lengths, state)
+    R.close(y, want, silu_bound(s, mag, 4, dt), "y")
+    assert torch.equal(new.double(), states)
+
+
 def test_conv_equal_lengths_and_no_tokens():
     case("conv equal lengths")
     r = rnd(4)
@@ -89,7 +102,8 @@ def test_conv_many_columns_and_nan_stay_apart():
 
 @pytest.mark.parametrize("io", ["bf16", "f32"])
 @pytest.mark.parametrize("Bt,H,G,K,V,W,w,n", [(1, 128, 8, 128, 64, 16, 4, 0), (3, 7, 1, 128, 64, 12, 3, 11), (2, 20, 4, 64, 64, 8, 2, 3),
-                                              (5, 32, 32, 128, 128, 32, 4, 31)])
+                                              (5, 32, 32, 128, 128, 32, 4, 31), (203, 128, 8, 128, 64, 4, 4, 2),
+                                              (513, 8, 1, 128, 128, 2, 2, 1)])
 def test_conv_token(io, Bt, H, G, K, V, W, w, n):
     case("token", io, Bt, H, G, K, V, W, w, n)
     dt, r = DT[io], rnd(Bt + H + n)
