@@ -442,10 +442,10 @@ __global__ __launch_bounds__(256, sizeof(IO) == 2 ? 2 : 1) void scan_kernel(Scan
   }
   int chunk = 0;
   for (int p = s.p0; p < s.p1; p += kChunk, chunk = (chunk + 1) & 3) {
-    __syncthreads();
+    lds_barrier();
     put();
     if (chunk == 0) gate(p);
-    __syncthreads();
+    lds_barrier();
     if (p + kChunk < s.p1) fetch(s.p1 - p - kChunk);
     const float* const rec = record(mine ? hl : 0, chunk);
 
@@ -537,7 +537,7 @@ __global__ __launch_bounds__(256, sizeof(IO) == 2 ? 2 : 1) void scan_kernel(Scan
 #pragma unroll
         for (int e = 0; e < 4; ++e) { y[tt][0][e] *= et; y[tt][1][e] *= et; }
       }
-      __syncthreads();
+      lds_barrier();
       const int n = mine ? s.p1 - p : 0;
 #pragma unroll
       for (int tt = 0; tt < 4; ++tt)
