@@ -8,11 +8,14 @@
 // tokens, and goes through it chunk by chunk; the state stays in registers (32 value
 // channels a wave) and each input is read once, a chunk ahead.
 //
-// Fragments.  Both operands of a product hold, per lane, 8 consecutive indices of
-// a 32-deep reduction (lane group g = lane / 16: 8 g .. 8 g + 7) of the row or
-// column lane % 16.  The state's accumulator tiles are assigned to channels so
-// that two of them are such a fragment as they lie: tile kt, row m is channel
-// 32 (kt / 2) + 8 (m / 4) + 4 (kt % 2) + m % 4.
+// Products.  The state's update and its reads run in tiles of 32 x 32, the scores
+// in tiles of 16 x 16.  An instruction takes the vector units' issue slots for some
+// 12 cycles whichever it is, 32x32x16 for 32 cycles of products and 16x16x32 for 16, and
+// the vector work between them (weights, decays, roundings) is what bounds this kernel.
+// Operands hold, per lane, 8 consecutive indices of the reduction (lane group h = lane /
+// 32, or g = lane / 16) of the row or column lane % 32 (lane % 16).  The state's
+// accumulator rows are assigned to channels so that eight of a lane's registers are
+// such an operand as they lie: row 8 q + 4 h + e of a tile is channel 16 (q / 2) + 8 h + 4 (q % 2) + e.
 //
 // Long sequences: a sequence is split into segments of `seg` tokens, a fair
 // share of the card.  A first launch runs the state part of every segment but a
@@ -28,71 +31,57 @@ constexpr int kChunk = 64;
 constexpr int kValues = 128;        // value channels of a workgroup
 constexpr int kGates = 4 * kChunk;  // tokens whose gates are computed together, a chunk per wave
 // places in a chunk's record of gates (floats)
-constexpr int kLeft = 0, kEnd = 64, kLocalRecord = 68, kLocal = 68, kStep = 196, kGate = 324, kPass = 388, kRecord = 484;
+constexpr int kLeft = 0, kEnd = 64, kLocalRecord = 68, kLocal = 68, kStep = 196, kGate = 324, kPass = 388, kSkip = 452, kRecord = 456;
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short shortx4 __attribute__((ext_vector_type(4)));
+typedef float floatx16 __attribute__((ext_vector_type(16)));
 
-// 64 rows of COLS elements in LDS, for reads of 16 bytes of a row by the lanes of
-// consecutive rows: the 16-byte chunks of a row are permuted by the row, so that the
-// eight rows a read takes at once lie in different banks.
-template <typename IO, int COLS> struct RowTile {
+// 64 rows of COLS elements in LDS.  The 16-byte chunks of a row are permuted by the row:
+// pairs of chunks by its low two bits, so that the four rows of 32 bytes that a transposed
+// read takes lie in different banks, and the two of a pair by the next bit, so that 16
+// bytes of eight consecutive rows do.
+template <typename IO, int COLS> struct Tile {
   static constexpr int kBytes = kChunk * COLS * (int)sizeof(IO), kChunks = COLS * (int)sizeof(IO) / 16;
   static constexpr int kPer = 16 / (int)sizeof(IO);  // elements of a chunk
   static __device__ __forceinline__ int at(int row, int col) {  // byte offset
-    return row * (COLS * (int)sizeof(IO)) + (((col / kPer) ^ (row & 7)) << 4) + (col % kPer) * (int)sizeof(IO);
+    return row * (COLS * (int)sizeof(IO)) + (((col / kPer) ^ (((row & 3) << 1) | ((row >> 2) & 1))) << 4) + (col % kPer) * (int)sizeof(IO);
   }
 };
-// The same where columns are read too.  fp32: as above.  bf16: a transposed read takes
-// 8-byte pieces of four rows, channels 32 q + 8 p + 4 h .. + 3 for p = 0..3: these are made
-// neighbours (32 bytes: unit h COLS / 32 + q of the row), units are permuted by the row's
-// low bits, so that the four rows cover 128 bytes, and pieces by the next two, so that
-// 16 rows of one piece do.
-template <typename IO, int COLS> struct ColTile : RowTile<IO, COLS> {};
-template <int COLS> struct ColTile<bf16_t, COLS> : RowTile<bf16_t, COLS> {
-  static __device__ __forceinline__ int at(int row, int col) {
-    const int unit = ((col >> 2) & 1) * (COLS / 32) + (col >> 5), piece = (col >> 3) & 3;
-    return row * (COLS * 2) + ((unit ^ (row & 3)) << 5) + ((piece ^ ((row >> 2) & 3)) << 3) + (col & 3) * 2;
-  }
-};
+
+// The channel of row (column) m of a 32-wide tile of the state.
+__device__ __forceinline__ int channel(int m) { return 16 * (m >> 4) + 8 * ((m >> 2) & 1) + 4 * ((m >> 3) & 1) + (m & 3); }
 
 struct FragF32 { float e[8]; };
 
 template <typename IO> struct Frags;
 template <> struct Frags<bf16_t> {
   using F = bf16x8;
-  // 8 consecutive columns of one row of a RowTile, and of a ColTile, from the places of the
-  // first four and the last four
+  static constexpr int kRow = 1, kCols = 2;  // places a lane holds of a row's and of a column's operand
+  // 8 consecutive columns of one row
+  template <int COLS> static __device__ __forceinline__ void row_at(uint32_t* at, int row, int col) { at[0] = Tile<bf16_t, COLS>::at(row, col); }
   static __device__ __forceinline__ F row(const char* t, const uint32_t* at, int off) {
     return __builtin_bit_cast(F, *reinterpret_cast<const uint4*>(t + at[0] + off));
   }
-  static __device__ __forceinline__ F row_c(const char* t, const uint32_t* at, int off) {
-    const uint2 a = *reinterpret_cast<const uint2*>(t + at[0] + off), b = *reinterpret_cast<const uint2*>(t + at[1] + off);
-    return __builtin_bit_cast(F, make_uint4(a.x, a.y, b.x, b.y));
-  }
-  template <int COLS> static __device__ __forceinline__ void put_c(char* t, int row, int col, uint4 x) {
-    *reinterpret_cast<uint2*>(t + ColTile<bf16_t, COLS>::at(row, col)) = make_uint2(x.x, x.y);
-    *reinterpret_cast<uint2*>(t + ColTile<bf16_t, COLS>::at(row, col + 4)) = make_uint2(x.z, x.w);
-  }
-  // 8 consecutive rows of the column that the lane's place i = lane % 16 stands for, where
-  // places 4 p .. 4 p + 3 are four consecutive columns: a transposed read takes, from
-  // the 16 lanes of a group, four rows (i / 4) of four 8-byte pieces (i % 4)
-  static constexpr int kCols = 2;  // places a lane holds: of row i / 4 and of row 4 + i / 4
-  template <int COLS> static __device__ __forceinline__ void cols_at(uint32_t* at, int row0, int i, int col0, int step) {
+  // rows 8 h .. 8 h + 7 of column col0 + channel(lane % 32): a transposed read takes, from 16
+  // lanes, four rows (i / 4) of four 8-byte pieces (i % 4) and leaves each lane a column
+  template <int COLS> static __device__ __forceinline__ void cols_at(uint32_t* at, int lane, int col0) {
+    const int i = lane & 15, p = i & 3;
 #pragma unroll
-    for (int q = 0; q < 2; ++q) at[q] = ColTile<bf16_t, COLS>::at(row0 + 4 * q + (i >> 2), col0 + step * (i & 3));
+    for (int q = 0; q < 2; ++q)
+      at[q] = Tile<bf16_t, COLS>::at(8 * (lane >> 5) + 4 * q + (i >> 2), col0 + channel(16 * ((lane >> 4) & 1) + 4 * p));
   }
-  // (odd: the same places four columns on, COLS / 32 units)
-  template <int COLS> static __device__ __forceinline__ F cols(const char* t, const uint32_t* at, int off, int odd) {
+  static __device__ __forceinline__ F cols(const char* t, const uint32_t* at, int off) {
     typedef __attribute__((address_space(3))) shortx4* lds4;
-    const uint32_t a = COLS == 128 ? at[0] + 128 * odd : at[0] ^ (COLS * odd), b = COLS == 128 ? at[1] + 128 * odd : at[1] ^ (COLS * odd);
-    const shortx4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(t + a + off));
-    const shortx4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(t + b + off));
+    const shortx4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(t + at[0] + off));
+    const shortx4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(t + at[1] + off));
     return __builtin_bit_cast(F, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
   }
   static __device__ __forceinline__ floatx4 mma(F a, F b, floatx4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
-  static __device__ __forceinline__ F of(floatx4 lo, floatx4 hi) {
-    return __builtin_bit_cast(F, make_uint4(bf16_pack2(lo[0], lo[1]), bf16_pack2(lo[2], lo[3]), bf16_pack2(hi[0], hi[1]), bf16_pack2(hi[2], hi[3])));
+  static __device__ __forceinline__ floatx16 mma(F a, F b, floatx16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+  static __device__ __forceinline__ F of(const floatx16& s, int r) {  // registers r .. r + 7
+    return __builtin_bit_cast(F, make_uint4(bf16_pack2(s[r], s[r + 1]), bf16_pack2(s[r + 2], s[r + 3]), bf16_pack2(s[r + 4], s[r + 5]),
+                                            bf16_pack2(s[r + 6], s[r + 7])));
   }
   static __device__ __forceinline__ void store4(char* t, int at, float a, float b, float c, float d) {
     *reinterpret_cast<uint2*>(t + at) = make_uint2(bf16_pack2(a, b), bf16_pack2(c, d));
@@ -100,6 +89,11 @@ template <> struct Frags<bf16_t> {
 };
 template <> struct Frags<float> {
   using F = FragF32;
+  static constexpr int kRow = 2, kCols = 8;
+  template <int COLS> static __device__ __forceinline__ void row_at(uint32_t* at, int row, int col) {
+    at[0] = Tile<float, COLS>::at(row, col);
+    at[1] = Tile<float, COLS>::at(row, col + 4);
+  }
   static __device__ __forceinline__ F row(const char* t, const uint32_t* at, int off) {
     F f;
     const float4 a = *reinterpret_cast<const float4*>(t + at[0] + off), b = *reinterpret_cast<const float4*>(t + at[1] + off);
@@ -107,20 +101,14 @@ template <> struct Frags<float> {
     f.e[4] = b.x; f.e[5] = b.y; f.e[6] = b.z; f.e[7] = b.w;
     return f;
   }
-  static constexpr int kCols = 8;
-  template <int COLS> static __device__ __forceinline__ void cols_at(uint32_t* at, int row0, int i, int col0, int step) {
+  template <int COLS> static __device__ __forceinline__ void cols_at(uint32_t* at, int lane, int col0) {
 #pragma unroll
-    for (int q = 0; q < 8; ++q) at[q] = ColTile<float, COLS>::at(row0 + q, col0 + step * (i >> 2) + (i & 3));
+    for (int q = 0; q < 8; ++q) at[q] = Tile<float, COLS>::at(8 * (lane >> 5) + q, col0 + channel(lane & 31));
   }
-  static __device__ __forceinline__ F row_c(const char* t, const uint32_t* at, int off) { return row(t, at, off); }
-  template <int COLS> static __device__ __forceinline__ void put_c(char* t, int row, int col, uint4 x) {
-    *reinterpret_cast<uint4*>(t + ColTile<float, COLS>::at(row, col)) = x;
-  }
-  // (odd: the same places four columns on, the other chunk of a pair)
-  template <int COLS> static __device__ __forceinline__ F cols(const char* t, const uint32_t* at, int off, int odd) {
+  static __device__ __forceinline__ F cols(const char* t, const uint32_t* at, int off) {
     F f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) f.e[e] = *reinterpret_cast<const float*>(t + (at[e] ^ (16 * odd)) + off);
+    for (int e = 0; e < 8; ++e) f.e[e] = *reinterpret_cast<const float*>(t + at[e] + off);
     return f;
   }
   static __device__ __forceinline__ floatx4 mma(const F& a, const F& b, floatx4 c) {
@@ -128,10 +116,15 @@ template <> struct Frags<float> {
     for (int e = 0; e < 8; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.e[e], b.e[e], c, 0, 0, 0);
     return c;
   }
-  static __device__ __forceinline__ F of(floatx4 lo, floatx4 hi) {
+  static __device__ __forceinline__ floatx16 mma(const F& a, const F& b, floatx16 c) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.e[e], b.e[e], c, 0, 0, 0);
+    return c;
+  }
+  static __device__ __forceinline__ F of(const floatx16& s, int r) {
     F f;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) { f.e[e] = lo[e]; f.e[e + 4] = hi[e]; }
+    for (int e = 0; e < 8; ++e) f.e[e] = s[r + e];
     return f;
   }
   static __device__ __forceinline__ void store4(char* t, int at, float a, float b, float c, float d) {
@@ -232,12 +225,12 @@ template <typename IO, int K, int V, bool LOCAL>
 __global__ __launch_bounds__(256, sizeof(IO) == 2 ? 2 : 1) void scan_kernel(ScanArgs a, int seg, bool apart) {
   using FR = Frags<IO>;
   using F = typename FR::F;
-  using TB = ColTile<IO, K>;
-  using TX = ColTile<IO, kValues>;
-  using TC = RowTile<IO, K>;
-  using TM = RowTile<IO, kChunk>;
-  constexpr int KT = K / 16, KF = K / 32, HEADS = kValues / V, PER = TB::kPer, ROW = (int)sizeof(IO) * 16;
+  using TB = Tile<IO, K>;
+  using TX = Tile<IO, kValues>;
+  using TM = Tile<IO, kChunk>;
+  constexpr int KT = K / 32, HEADS = kValues / V, PER = TB::kPer, ROW = (int)sizeof(IO) * 16;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, g = lane >> 4;
+  const int c32 = lane & 31, h32 = lane >> 5;
   // workgroups go round the eight XCDs: each takes a run of heads, whose groups' B and C stay in its L2
   const int per_group = a.H / a.G, parts = a.G * ((per_group + HEADS - 1) / HEADS);
   const int slot = blockIdx.x / parts;
@@ -265,43 +258,46 @@ __global__ __launch_bounds__(256, sizeof(IO) == 2 ? 2 : 1) void scan_kernel(Scan
   char* const lb = lds;
   char* const lx = lb + TB::kBytes;
   char* const lc = lx + TX::kBytes;
-  char* const lm = lc + TC::kBytes;
+  char* const lm = lc + TB::kBytes;
   float* const gates = reinterpret_cast<float*>(LOCAL ? lc : lm + HEADS * TM::kBytes);
 
-  // channels: the lane's four state values (v of place i, k of group g) of tile (u, kt) in a tile-major state
-  auto state_at = [&](int u, int kt) {
-    const int v = vbase + 8 * (i >> 2) + 4 * u + (i & 3), k = 32 * (kt >> 1) + 8 * g + 4 * (kt & 1);
-    return ((v >> 4) * (K / 16) + (k >> 4)) * 256 + 4 * ((v & 15) + 16 * ((k & 15) >> 2));
+  // the place of registers 4 q .. 4 q + 3 of tile kt (value channel of column c32, four key channels) in a tile-major state
+  auto state_at = [&](int kt, int q) {
+    const int v = vbase + channel(c32);
+    return ((v >> 4) * (K / 16) + 2 * kt + (q >> 1)) * 256 + 4 * ((v & 15) + 16 * (2 * h32 + (q & 1)));
   };
   auto work_at = [&](int j) { return a.work + ((size_t)(j - 1) * a.H + h) * (V * K); };  // before segment start j
   float* const decays = a.work ? a.work + (size_t)(a.seq.tokens / seg) * a.H * (V * K) : nullptr;
 
-  floatx4 S[2][KT];
+  floatx16 S[KT];
 #pragma unroll
-  for (int u = 0; u < 2; ++u)
+  for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
-    for (int kt = 0; kt < KT; ++kt) S[u][kt] = floatx4{0.f, 0.f, 0.f, 0.f};
+    for (int r = 0; r < 16; ++r) S[kt][r] = 0.f;
+  // S = S d + a stored state
+  auto add_state = [&](const float* from, float d) {
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const floatx4 t = *reinterpret_cast<const floatx4*>(from + state_at(kt, q));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) S[kt][4 * q + e] = fmaf(S[kt][4 * q + e], d, t[e]);
+      }
+  };
+  auto put_state = [&](float* to) {
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        *reinterpret_cast<floatx4*>(to + state_at(kt, q)) = floatx4{S[kt][4 * q], S[kt][4 * q + 1], S[kt][4 * q + 2], S[kt][4 * q + 3]};
+  };
   if (s.k == 0) {
-    if (a.S_in) {
-      const float* in = a.S_in + ((size_t)s.b * a.H + h) * (V * K);
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int kt = 0; kt < KT; ++kt) S[u][kt] = *reinterpret_cast<const floatx4*>(in + state_at(u, kt));
-    }
+    if (a.S_in) add_state(a.S_in + ((size_t)s.b * a.H + h) * (V * K), 1.f);
   } else if (!LOCAL) {
     for (int k = 0; k < s.k; ++k) {  // the segments before this one, in order
       const int j = (int)(((int64_t)s.lo + (int64_t)(k + 1) * seg) / seg);
-      const float* w = work_at(j);
-      const float d = k ? __builtin_amdgcn_exp2f(decays[(size_t)(j - 1) * a.H + h]) : 0.f;
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int kt = 0; kt < KT; ++kt) {
-          const floatx4 t = *reinterpret_cast<const floatx4*>(w + state_at(u, kt));
-#pragma unroll
-          for (int e = 0; e < 4; ++e) S[u][kt][e] = k ? fmaf(S[u][kt][e], d, t[e]) : t[e];
-        }
+      add_state(work_at(j), k ? __builtin_amdgcn_exp2f(decays[(size_t)(j - 1) * a.H + h]) : 1.f);
     }
   }
 
@@ -346,11 +342,11 @@ __global__ __launch_bounds__(256, sizeof(IO) == 2 ? 2 : 1) void scan_kernel(Scan
   auto put = [&]() {
 #pragma unroll
     for (int q = 0; q < NB; ++q) {
-      FR::template put_c<K>(lb, q * RB + rb, cb, pb[q]);
-      if (!LOCAL) *reinterpret_cast<uint4*>(lc + TC::at(q * RB + rb, cb)) = pc[q];
+      *reinterpret_cast<uint4*>(lb + TB::at(q * RB + rb, cb)) = pb[q];
+      if (!LOCAL) *reinterpret_cast<uint4*>(lc + TB::at(q * RB + rb, cb)) = pc[q];
     }
 #pragma unroll
-    for (int q = 0; q < NX; ++q) FR::template put_c<kValues>(lx, q * RX + rx, cx, px[q]);
+    for (int q = 0; q < NX; ++q) *reinterpret_cast<uint4*>(lx + TX::at(q * RX + rx, cx)) = px[q];
   };
 
   // Step sizes and decays of four chunks, a chunk per wave.  Sums of log decays run in
@@ -359,7 +355,7 @@ __global__ __launch_bounds__(256, sizeof(IO) == 2 ? 2 : 1) void scan_kernel(Scan
   // the tile of 16 tokens t / 16 = w and G(w) the sum before it, base 2:
   //   kLocal  g_t - G(w) in two parts       kStep  g_s - G(w) - log2 dt_s in two parts
   //   kGate   2^{g_t}
-  //   kPass   dt_s 2^{G(w) - g_s} of the tokens s before tile w = 1, 2, 3
+  //   kPass   dt_s 2^{G(w + 1) - g_s}       kSkip  1 and 2^{G(w) - G(w' + 1)}, (w, w') = (2, 0), (3, 1), (3, 0)
   //   kLeft   dt_s 2^{g_L - g_s}            kEnd   g_L
   // LOCAL keeps kLeft and kEnd.
   auto record = [&](int head, int chunk) { return gates + (head * 4 + chunk) * (LOCAL ? kLocalRecord : kRecord); };
@@ -404,32 +400,29 @@ __global__ __launch_bounds__(256, sizeof(IO) == 2 ? 2 : 1) void scan_kernel(Scan
         r[kStep + lane] = at;
         r[kStep + 64 + lane] = (float)(low - (double)at);
         r[kGate + lane] = __builtin_amdgcn_exp2f((float)sum[q]);
-        if (lane < 16) r[kPass + lane] = dt[q] * __builtin_amdgcn_exp2f((float)(g1 - sum[q]));
-        if (lane < 32) r[kPass + 16 + lane] = dt[q] * __builtin_amdgcn_exp2f((float)(g2 - sum[q]));
-        if (lane < 48) r[kPass + 48 + lane] = dt[q] * __builtin_amdgcn_exp2f((float)(g3 - sum[q]));
+        r[kPass + lane] = dt[q] * __builtin_amdgcn_exp2f((float)((lane < 16 ? g1 : lane < 32 ? g2 : lane < 48 ? g3 : end) - sum[q]));
+        const float skip = __builtin_amdgcn_exp2f((float)(lane == 1 ? g2 - g1 : lane == 2 ? g3 - g2 : lane == 3 ? g3 - g1 : 0.0));
+        if (lane < 4) r[kSkip + lane] = skip;
       }
     }
   };
 
-  // the lane's places in the tiles: rows i (+ 16 per 16 ROW COLS bytes) of B, C and M, columns of B and x
-  constexpr int NR = (int)sizeof(IO) / 2;  // 16-byte chunks of a fragment's row
-  uint32_t brow[KF][2], crow[KF][NR], mrow[2][NR], bcol[KF][FR::kCols], xcol[FR::kCols];
+  // the lane's places in the tiles: rows i of B and C by 32 channels (scores), rows c32 of C by 16
+  // channels and of M, columns of B and x
+  uint32_t row16[KT][FR::kRow], row32[2 * KT][FR::kRow], mrow[4][FR::kRow], bcol[KT][FR::kCols], xcol[FR::kCols];
 #pragma unroll
-  for (int q = 0; q < 2; ++q)
-#pragma unroll
-    for (int kf = 0; kf < KF; ++kf) brow[kf][q] = TB::at(i, 32 * kf + 8 * g + 4 * q);
-#pragma unroll
-  for (int q = 0; q < NR; ++q) {
-#pragma unroll
-    for (int kf = 0; kf < KF; ++kf) crow[kf][q] = TC::at(i, 32 * kf + 8 * g + 4 * q);
-#pragma unroll
-    for (int sf = 0; sf < 2; ++sf) mrow[sf][q] = hl * TM::kBytes + TM::at(i, 32 * sf + 8 * g + 4 * q);
+  for (int kt = 0; kt < KT; ++kt) {
+    FR::template row_at<K>(row16[kt], i, 32 * kt + 8 * g);
+    FR::template row_at<K>(row32[2 * kt], c32, 32 * kt + 8 * h32);
+    FR::template row_at<K>(row32[2 * kt + 1], c32, 32 * kt + 16 + 8 * h32);
+    FR::template cols_at<K>(bcol[kt], lane, 32 * kt);
   }
 #pragma unroll
-  for (int kf = 0; kf < KF; ++kf) FR::template cols_at<K>(bcol[kf], 8 * g, i, 32 * kf, 8);
-  FR::template cols_at<kValues>(xcol, 8 * g, i, 32 * wave, 8);
-  const uint32_t oy = (uint32_t)((i * a.ldy + vbase + 8 * g) * sizeof(IO));
-  const size_t ny = 16 * a.ldy * sizeof(IO);
+  for (int st = 0; st < 4; ++st) FR::template row_at<kChunk>(mrow[st], c32, 16 * st + 8 * h32);
+  FR::template cols_at<kValues>(xcol, lane, 32 * wave);
+  char* const lmh = lm + hl * TM::kBytes;
+  const uint32_t oy = (uint32_t)((c32 * a.ldy + vbase + 8 * h32) * sizeof(IO));
+  const size_t ny = 32 * a.ldy * sizeof(IO);
   char* py = static_cast<char*>(a.y) + (size_t)h * V * sizeof(IO) + (size_t)s.p0 * sizeof(IO) * a.ldy;
 
   if (!LOCAL) {  // scores of tokens after t in the 32 that a fragment spans: zero throughout
@@ -452,16 +445,19 @@ __global__ __launch_bounds__(256, sizeof(IO) == 2 ? 2 : 1) void scan_kernel(Scan
     if constexpr (!LOCAL) {
       // scores of tiles (w, st): tokens t (place i) of tile w against s of tile st <= w, with
       // decay and step, as rows of M; D on the diagonal.  The ten tiles by wave:
-      // its diagonal one, then 0: (1,0) (2,0)  1: (2,1) (3,0)  2: (3,1)  3: (3,2).  (What a missing
-      // second head finds in its record is never stored.)
-      auto score = [&](int tw, int ts, auto diagonal) {
+      // its diagonal one, then 0: (1,0), 1: (2,1), 2: (3,1), 3: (3,2), then (2,0) and (3,0), each
+      // head by a wave of its own where there are two.  (What a missing second head finds in
+      // its record is never stored.)
+      auto score = [&](int tw, int ts, int one, auto diagonal) {  // one: the only head, or -1
         floatx4 m = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int kf = 0; kf < KF; ++kf)
-          m = FR::mma(FR::row_c(lb, brow[kf], ts * ROW * K), FR::row(lc, crow[kf], tw * ROW * K), m);
+        for (int kt = 0; kt < KT; ++kt)
+          m = FR::mma(FR::row(lb, row16[kt], ts * ROW * K), FR::row(lc, row16[kt], tw * ROW * K), m);
         const int to = TM::at(16 * tw + i, 16 * ts + 4 * g);
 #pragma unroll
-        for (int hh = 0; hh < HEADS; ++hh) {
+        for (int q = 0; q < HEADS; ++q) {
+          if (one >= 0 && q > 0) break;
+          const int hh = one >= 0 ? one : q;
           const float* r = record(hh, chunk);
           float f[4];
           if constexpr (decltype(diagonal)::value) {
@@ -473,146 +469,112 @@ __global__ __launch_bounds__(256, sizeof(IO) == 2 ? 2 : 1) void scan_kernel(Scan
             for (int e = 0; e < 4; ++e) {
               const int o = 4 * g + e - i;  // s - t
               f[e] = m[e] * __builtin_amdgcn_exp2f((th - h4[e]) + (tl - l4[e]));
-              f[e] = (o > 0 ? 0.f : f[e]) + (o == 0 ? Dh[hh] : 0.f);
+              f[e] = (o > 0 ? 0.f : f[e]) + (o == 0 ? Dh[q] : 0.f);
             }
           } else {
-            const float et = __builtin_amdgcn_exp2f(r[kLocal + 16 * tw + i]);
-            const float4 w4 = *reinterpret_cast<const float4*>(r + kPass + (tw == 1 ? 0 : tw == 2 ? 16 : 48) + 16 * ts + 4 * g);
+            const float et = __builtin_amdgcn_exp2f(r[kLocal + 16 * tw + i]) * r[kSkip + (tw - ts == 1 ? 0 : tw - ts == 3 ? 3 : ts + 1)];
+            const float4 w4 = *reinterpret_cast<const float4*>(r + kPass + 16 * ts + 4 * g);
             f[0] = m[0] * et * w4.x; f[1] = m[1] * et * w4.y; f[2] = m[2] * et * w4.z; f[3] = m[3] * et * w4.w;
           }
           FR::store4(lm + hh * TM::kBytes, to, f[0], f[1], f[2], f[3]);
         }
       };
-      score(wave, wave, std::true_type{});
-      score(wave == 0 ? 1 : wave == 1 ? 2 : 3, wave == 0 ? 0 : wave == 3 ? 2 : 1, std::false_type{});
-      if (wave < 2) score(wave + 2, 0, std::false_type{});
+      score(wave, wave, -1, std::true_type{});
+      score(wave == 0 ? 1 : wave == 1 ? 2 : 3, wave == 0 ? 0 : wave == 3 ? 2 : 1, -1, std::false_type{});
+      if (HEADS == 2) score(2 + (wave & 1), 0, wave >> 1, std::false_type{});
+      else if (wave < 2) score(2 + wave, 0, -1, std::false_type{});
     }
-    // Between products the vector units have work of their own: an instruction of the matrix
-    // cores takes the time of four others (a product, then three of them, in the
-    // orders asked for below).
-    F xt[2][2];
+    F xt[4];  // columns of x by 16 tokens
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-      for (int sf = 0; sf < 2; ++sf) xt[u][sf] = FR::template cols<kValues>(lx, xcol, sf * 2 * ROW * kValues, u);
+    for (int st = 0; st < 4; ++st) xt[st] = FR::cols(lx, xcol, st * ROW * kValues);
     const float end = rec[kEnd], d = __builtin_amdgcn_exp2f(end);
     total += end;
-    Weighted<IO> w[2][2];
-    auto weigh = [&](int sf) {
+    Weighted<IO> w[4];
+    auto weigh = [&](int st) {
       Vec<8> ws;
-      ws.load(rec + kLeft + 32 * sf + 8 * g);
-      w[0][sf].set(xt[0][sf], ws.e);
-      w[1][sf].set(xt[1][sf], ws.e);
+      ws.load(rec + kLeft + 16 * st + 8 * h32);
+      w[st].set(xt[st], ws.e);
     };
     if constexpr (!LOCAL) {
       // y: the state's part first, so that its products run while the scores settle
-      floatx4 y[4][2];
+      floatx16 y[2];
 #pragma unroll
-      for (int tt = 0; tt < 4; ++tt)
+      for (int r = 0; r < 16; ++r) y[0][r] = y[1][r] = 0.f;
 #pragma unroll
-        for (int u = 0; u < 2; ++u) y[tt][u] = floatx4{0.f, 0.f, 0.f, 0.f};
+      for (int kt = 0; kt < KT; ++kt) {
 #pragma unroll
-      for (int kf = 0; kf < KF; ++kf) {
-        const F s0 = FR::of(S[0][2 * kf], S[0][2 * kf + 1]), s1 = FR::of(S[1][2 * kf], S[1][2 * kf + 1]);
+        for (int j = 0; j < 2; ++j) {
+          const F sk = FR::of(S[kt], 8 * j);
 #pragma unroll
-        for (int tt = 0; tt < 4; ++tt) {
-          const F ct = FR::row(lc, crow[kf], tt * ROW * K);
-          y[tt][0] = FR::mma(s0, ct, y[tt][0]);
-          y[tt][1] = FR::mma(s1, ct, y[tt][1]);
+          for (int tt = 0; tt < 2; ++tt) y[tt] = FR::mma(sk, FR::row(lc, row32[2 * kt + j], 2 * tt * ROW * K), y[tt]);
         }
 #pragma unroll
-        for (int u = 0; u < 2; ++u) { S[u][2 * kf] *= d; S[u][2 * kf + 1] *= d; }
-      }
-      weigh(0);
-      if constexpr (sizeof(IO) == 2) {
-#pragma unroll
-        for (int q = 0; q < 8 * KF; ++q) {
-          __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-          __builtin_amdgcn_sched_group_barrier(0x2, 5, 0);
-        }
+        for (int r = 0; r < 16; ++r) S[kt][r] *= d;
       }
 #pragma unroll
-      for (int tt = 0; tt < 4; ++tt) {
-        const float et = rec[kGate + 16 * tt + i];
+      for (int tt = 0; tt < 2; ++tt) {
+        const float et = rec[kGate + 32 * tt + c32];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) { y[tt][0][e] *= et; y[tt][1][e] *= et; }
+        for (int r = 0; r < 16; ++r) y[tt][r] *= et;
       }
       lds_barrier();
       const int n = mine ? s.p1 - p : 0;
 #pragma unroll
-      for (int tt = 0; tt < 4; ++tt)
+      for (int st = 0; st < 4; ++st)
 #pragma unroll
-        for (int sf = 0; sf <= tt / 2; ++sf) {
-          const F mt = FR::row(lm, mrow[sf], tt * ROW * kChunk);
-          y[tt][0] = FR::mma(xt[0][sf], mt, y[tt][0]);
-          y[tt][1] = FR::mma(xt[1][sf], mt, y[tt][1]);
-        }
+        for (int tt = st / 2; tt < 2; ++tt) y[tt] = FR::mma(xt[st], FR::row(lmh, mrow[st], 2 * tt * ROW * kChunk), y[tt]);
       auto rows = [&](auto all) {
 #pragma unroll
-        for (int tt = 0; tt < 4; ++tt) {
-          if (!decltype(all)::value && 16 * tt + i >= n) continue;
-          Raw<IO, 8> o;
+        for (int tt = 0; tt < 2; ++tt) {
+          if (!decltype(all)::value && 32 * tt + c32 >= n) continue;
 #pragma unroll
-          for (int u = 0; u < 2; ++u)
+          for (int j = 0; j < 2; ++j) {  // channels 16 j + 8 h32 ..
+            Raw<IO, 8> o;
 #pragma unroll
-            for (int e = 0; e < 4; e += 2) {
-              if constexpr (sizeof(IO) == 2) o.w[2 * u + e / 2] = bf16_pack2(y[tt][u][e], y[tt][u][e + 1]);
-              else { o.e[4 * u + e] = y[tt][u][e]; o.e[4 * u + e + 1] = y[tt][u][e + 1]; }
+            for (int e = 0; e < 8; e += 2) {
+              if constexpr (sizeof(IO) == 2) o.w[e / 2] = bf16_pack2(y[tt][8 * j + e], y[tt][8 * j + e + 1]);
+              else { o.e[e] = y[tt][8 * j + e]; o.e[e + 1] = y[tt][8 * j + e + 1]; }
             }
-          o.store(reinterpret_cast<IO*>(py + tt * ny + oy));
+            o.store(reinterpret_cast<IO*>(py + tt * ny + oy) + 16 * j);
+          }
         }
       };
       if (n >= kChunk) rows(std::true_type{});
       else rows(std::false_type{});
-      py += 4 * ny;
+      py += 2 * ny;
     } else {
-      weigh(0);
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
+      for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
-        for (int kt = 0; kt < KT; ++kt) S[u][kt] *= d;
+        for (int r = 0; r < 16; ++r) S[kt][r] *= d;
     }
     // the state: decayed already, now the chunk's tokens
+    weigh(0);
 #pragma unroll
-    for (int sf = 0; sf < 2; ++sf) {
-      if (sf == 0) weigh(1);
+    for (int st = 0; st < 4; ++st) {
+      if (st < 3) weigh(st + 1);
 #pragma unroll
-      for (int kt = 0; kt < KT; kt += 2) {
-        const F b0t = FR::template cols<K>(lb, bcol[kt / 2], sf * 2 * ROW * K, 0), b1t = FR::template cols<K>(lb, bcol[kt / 2], sf * 2 * ROW * K, 1);
+      for (int k = 0; k < Weighted<IO>::kParts; ++k)
 #pragma unroll
-        for (int k = 0; k < Weighted<IO>::kParts; ++k) {
-          S[0][kt] = FR::mma(b0t, w[0][sf].part(k), S[0][kt]);
-          S[1][kt] = FR::mma(b0t, w[1][sf].part(k), S[1][kt]);
-          S[0][kt + 1] = FR::mma(b1t, w[0][sf].part(k), S[0][kt + 1]);
-          S[1][kt + 1] = FR::mma(b1t, w[1][sf].part(k), S[1][kt + 1]);
-        }
-      }
+        for (int kt = 0; kt < KT; ++kt) S[kt] = FR::mma(FR::cols(lb, bcol[kt], st * ROW * K), w[st].part(k), S[kt]);
     }
     if constexpr (sizeof(IO) == 2) {
 #pragma unroll
-      for (int q = 0; q < 12 * KT / 2; ++q) {
+      for (int q = 0; q < 12 * KT; ++q) {
         __builtin_amdgcn_sched_group_barrier(0x8, 1, 1);
-        __builtin_amdgcn_sched_group_barrier(0x2, 3, 1);
+        __builtin_amdgcn_sched_group_barrier(0x2, 5, 1);
       }
     }
   }
 
   if (!mine) return;
   if (LOCAL) {
-    float* w = work_at(slot + 1);
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-      for (int kt = 0; kt < KT; ++kt) *reinterpret_cast<floatx4*>(w + state_at(u, kt)) = S[u][kt];
+    put_state(work_at(slot + 1));
     if (vbase == 0 && lane == 0) decays[(size_t)slot * a.H + h] = total;
   } else if (s.p1 == s.hi) {
     // S_out in place of S_in: other segments' workgroups may still read it, so that a later
     // segment leaves its state where only this workgroup reads, for a copy after the launch
-    float* out = apart && s.k > 0 ? work_at(slot - a.seq.batch + 1) : a.S_out + ((size_t)s.b * a.H + h) * (V * K);
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-      for (int kt = 0; kt < KT; ++kt) *reinterpret_cast<floatx4*>(out + state_at(u, kt)) = S[u][kt];
+    put_state(apart && s.k > 0 ? work_at(slot - a.seq.batch + 1) : a.S_out + ((size_t)s.b * a.H + h) * (V * K));
   }
 }
 
@@ -652,8 +614,8 @@ int launch_scan(const ScanArgs& a, hipStream_t s) {
   const int parts = scan_parts(a.H, a.G, V), seg = scan_segment(a.seq, parts), windows = scan_windows(a.seq, seg);
   const bool apart = windows && a.S_in && a.S_in == a.S_out;
   constexpr int heads = kValues / V;
-  constexpr size_t local = RowTile<IO, K>::kBytes + RowTile<IO, kValues>::kBytes;
-  constexpr size_t full = local + RowTile<IO, K>::kBytes + heads * RowTile<IO, kChunk>::kBytes;
+  constexpr size_t local = Tile<IO, K>::kBytes + Tile<IO, kValues>::kBytes;
+  constexpr size_t full = local + Tile<IO, K>::kBytes + heads * Tile<IO, kChunk>::kBytes;
   if (windows)
     hipLaunchKernelGGL((scan_kernel<IO, K, V, true>), dim3((unsigned)windows * (unsigned)parts), dim3(256),
                        local + heads * 4 * kLocalRecord * sizeof(float), s, a, seg, false);
