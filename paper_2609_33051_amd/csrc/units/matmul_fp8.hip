@@ -330,8 +330,7 @@ void launch_tiles(const MatmulArgs& p, int splits, hipStream_t s) {
 // 4096 x 4096 12.1 / 10.4 / 9.6; 200 x 2048 x 4096 13.8 / 13.2 / 13.6; 100 x 2048 x 2048 8.1 / 8.7 / 8.7: over what fills the
 // CUs in parts of 8 blocks at least, or twice that in parts of 16.
 struct MatmulPlan { int wide, rest, splits; };
-MatmulPlan matmul_plan(int M, int N, int K, bool narrow) {
-
+MatmulPlan matmul_plan(int M, int N, int K, bool narrow) {  // M, N, K >= 1
   constexpr int64_t cus = 256;
   auto tiles = [&](int bm, int bn, int n) { return (int64_t)((M + bm - 1) / bm) * ((n + bn - 1) / bn); };
   if (narrow && tiles(256, 256, N) >= cus) {

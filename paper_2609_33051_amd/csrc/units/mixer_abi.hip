@@ -296,7 +296,7 @@ int sketchssm_norm(const skssm_norm_args* args, void* stream) {
 }
 
 size_t sketchssm_matmul_fp8_workspace(int64_t M, int32_t N, int32_t K) {
-  if (M < 0 || M > kMaxTokens || N < 1 || K < 1) return 0;
+  if (M < 1 || M > kMaxTokens || N < 1 || N > kMaxTokens || K < 1) return 0;
   return skssm::matmul_fp8_workspace((int)M, N, K);
 }
 
@@ -306,7 +306,7 @@ int sketchssm_matmul_fp8(int64_t M, int32_t N, int32_t K, const void* a, int64_t
   const char* what = "sketchssm_matmul_fp8";
   if (M < 0 || N < 1 || K < 1) return fail(SKSSM_EINVAL, "%s: sizes %lld x %d x %d", what, (long long)M, N, K);
   if (K % 16) return fail(SKSSM_EUNSUPPORTED, "%s: K = %d is not a multiple of 16", what, K);
-  if (M > kMaxTokens || ((M + 127) / 128) * ((N + 127) / 128) > kMaxGrid) return fail(SKSSM_EUNSUPPORTED, "%s: M x N too large for one launch", what);
+  if (M > kMaxTokens || N > kMaxTokens || ((M + 127) / 128) * ((N + 127) / 128) > kMaxGrid) return fail(SKSSM_EUNSUPPORTED, "%s: M x N too large for one launch", what);
   if (out_dtype != SKSSM_F32 && out_dtype != SKSSM_BF16) return fail(SKSSM_EINVAL, "%s: unknown out_dtype %d", what, out_dtype);
   int rc;
   if ((rc = check_stride(what, "a", lda, K, 1)) || (rc = check_stride(what, "w", ldw, K, 1))) return rc;
@@ -317,7 +317,7 @@ int sketchssm_matmul_fp8(int64_t M, int32_t N, int32_t K, const void* a, int64_t
   if (!w || !w_scale || (M > 0 && (!a || !a_scale || !y))) return fail(SKSSM_EINVAL, "%s: a, w, their scales and y are required", what);
   if (!aligned(a) || !aligned(w) || !aligned(a_scale) || !aligned(w_scale) || !aligned(y) || !aligned(workspace))
     return fail(SKSSM_EALIGN, "%s: a pointer is not 16-byte aligned", what);
-  const size_t need = skssm::matmul_fp8_workspace((int)M, N, K);
+  const size_t need = sketchssm_matmul_fp8_workspace(M, N, K);
   if (need && (!workspace || workspace_bytes < need))
     return fail(SKSSM_EINVAL, "%s: workspace of %zu bytes, %zu needed", what, workspace ? workspace_bytes : (size_t)0, need);
   const int64_t kb = ((int64_t)K + 127) / 128, nb = ((int64_t)N + 127) / 128;

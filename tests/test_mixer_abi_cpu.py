@@ -153,6 +153,20 @@ def test_matmul_refusals(lib):
 
 
 @cpu_only
+def test_matmul_extreme_sizes(lib):
+    assert lib.sketchssm_matmul_fp8_workspace(0, 256, 8192) == 0 and lib.sketchssm_matmul_fp8_workspace(-1, 256, 8192) == 0
+    assert lib.sketchssm_matmul_fp8_workspace(1, (1 << 31) - 1, 256) == 0
+    assert matmul(lib, M=1, N=(1 << 31) - 1, ldy=1 << 31) == -2
+    assert matmul(lib, lda=1 << 24) == -2 and matmul(lib, ldw=1 << 24) == -2 and "stride" in B.sketchssm_last_error()
+    # K split over workgroups: the workspace is required
+    need = lib.sketchssm_matmul_fp8_workspace(16, 256, 8192)
+    assert need > 0
+    big = dict(M=16, K=8192, lda=8192, ldw=8192, ldsa=16)
+    assert matmul(lib, **big, nws=need - 1) == -1 and "workspace" in B.sketchssm_last_error()
+    assert matmul(lib, **big, ws=None) == -1 and matmul(lib, **big, ws=at(1)) == -1
+
+
+@cpu_only
 def test_ops_refuse_cpu_tensors(lib):
     x = torch.zeros(4, 64)
     with pytest.raises((ValueError, RuntimeError, AssertionError)):
