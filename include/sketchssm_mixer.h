@@ -85,7 +85,10 @@ int sketchssm_conv_token(const skssm_config* cfg, int32_t groups, int32_t width,
  * sketchssm_update(q = NULL) can follow.  y [T][heads*dv] io may not overlap
  * the inputs.  The state and every sum are fp32; with bf16 io the products
  * inside a chunk of tokens take bf16 operands (the decayed scores and the state
- * as read by C_t are rounded to nearest), while what enters the state is kept to 16 bits.
+ * as read by C_t are rounded to nearest), while what enters the state keeps 24 bits.
+ * Row strides of x, b, c and y are less than 2^24.  A value that is not finite stays in its
+ * head (x, dt) or group (b, c) and its sequence; within its chunk of 64 tokens it may
+ * reach the outputs of tokens before it.
  *
  * workspace: sketchssm_scan_workspace bytes (may be 0), used where a sequence's
  * scan is split over workgroups; its contents need not be kept.
@@ -146,7 +149,9 @@ int sketchssm_norm(const skssm_norm_args* args, void* stream);
  *     y[m][n] = sum_kb a_scale[kb][m] w_scale[n / 128][kb] sum_{k in block kb} a[m][k] w[n][k]
  * a [M][K] (row stride lda), w [N][K] (row stride ldw), a_scale [ceil(K/128)][M] (rows
  * ld_ascale apart), w_scale [ceil(N/128)][ceil(K/128)] fp32; y [M][N] of
- * out_dtype F32 or BF16, row stride ldy (any, >= N).  K is a multiple of 16; sums are fp32.
+ * out_dtype F32 or BF16, row stride ldy (any, >= N).  K is a multiple of 16, lda and ldw are
+ * less than 2^24.  Sums are fp32; for a BF16 output the 8-bit matrix instructions, which keep
+ * 2^-11 of the largest product they add, for F32 those of 16 bits, which keep fp32's.
  * workspace: sketchssm_matmul_fp8_workspace bytes (may be 0), for products
  * whose K axis is split over workgroups; its contents need not be kept.
  */

@@ -171,6 +171,8 @@ int sketchssm_scan(const skssm_config* cfg, int32_t groups, int64_t tokens, cons
   if ((rc = check_stride(what, "x", ldx, HV, e)) || (rc = check_stride(what, "b", ldb, GK, e)) ||
       (rc = check_stride(what, "c", ldc, GK, e)) || (rc = check_stride(what, "y", ldy, HV, e)))
     return rc;
+  for (const int64_t ld : {ldx, ldb, ldc, ldy})  // 32 rows are reached by 32-bit offsets
+    if (ld >= (int64_t)1 << 24) return fail(SKSSM_EUNSUPPORTED, "%s: a row stride of %lld: less than 2^24", what, (long long)ld);
   if (lddt < H) return fail(SKSSM_EINVAL, "%s: dt stride %lld is less than %lld heads", what, (long long)lddt, (long long)H);
   const size_t need = skssm::scan_workspace(cfg->batch, (int)tokens, cfg->heads, groups, cfg->dk, cfg->dv);
   if (need && (!workspace || workspace_bytes < need))

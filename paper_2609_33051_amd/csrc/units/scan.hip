@@ -21,6 +21,8 @@
 // share of the card.  A first launch runs the state part of every segment but a
 // sequence's last, from zero (the first: from S_in), and keeps its end state and
 // total decay; the second begins each segment from the states before it, joined.
+#include <math.h>
+
 #include <type_traits>
 
 #include "../mixer.h"
@@ -255,11 +257,11 @@ __global__ __launch_bounds__(256, sizeof(IO) == 2 ? 2 : 1) void scan_kernel(Scan
   }
 
   extern __shared__ __attribute__((aligned(16))) char lds[];
-  char* const lb = lds;
-  char* const lx = lb + TB::kBytes;
+  char* lb = lds;  // (LOCAL: of two buffers in turn)
+  char* lx = lb + TB::kBytes;
   char* const lc = lx + TX::kBytes;
   char* const lm = lc + TB::kBytes;
-  float* const gates = reinterpret_cast<float*>(LOCAL ? lc : lm + HEADS * TM::kBytes);
+  float* gates = reinterpret_cast<float*>(LOCAL ? lds + 2 * (TB::kBytes + TX::kBytes) : lm + HEADS * TM::kBytes);
 
   // the place of registers 4 q .. 4 q + 3 of tile kt (value channel of column c32, four key channels) in a tile-major state
   auto state_at = [&](int kt, int q) {
@@ -341,10 +343,10 @@ __global__ __launch_bounds__(256, sizeof(IO) == 2 ? 2 : 1) void scan_kernel(Scan
   };
   auto put = [&]() {
 #pragma unroll
-    for (int q = 0; q < NB; ++q) {
-      *reinterpret_cast<uint4*>(lb + TB::at(q * RB + rb, cb)) = pb[q];
+    for (int q = 0; q < NB; ++q) *reinterpret_cast<uint4*>(lb + TB::at(q * RB + rb, cb)) = pb[q];
+#pragma unroll
+    for (int q = 0; q < NB; ++q)
       if (!LOCAL) *reinterpret_cast<uint4*>(lc + TB::at(q * RB + rb, cb)) = pc[q];
-    }
 #pragma unroll
     for (int q = 0; q < NX; ++q) *reinterpret_cast<uint4*>(lx + TX::at(q * RX + rx, cx)) = px[q];
   };
@@ -435,7 +437,15 @@ __global__ __launch_bounds__(256, sizeof(IO) == 2 ? 2 : 1) void scan_kernel(Scan
   }
   int chunk = 0;
   for (int p = s.p0; p < s.p1; p += kChunk, chunk = (chunk + 1) & 3) {
-    lds_barrier();
+    if (LOCAL) {
+      // waves still at the chunk before read the other buffer, and at most one is behind
+      const bool odd = ((p - s.p0) / kChunk) & 1, high = ((p - s.p0) / kGates) & 1;
+      lb = lds + (odd ? TB::kBytes + TX::kBytes : 0);
+      lx = lb + TB::kBytes;
+      gates = reinterpret_cast<float*>(lds + 2 * (TB::kBytes + TX::kBytes)) + (high ? HEADS * 4 * kLocalRecord : 0);
+    } else {
+      lds_barrier();
+    }
     put();
     if (chunk == 0) gate(p);
     lds_barrier();
@@ -548,6 +558,7 @@ __global__ __launch_bounds__(256, sizeof(IO) == 2 ? 2 : 1) void scan_kernel(Scan
 #pragma unroll
         for (int r = 0; r < 16; ++r) S[kt][r] *= d;
     }
+    __builtin_amdgcn_s_setprio(1);
     // the state: decayed already, now the chunk's tokens
     weigh(0);
 #pragma unroll
@@ -558,13 +569,7 @@ __global__ __launch_bounds__(256, sizeof(IO) == 2 ? 2 : 1) void scan_kernel(Scan
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt) S[kt] = FR::mma(FR::cols(lb, bcol[kt], st * ROW * K), w[st].part(k), S[kt]);
     }
-    if constexpr (sizeof(IO) == 2) {
-#pragma unroll
-      for (int q = 0; q < 12 * KT; ++q) {
-        __builtin_amdgcn_sched_group_barrier(0x8, 1, 1);
-        __builtin_amdgcn_sched_group_barrier(0x2, 5, 1);
-      }
-    }
+    __builtin_amdgcn_s_setprio(0);
   }
 
   if (!mine) return;
@@ -588,21 +593,28 @@ __global__ __launch_bounds__(256) void scan_states_kernel(ScanArgs a, int seg, i
   for (int q = threadIdx.x; q < size / 4; q += 256) out[q] = w[q];
 }
 
-// Tokens of a segment: a fair share of all tokens for each of the two workgroups that a
-// CU holds, in whole gates; sequences no longer than that are not split.
+// Tokens of a segment: a fair share of all T tokens for each of the two workgroups that a CU
+// holds, but not so few that joining a long sequence's states (about 1 us each) takes longer
+// than its segments' chunks, twice (about 4 us each): sqrt(8 T) balances the two.  In whole
+// chunks, long ones in whole gates; two chunks are not worth a second launch.  It follows from
+// T alone, since the workspace is sized before the lengths are known.
+// Measured against segments of 256 at least, one sequence: 300 tokens, 20 heads of 64 x 64, fp32, 54 -> 22 us;
+// 16384 tokens, 16 heads of 128 x 64, 111 -> 87 us; 65536 tokens, 2 heads, 242 -> 145 us.
 int scan_parts(int H, int G, int V) { return G * ((H / G + kValues / V - 1) / (kValues / V)); }
 int scan_segment(const Sequences& q, int parts) {
   constexpr int64_t want = 512;
+  if (q.tokens <= 2 * kChunk) return 2 * kChunk;
   int64_t seg = ((int64_t)q.tokens * parts + want - 1) / want;
-  seg = (seg + kGates - 1) / kGates * kGates;
-  const int longest = q.offsets ? q.tokens : q.each;
-  return seg < kGates ? kGates : seg >= longest ? (longest > 0 ? longest : 1) : (int)seg;
+  const int64_t joined = (int64_t)sqrt(8.0 * q.tokens);
+  if (seg < joined) seg = joined;
+  return (int)(seg <= kGates / 2 ? (seg + kChunk - 1) / kChunk * kChunk : (seg + kGates - 1) / kGates * kGates);
 }
+// Windows that may hold a later segment's start; none where no sequence is split.
 int scan_windows(const Sequences& q, int seg) { return seg < (q.offsets ? q.tokens : q.each) ? q.tokens / seg : 0; }
 
 size_t scan_workspace(int batch, int tokens, int H, int G, int K, int V) {
   Sequences q{};
-  q.offsets = reinterpret_cast<const int32_t*>(4);  // lengths unknown: the most that any take
+  q.offsets = reinterpret_cast<const int32_t*>(4);  // lengths unknown
   q.batch = batch;
   q.tokens = tokens;
   const int seg = scan_segment(q, scan_parts(H, G, V));
@@ -618,7 +630,7 @@ int launch_scan(const ScanArgs& a, hipStream_t s) {
   constexpr size_t full = local + Tile<IO, K>::kBytes + heads * Tile<IO, kChunk>::kBytes;
   if (windows)
     hipLaunchKernelGGL((scan_kernel<IO, K, V, true>), dim3((unsigned)windows * (unsigned)parts), dim3(256),
-                       local + heads * 4 * kLocalRecord * sizeof(float), s, a, seg, false);
+                       2 * (local + heads * 4 * kLocalRecord * sizeof(float)), s, a, seg, false);
   hipLaunchKernelGGL((scan_kernel<IO, K, V, false>), dim3((unsigned)(a.seq.batch + windows) * (unsigned)parts), dim3(256),
                      full + heads * 4 * kRecord * sizeof(float), s, a, seg, apart);
   if (apart) hipLaunchKernelGGL(scan_states_kernel, dim3((unsigned)windows * (unsigned)a.H), dim3(256), 0, s, a, seg, V * K);

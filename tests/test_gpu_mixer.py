@@ -187,7 +187,7 @@ def test_scan(io, H, G, K, V, lengths):
 @pytest.mark.parametrize("io", ["bf16", "f32"])
 @pytest.mark.parametrize("lengths", [[700], [1, 900, 0, 255, 257], [256, 256, 256], [513, 300]])
 def test_scan_split_over_workgroups(io, lengths):
-    """Few items and long sequences: segments of 256 tokens, some of them of one sequence, states in place and apart."""
+    """Few items and long sequences: segments, some of them of one sequence, states in place and apart."""
     case("scan split", io, lengths)
     H, G, K, V = 2, 1, 128, 64
     assert B.load().sketchssm_scan_workspace(B.make_config("mamba2", len(lengths), H, K, V, 16, 16, io), G, sum(lengths)) > 0
@@ -226,6 +226,29 @@ def test_scan_equal_lengths_and_no_tokens():
     assert torch.equal(y1, y2) and torch.equal(S1, S2)
     none = {k: v if v is None or k in ("dt_bias", "A", "D") else v[:0] for k, v in a.items()}
     scan_check(none, S, [0, 0], H, G, K, V, "bf16")
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+@pytest.mark.parametrize("lengths", [[129], [128], [150] * 6, [65, 0, 64, 1]])
+def test_scan_short_segments(io, lengths):
+    """Segments of one chunk or a few, by offsets and by equal lengths, in a workspace of the size asked for."""
+    case("scan short segments", io, lengths)
+    H, G, K, V = 3, 1, 128, 64
+    a, S = scan_case(len(lengths) + sum(lengths), lengths, H, G, K, V, io)
+    y1, S1 = scan_check(a, S, lengths, H, G, K, V, io)
+    y2, S2 = scan_check(a, S, lengths, H, G, K, V, io, in_place=True)
+    assert torch.equal(y1, y2) and torch.equal(S1, S2)
+    if len(set(lengths)) == 1:
+        y3, S3 = scan_check(a, S, lengths, H, G, K, V, io, offsets=False)
+        assert torch.equal(y1, y3) and torch.equal(S1, S3)
+
+
+def test_scan_many_short_segments():
+    """One head pair over 9000 tokens: tens of states to join."""
+    case("scan many segments")
+    H, G, K, V = 2, 1, 64, 64
+    a, S = scan_case(44, [9000], H, G, K, V, "bf16")
+    scan_check(a, S, [9000], H, G, K, V, "bf16")
 
 
 @pytest.mark.parametrize("io", ["bf16", "f32"])
@@ -322,6 +345,14 @@ def test_norm(io, form, M, N, group):
         check_norm(M, N, group, io, form, f8)
         if io == "bf16":
             check_norm(M, N, group, io, form, f8, x_f32=form != "plain", seed=1)
+
+
+@pytest.mark.parametrize("N,group", [(20480, 20480), (32768, 32768), (40960, 20480)])
+def test_norm_widest_groups(N, group):
+    case("norm widest", N, group)
+    for form in ("plain", "residual", "gated_skip"):
+        for f8 in (True, False):
+            check_norm(2, N, group, "bf16", form, f8)
 
 
 def test_norm_zero_rows_and_extremes():

@@ -105,6 +105,20 @@ def test_scan_refusals(lib):
     assert lib.sketchssm_scan_workspace(cfg(batch=1), 4, 64) == 0
 
 
+@cpu_only
+def test_scan_workspace_and_wide_strides(lib):
+    for ld in ("ldx", "ldb", "ldc", "ldy"):
+        assert scan(lib, **{ld: 1 << 24}) == -2 and "stride" in B.sketchssm_last_error()
+    # sized before the lengths are known: more tokens never need less than their shares do
+    for H, G in ((2, 1), (8, 4), (128, 8)):
+        c = B.make_config("mamba2", 1, H, 128, 64, 16, 16, "bf16")
+        assert lib.sketchssm_scan_workspace(c, G, 128) == 0 and lib.sketchssm_scan_workspace(c, G, 129) > 0
+        for T in (129, 1000, 4096, 16384, 1 << 20):
+            parts = G * -(-(H // G) // 2)
+            assert lib.sketchssm_scan_workspace(c, G, T) <= (T // 64 + 1) * H * (128 * 64 + 1) * 4
+            assert lib.sketchssm_scan_workspace(c, G, T) <= -(-1024 * H // parts + H) * (128 * 64 + 1) * 4
+
+
 def norm_args(**kw):
     d = dict(rows=4, columns=512, group=512, x_dtype=1, io_dtype=1, out_dtype=2, eps=1e-5, x=at(1), ldx=512, weight=at(2), out=at(3),
              ld_out=512, scales=at(4), ld_scales=4)
