@@ -381,7 +381,8 @@ __global__ __launch_bounds__(256, sizeof(IO) == 2 ? 2 : 1) void scan_kernel(Scan
 #pragma unroll
     for (int q = 0; q < HEADS; ++q) {
       dt[q] = p + tid < s.p1 ? softplus(raw[q] + bias[q]) : 0.f;
-      sum[q] = wave_scan((double)fmaxf(dt[q] * A2[q], -150.f));
+      const float log = dt[q] * A2[q];
+      sum[q] = wave_scan((double)(log < -150.f ? -150.f : log));  // (NaN stays)
     }
     if (p + kGates < s.p1) steps(p + kGates);
 #pragma unroll
