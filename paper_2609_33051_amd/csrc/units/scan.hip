@@ -39,15 +39,16 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short shortx4 __attribute__((ext_vector_type(4)));
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 
-// 64 rows of COLS elements in LDS.  The 16-byte chunks of a row are permuted by the row:
-// pairs of chunks by its low two bits, so that the four rows of 32 bytes that a transposed
-// read takes lie in different banks, and the two of a pair by the next bit, so that 16
-// bytes of eight consecutive rows do.
+// 64 rows of COLS elements in LDS.  The 16-byte chunks of a row are permuted by the row, so
+// that neither of two reads finds its lanes in the same banks: 16 bytes of 16 consecutive
+// rows, and the transposed read's four rows of 64 bytes (rows of 128 bytes differ by their
+// place already where they follow one another).
 template <typename IO, int COLS> struct Tile {
   static constexpr int kBytes = kChunk * COLS * (int)sizeof(IO), kChunks = COLS * (int)sizeof(IO) / 16;
   static constexpr int kPer = 16 / (int)sizeof(IO);  // elements of a chunk
   static __device__ __forceinline__ int at(int row, int col) {  // byte offset
-    return row * (COLS * (int)sizeof(IO)) + (((col / kPer) ^ (((row & 3) << 1) | ((row >> 2) & 1))) << 4) + (col % kPer) * (int)sizeof(IO);
+    const int key = (kChunks >= 16 ? (row & 3) << 2 : (row & 2) << 1) | ((row >> 2) & 3);
+    return row * (COLS * (int)sizeof(IO)) + (((col / kPer) ^ key) << 4) + (col % kPer) * (int)sizeof(IO);
   }
 };
 
