@@ -66,6 +66,7 @@ int sketchssm_conv(const skssm_conv_config* cfg, int32_t batch, int64_t tokens, 
   const int e = elem(cfg->io_dtype), C = cfg->channels, w = cfg->width;
   if (C < 1) return fail(SKSSM_EINVAL, "%s: channels must be >= 1", what);
   if ((int64_t)C * e % 16) return fail(SKSSM_EUNSUPPORTED, "%s: %d channels are not a multiple of 16 bytes", what, C);
+  if (C > kMaxTokens) return fail(SKSSM_EUNSUPPORTED, "%s: %d channels: at most 2^30", what, C);
   if (w < 2 || w > 4) return fail(SKSSM_EUNSUPPORTED, "%s: width %d outside 2..4", what, w);
   if (cfg->silu != 0 && cfg->silu != 1) return fail(SKSSM_EINVAL, "%s: silu must be 0 or 1", what);
   int rc = check_packed(what, batch, tokens, offsets);
@@ -105,6 +106,7 @@ int sketchssm_conv_token(const skssm_config* cfg, int32_t groups, int32_t width,
   if (width < 2 || width > 4) return fail(SKSSM_EUNSUPPORTED, "%s: width %d outside 2..4", what, width);
   const int e = elem(cfg->io_dtype);
   const int64_t B = cfg->batch, H = cfg->heads, C = H * cfg->dv + 2 * (int64_t)groups * cfg->dk;
+  if (C > kMaxTokens) return fail(SKSSM_EUNSUPPORTED, "%s: %lld channels: at most 2^30", what, (long long)C);
   if (n_buffered < 0 || n_buffered >= cfg->window)
     return fail(SKSSM_ESTATE, "%s: n_buffered %d outside 0..%d", what, n_buffered, cfg->window - 1);
   if (!x || !taps || !state || !dt || !A || !q) return fail(SKSSM_EINVAL, "%s: x, taps, state, dt, A and q are required", what);
@@ -121,6 +123,9 @@ int sketchssm_conv_token(const skssm_config* cfg, int32_t groups, int32_t width,
   for (const auto& o : out)
     if (overlap(o.p, o.n, x, span(B, ldx, C, e)) || overlap(o.p, o.n, dt, span(B, lddt, H, e)))
       return fail(SKSSM_EINVAL, "%s: x or dt overlaps what is written", what);
+  for (int i = 0; i < 6; ++i)
+    for (int j = 0; j < i; ++j)
+      if (overlap(out[i].p, out[i].n, out[j].p, out[j].n)) return fail(SKSSM_EINVAL, "%s: the arrays that are written overlap", what);
   skssm::ConvTokenArgs a{};
   a.B = cfg->batch;
   a.H = cfg->heads;

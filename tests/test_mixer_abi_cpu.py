@@ -81,6 +81,16 @@ def test_conv_token_refusals(lib):
     assert token(lib, dt=at(4)) == -1
 
 
+@cpu_only
+def test_conv_wide_and_token_overlaps(lib):
+    wide = (1 << 31) - 8
+    assert conv(lib, C=wide, ldx=1 << 31, ldy=1 << 31) == -2 and "2^30" in B.sketchssm_last_error()
+    assert token(lib, c=cfg(heads=1 << 24, batch=1), G=1, ldx=1 << 31, lddt=1 << 24) == -2
+    assert token(lib, q=at(4)) == -1 and "written overlap" in B.sketchssm_last_error()
+    assert token(lib, ring=B.make_ring(k=at(8), v=at(8) + 64, beta=at(10), log_decay=at(11))) == -1
+    assert token(lib, ring=B.make_ring(k=at(8), v=at(9), beta=at(10), log_decay=at(10))) == -1
+
+
 def scan(lib, c=None, G=4, T=64, off=at(1), x=at(2), ldx=512, b=at(3), ldb=512, cc=at(4), ldc=512, dt=at(5), lddt=8, bias=None, A=at(6),
          D=None, s_in=None, s_out=at(7), y=at(8), ldy=512, ws=None, nws=0):
     return lib.sketchssm_scan(c or cfg(), G, T, off, x, ldx, b, ldb, cc, ldc, dt, lddt, bias, A, D, s_in, s_out, y, ldy, ws, nws, None)
