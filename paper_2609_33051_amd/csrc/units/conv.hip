@@ -188,7 +188,9 @@ int run_conv(const ConvArgs& a, int width, int io, int silu, bool states_apart, 
 // them in LDS and writes them to every head of the group (ring.k and q): those
 // writes, H (V + 2 K) values a request against the H V + 2 G K that are read, are
 // half of what the call moves.  A thread's taps and bias, 10 bytes for each byte of x,
-// serve RB requests.
+// serve RB requests.  10240 channels bf16, 8 groups of 16 heads, RB = 1 / 4 (us): 32 requests 4.5 / 5.5,
+// 128 8.7 / 9.2, 170 12.0 / 9.9, 256 15.9 / 11.5 (5.0 TB/s), 1024 69 / 64 (3.6: past the caches the
+// slots' 128 and 256 byte pieces cost).
 template <typename IO, int W, int RB>
 __global__ __launch_bounds__(256) void conv_token_kernel(ConvTokenArgs a, int xparts) {
   constexpr int CH = 16 / sizeof(IO);
@@ -258,8 +260,8 @@ int launch_conv_token(const ConvTokenArgs& a, hipStream_t s) {
   constexpr int CH = 16 / sizeof(IO);
   const int xparts = (a.H * a.V / CH + 255) / 256;
   const unsigned parts = (unsigned)(xparts + a.G);
-  // four requests a workgroup where that leaves two workgroups a CU
-  if ((int64_t)parts * a.B >= 4 * 512)
+  // four requests a workgroup where that leaves seven workgroups for four CUs
+  if ((int64_t)parts * a.B >= 4 * 448)
     hipLaunchKernelGGL((conv_token_kernel<IO, W, 4>), dim3(parts * (unsigned)((a.B + 3) / 4)), dim3(256), 0, s, a, xparts);
   else
     hipLaunchKernelGGL((conv_token_kernel<IO, W, 1>), dim3(parts * (unsigned)a.B), dim3(256), 0, s, a, xparts);
