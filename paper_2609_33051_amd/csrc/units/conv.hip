@@ -24,6 +24,29 @@ template <typename IO, int W> struct Taps {
       for (int j = 0; j < W; ++j) t[j][i] = r.get(i * W + j);
     }
   }
+  // The same for the 64 lanes of a wave whose first channel is c0, by `threads` threads through LDS: lanes
+  // lie 128 bytes apart in the array (bf16, four taps), and an instruction that loads 16 of each would
+  // take the 64 lines one after the other.  A lane's place in LDS is an odd number of 16 bytes.
+  static constexpr int NT = CH * W / 4, NB = CH / 4, ST = NT | 1, SB = NB | 1, kShared = 64 * (ST + SB);  // in 16 bytes
+  static __device__ __forceinline__ void share(uint4* lds, const float* taps, const float* bias, int c0, int C, int tid, int threads) {
+    const int n = min(64 * CH, C - c0) / CH;  // lanes that have channels
+    for (int j = tid; j < n * NT; j += threads) lds[j / NT * ST + j % NT] = reinterpret_cast<const uint4*>(taps + (size_t)c0 * W)[j];
+    for (int j = tid; j < n * NB; j += threads)
+      lds[64 * ST + j / NB * SB + j % NB] = bias ? reinterpret_cast<const uint4*>(bias + c0)[j] : make_uint4(0, 0, 0, 0);
+  }
+  __device__ __forceinline__ void load(const uint4* lds, int lane) {
+    float r[4 * NT], rb[4 * NB];
+#pragma unroll
+    for (int j = 0; j < NT; ++j) __builtin_memcpy(r + 4 * j, lds + lane * ST + j, 16);
+#pragma unroll
+    for (int j = 0; j < NB; ++j) __builtin_memcpy(rb + 4 * j, lds + 64 * ST + lane * SB + j, 16);
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+      b[i] = rb[i];
+#pragma unroll
+      for (int j = 0; j < W; ++j) t[j][i] = r[i * W + j];
+    }
+  }
   // z of the window's W inputs, oldest first
   __device__ __forceinline__ float sum(const Raw<IO, CH>* win, int i) const {
     float z = b[i];
@@ -51,12 +74,13 @@ __device__ __forceinline__ Raw<IO, 16 / sizeof(IO)> conv_row(const Taps<IO, W>& 
   return y;
 }
 
-// Tokens of a workgroup, loaded together: 16, or 8 where 16 would leave less than
-// four workgroups a CU.  16384 x 10240 bf16 (four taps): 127.7 us, 5.26 TB/s, what a copy
-// of its size reaches (5.1 to 5.4); two loads of 8 133, 32 tokens as four loads of 8 139,
-// 64 154, and 32 with ordinary loads and stores 150 (nothing here is read twice but
-// the w - 1 tokens before a workgroup's).  777 x 1792 fp32: 6.5 us with 16, 5.4 with 8.
-constexpr int kConvRows = 16, kConvFew = 8;
+// Tokens of a wave, loaded together, and waves of a workgroup, one below the other on the
+// same 64 lanes of channels, so that they share their taps: 12, or 4 where there would be fewer than ten for
+// each SIMD.  Measured, rows of 10240 bf16, four taps, 12 / 4 (us): 16384 tokens 122 / 138 (5.5 TB/s, 91 % of what the
+// same loads and stores reach without the sums, 110; 16 tokens 123, 8 129), 4096 37.1 / 38.9,
+// 512 6.5 / 7.5, 256 5.7 / 4.8; 777 x 1792 fp32 6.9 / 5.2.  Each thread loading its own taps took 128 for the
+// first; a workgroup of 16 tokens by 4 KB, which only reads what it writes, 114.
+constexpr int kConvRows = 12, kConvFew = 4, kDown = 4;
 
 template <typename IO, int CH> __device__ __forceinline__ void store_nt(const Raw<IO, CH>& r, IO* p) {
   static_assert(sizeof(r) == 16, "one store");
@@ -84,82 +108,96 @@ __device__ __forceinline__ void conv_state(const ConvArgs& a, int b, int c) {
 }
 
 template <typename IO, int W, bool SILU, int ROWS>
-__global__ __launch_bounds__(256) void conv_kernel(ConvArgs a, int cols, int tiles) {
+__global__ __launch_bounds__(64 * kDown) void conv_kernel(ConvArgs a, int cols, int tiles, int states) {
   constexpr int CH = 16 / sizeof(IO);
-  const int c = ((blockIdx.x % cols) * 256 + threadIdx.x) * CH;
-  const int part = blockIdx.x / cols;
-  if (c >= a.C) return;
-  if (part >= tiles) {
-    conv_state<IO, W>(a, part - tiles, c);
-    return;
-  }
-  const int T = a.seq.tokens, t0 = part * ROWS, t1 = min(T, t0 + ROWS);
-  Taps<IO, W> k;
-  k.load(a.taps, a.bias, c);
+  __shared__ uint4 shared[Taps<IO, W>::kShared];
+  const int lane = threadIdx.x & 63, c0 = (blockIdx.x % cols) * 64 * CH, c = c0 + lane * CH;
+  const int part = blockIdx.x / cols * kDown + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int T = a.seq.tokens, t0 = part * ROWS;
+  const bool work = part < tiles && c < a.C;
   const IO* x = static_cast<const IO*>(a.x) + c;
   IO* y = static_cast<IO*>(a.y) + c;
   const IO* in = static_cast<const IO*>(a.state_in);
 
+  // the window, then the rows: loaded before the sequence is known, which takes loads of its own
+  Raw<IO, CH> win[W - 1 + ROWS];
+  if (work) {
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) win[W - 1 + i].load_nt(x + (size_t)min(t0 + i, T - 1) * a.ldx);
+#pragma unroll
+    for (int j = 0; j < W - 1; ++j) win[j].load(x + (size_t)max(t0 - (W - 1) + j, 0) * a.ldx);
+  }
   // lo is held to the row (offsets that do not start at 0), so that a state's row index stays in 0..W-2
-  int b = a.seq.of(t0), lo = min(t0, a.seq.start(b)), hi = a.seq.start(b + 1);
-  Raw<IO, CH> win[W - 1 + ROWS];  // the window, then the rows
-  // the W - 1 inputs before row t of sequence b
-  auto before = [&](int t) {
-#pragma unroll
-    for (int j = 0; j < W - 1; ++j) {
-      const int p = t - (W - 1) + j, s = p - lo + (W - 1);  // row of x; row of the state
-      if (p >= lo) win[j].load(x + (size_t)p * a.ldx);
-      else if (in) win[j].load(in + ((size_t)b * (W - 1) + s) * a.C + c);
-      else win[j].zero();
-    }
+  int b = 0, lo = 0, hi = 0;
+  if (part < tiles) {
+    b = a.seq.of(t0);
+    lo = min(t0, a.seq.start(b));
+    hi = a.seq.start(b + 1);
+  }
+  // row p < lo: one of the state's
+  auto past = [&](Raw<IO, CH>& r, int p) {
+    if (in) r.load(in + ((size_t)b * (W - 1) + (p - lo + (W - 1))) * a.C + c);
+    else r.zero();
   };
-  if (t0 + ROWS <= min(T, hi)) {  // all of one sequence
+  const bool whole = work && t0 + ROWS <= min(T, hi);  // all of one sequence
+  if (whole) {
 #pragma unroll
-    for (int i = 0; i < ROWS; ++i) win[W - 1 + i].load_nt(x + (size_t)(t0 + i) * a.ldx);
-    before(t0);
+    for (int j = 0; j < W - 1; ++j)
+      if (t0 - (W - 1) + j < lo) past(win[j], t0 - (W - 1) + j);
+  }
+  Taps<IO, W>::share(shared, a.taps, a.bias, c0, a.C, threadIdx.x, 64 * kDown);
+  lds_barrier();
+  if (!work) {
+    if (part >= tiles && part - tiles < states && c < a.C) conv_state<IO, W>(a, part - tiles, c);
+    return;
+  }
+  Taps<IO, W> k;
+  k.load(shared, lane);
+  if (whole) {
 #pragma unroll
     for (int i = 0; i < ROWS; ++i) store_nt<IO, CH>(conv_row<IO, W, SILU>(k, win + i), y + (size_t)(t0 + i) * a.ldy);
     return;
   }
-  before(t0);
-  for (int t = t0; t < t1;) {
+#pragma unroll
+  for (int i = 0; i < ROWS; ++i) {
+    const int t = t0 + i;
+    if (t >= T) break;
     if (t >= hi && b + 1 < a.seq.batch) {  // the next sequence that has tokens (or the last one)
       do {
         ++b;
-        lo = a.seq.start(b);
         hi = a.seq.start(b + 1);
       } while (t >= hi && b + 1 < a.seq.batch);
-      lo = min(t, lo);
-      before(t);
+      lo = min(t, a.seq.start(b));
     }
-    const int end = t >= hi ? t1 : min(t1, hi);  // of this sequence here
-    for (; t < end; ++t) {
-      win[W - 1].load(x + (size_t)t * a.ldx);
-      store_nt<IO, CH>(conv_row<IO, W, SILU>(k, win), y + (size_t)t * a.ldy);
+    Raw<IO, CH> w[W];
 #pragma unroll
-      for (int j = 0; j < W - 1; ++j) win[j] = win[j + 1];
+    for (int j = 0; j < W; ++j) {
+      if (t - (W - 1) + j >= lo) w[j] = win[i + j];
+      else past(w[j], t - (W - 1) + j);
     }
+    store_nt<IO, CH>(conv_row<IO, W, SILU>(k, w), y + (size_t)t * a.ldy);
   }
 }
 
 template <typename IO, int W, bool SILU, int ROWS>
 int launch_conv_rows(const ConvArgs& a, bool apart, hipStream_t s) {
   constexpr int CH = 16 / sizeof(IO);
-  const int cols = (a.C / CH + 255) / 256, tiles = (a.seq.tokens + ROWS - 1) / ROWS;
-  const int states = a.state_out ? a.seq.batch : 0;
-  const unsigned first = (unsigned)cols * (unsigned)(tiles + (apart ? 0 : states));
-  if (first) hipLaunchKernelGGL((conv_kernel<IO, W, SILU, ROWS>), dim3(first), dim3(256), 0, s, a, cols, tiles);
+  const int cols = (a.C / CH + 63) / 64, tiles = (a.seq.tokens + ROWS - 1) / ROWS;
+  const int states = a.state_out ? a.seq.batch : 0, with = apart ? 0 : states;
+  const unsigned first = (unsigned)cols * (unsigned)((tiles + with + kDown - 1) / kDown);
+  if (first) hipLaunchKernelGGL((conv_kernel<IO, W, SILU, ROWS>), dim3(first), dim3(64 * kDown), 0, s, a, cols, tiles, with);
   // the new states in place of the old ones: after the outputs, which read those
   if (apart && states)
-    hipLaunchKernelGGL((conv_kernel<IO, W, SILU, ROWS>), dim3((unsigned)cols * (unsigned)states), dim3(256), 0, s, a, cols, 0);
+    hipLaunchKernelGGL((conv_kernel<IO, W, SILU, ROWS>), dim3((unsigned)cols * (unsigned)((states + kDown - 1) / kDown)), dim3(64 * kDown), 0, s,
+                       a, cols, 0, states);
   return 0;
 }
 
 template <typename IO, int W, bool SILU>
 int launch_conv(const ConvArgs& a, bool apart, hipStream_t s) {
-  const int64_t cols = (a.C / (16 / (int)sizeof(IO)) + 255) / 256;
-  return cols * a.seq.tokens >= 4 * 256 * kConvRows ? launch_conv_rows<IO, W, SILU, kConvRows>(a, apart, s)
-                                                    : launch_conv_rows<IO, W, SILU, kConvFew>(a, apart, s);
+  const int64_t cols = (a.C / (16 / (int)sizeof(IO)) + 63) / 64;
+  return cols * a.seq.tokens >= 10 * 1024 ? launch_conv_rows<IO, W, SILU, kConvRows>(a, apart, s)
+                                          : launch_conv_rows<IO, W, SILU, kConvFew>(a, apart, s);
 }
 
 template <typename IO, int W>
