@@ -112,10 +112,11 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(NormArgs a) {
 }
 
 // Threads and 8-column pieces a thread, by the group's width.  8192 rows with the residual into
-// 8 bits, bf16 (us, share of a copy's 5.2 TB/s): 1024 columns 11.7, 2048 23.2 (97 %; 256
-// threads 26.4), 4096 46.6 (97 %), 8192 90 (100 %; 1024 threads 92.8); 16384 columns of
-// an ordinary norm 93.9 (82 %; 1024 threads 108); gated, 8192 columns by groups of 1024 68.7 (94 %).
-// Reads past the caches move these by -4 % to +18 % (the latter where they fit them).
+// 8 bits, bf16 (us; the best copy moves 6.4 TB/s): 1024 columns 11.7, 2048 23.2 to 25 (5.0 TB/s; 256
+// threads 26.4), 4096 46.6 (5.0), 8192 90 (5.2; 1024 threads 92.8); 16384 columns of
+// an ordinary norm 93.9 (4.3; 1024 threads 108); gated, 8192 columns by groups of 1024 68.7 (4.9).
+// Reads past the caches move these by -4 % to +18 %, reads and writes past them by -9 % to +9 %:
+// they gain where nothing is used again soon and lose where it is, and a norm's output is.
 template <typename TX, typename IO, bool FP8, int FORM>
 int launch_norm(const NormArgs& a, hipStream_t s) {
   const dim3 grid((unsigned)a.rows * (unsigned)(a.columns / a.group));
