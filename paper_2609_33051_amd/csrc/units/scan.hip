@@ -229,6 +229,25 @@ __device__ __forceinline__ double lane_of(double x, int lane) {
   return __builtin_bit_cast(double, make_uint2(__builtin_amdgcn_readlane((int)u.x, lane), __builtin_amdgcn_readlane((int)u.y, lane)));
 }
 
+// The sequence that is `rank`-th by length, longest first: workgroups start in this order, so
+// that the card does not wait for a long sequence that began last.  (37 prompts of 0 to
+// 1214 tokens, 128 heads: 218 -> 211 us.)  Each workgroup of 256 threads counts for itself, a thread
+// a sequence; of more than 256 one is little of the whole.
+__device__ __forceinline__ int by_length(const Sequences& q, int rank, int* lds, int tid) {
+  if (!q.offsets || q.batch < 2 || q.batch > 256) return rank;
+  const int length = tid < q.batch ? q.start(tid + 1) - q.start(tid) : 0;
+  lds[tid] = length;
+  lds_barrier();
+  int before = 0;
+  for (int b = 0; b < q.batch; ++b) {
+    const int other = lds[b];
+    before += other > length || (other == length && b < tid);
+  }
+  if (tid < q.batch && before == rank) lds[256] = tid;
+  lds_barrier();
+  return __builtin_amdgcn_readfirstlane(lds[256]);
+}
+
 // LOCAL: the state part alone, over the segment before the slot's (first launch).
 template <typename IO, int K, int V, bool LOCAL>
 __global__ __launch_bounds__(256, sizeof(IO) == 2 ? 2 : 1) void scan_kernel(ScanArgs a, int seg, bool apart) {
@@ -251,19 +270,19 @@ __global__ __launch_bounds__(256, sizeof(IO) == 2 ? 2 : 1) void scan_kernel(Scan
   const bool mine = hl < heads;                          // (an odd group's last workgroup has one head)
   const int h = h0 + (mine ? hl : 0), vbase = HEADS == 2 ? 32 * (wave & 1) : 32 * wave;
 
+  extern __shared__ __attribute__((aligned(16))) char lds[];
   Segment s;
+  const int windows = LOCAL ? 0 : (int)gridDim.x / parts - a.seq.batch;
   if (LOCAL) {
     if (!s.later(a.seq, slot + 1, seg)) return;
     s.p1 = s.p0;
     s.p0 -= seg;
     --s.k;
-  } else if (slot < a.seq.batch) {
-    s.first(a.seq, slot, seg);
-  } else if (!s.later(a.seq, slot - a.seq.batch + 1, seg)) {
-    return;
+  } else if (slot < windows) {
+    if (!s.later(a.seq, slot + 1, seg)) return;
+  } else {
+    s.first(a.seq, by_length(a.seq, slot - windows, reinterpret_cast<int*>(lds), tid), seg);
   }
-
-  extern __shared__ __attribute__((aligned(16))) char lds[];
   char* lb = lds;  // (LOCAL: of two buffers in turn)
   char* lx = lb + TB::kBytes;
   char* const lc = lx + TX::kBytes;
@@ -587,7 +606,7 @@ __global__ __launch_bounds__(256, sizeof(IO) == 2 ? 2 : 1) void scan_kernel(Scan
   } else if (s.p1 == s.hi) {
     // S_out in place of S_in: other segments' workgroups may still read it, so that a later
     // segment leaves its state where only this workgroup reads, for a copy after the launch
-    put_state(apart && s.k > 0 ? work_at(slot - a.seq.batch + 1) : a.S_out + ((size_t)s.b * a.H + h) * (V * K));
+    put_state(apart && s.k > 0 ? work_at(slot + 1) : a.S_out + ((size_t)s.b * a.H + h) * (V * K));
   }
 }
 
