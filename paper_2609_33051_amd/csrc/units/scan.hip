@@ -24,7 +24,7 @@
 //
 // Measured, 128 heads of 128 x 64 in 8 groups, bf16: one prompt of 16384 tokens 331 us (states 110,
 // outputs 220; its bytes take 96 at the best copy's rate, its products in this form 100 of
-// the matrix units'), 37 prompts of 12000 tokens 219 us.  Matrix and vector units add up to
+// the matrix units'), 37 prompts of 12000 tokens 212 us.  Matrix and vector units add up to
 // 96 % of the first launch's time and 87 % of the second's: what is left is
 // waiting at the barriers and for LDS, with the two waves a SIMD that registers and LDS allow.
 #include <math.h>
@@ -272,16 +272,15 @@ __global__ __launch_bounds__(256, sizeof(IO) == 2 ? 2 : 1) void scan_kernel(Scan
 
   extern __shared__ __attribute__((aligned(16))) char lds[];
   Segment s;
-  const int windows = LOCAL ? 0 : (int)gridDim.x / parts - a.seq.batch;
   if (LOCAL) {
     if (!s.later(a.seq, slot + 1, seg)) return;
     s.p1 = s.p0;
     s.p0 -= seg;
     --s.k;
-  } else if (slot < windows) {
-    if (!s.later(a.seq, slot + 1, seg)) return;
-  } else {
-    s.first(a.seq, by_length(a.seq, slot - windows, reinterpret_cast<int*>(lds), tid), seg);
+  } else if (slot < a.seq.batch) {
+    s.first(a.seq, by_length(a.seq, slot, reinterpret_cast<int*>(lds), tid), seg);
+  } else if (!s.later(a.seq, slot - a.seq.batch + 1, seg)) {
+    return;
   }
   char* lb = lds;  // (LOCAL: of two buffers in turn)
   char* lx = lb + TB::kBytes;
@@ -606,7 +605,7 @@ __global__ __launch_bounds__(256, sizeof(IO) == 2 ? 2 : 1) void scan_kernel(Scan
   } else if (s.p1 == s.hi) {
     // S_out in place of S_in: other segments' workgroups may still read it, so that a later
     // segment leaves its state where only this workgroup reads, for a copy after the launch
-    put_state(apart && s.k > 0 ? work_at(slot + 1) : a.S_out + ((size_t)s.b * a.H + h) * (V * K));
+    put_state(apart && s.k > 0 ? work_at(slot - a.seq.batch + 1) : a.S_out + ((size_t)s.b * a.H + h) * (V * K));
   }
 }
 
@@ -626,7 +625,7 @@ __global__ __launch_bounds__(256) void scan_states_kernel(ScanArgs a, int seg, i
 // chunks, long ones in whole gates; two chunks are not worth a second launch.  It follows from
 // T alone, since the workspace is sized before the lengths are known.
 // Measured against segments of 256 at least, one sequence: 300 tokens, 20 heads of 64 x 64, fp32, 54 -> 22 us;
-// 16384 tokens, 16 heads of 128 x 64, 111 -> 87 us; 65536 tokens, 2 heads, 242 -> 145 us.
+// 16384 tokens, 16 heads of 128 x 64, 111 -> 81 us; 65536 tokens, 2 heads, 242 -> 123 us.
 int scan_parts(int H, int G, int V) { return G * ((H / G + kValues / V - 1) / (kValues / V)); }
 int scan_segment(const Sequences& q, int parts) {
   constexpr int64_t want = 512;
