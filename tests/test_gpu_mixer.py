@@ -243,6 +243,15 @@ def test_scan_short_segments(io, lengths):
         assert torch.equal(y1, y3) and torch.equal(S1, S3)
 
 
+@pytest.mark.parametrize("lengths", [[(7 * i) % 11 for i in range(256)], [(5 * i) % 9 for i in range(300)], [4] * 33])
+def test_scan_many_sequences(lengths):
+    """Every sequence is scanned once, whatever order the workgroups take them in: equal lengths, empty ones, more than are sorted."""
+    case("scan many sequences", len(lengths))
+    H, G, K, V = 2, 1, 64, 64
+    a, S = scan_case(len(lengths), lengths, H, G, K, V, "bf16")
+    scan_check(a, S, lengths, H, G, K, V, "bf16")
+
+
 def test_scan_many_short_segments():
     """One head pair over 9000 tokens: tens of states to join."""
     case("scan many segments")
