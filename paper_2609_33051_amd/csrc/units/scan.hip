@@ -22,9 +22,9 @@
 // sequence's last, from zero (the first: from S_in), and keeps its end state and
 // total decay; the second begins each segment from the states before it, joined.
 //
-// Measured, 128 heads of 128 x 64 in 8 groups, bf16: one prompt of 16384 tokens 331 us (states 110,
+// Measured, 128 heads of 128 x 64 in 8 groups, bf16: one prompt of 16384 tokens 330 us (states 110,
 // outputs 220; its bytes take 96 at the best copy's rate, its products in this form 100 of
-// the matrix units'), 37 prompts of 12000 tokens 212 us.  Matrix and vector units add up to
+// the matrix units'), 37 prompts of 12000 tokens 211 us.  Matrix and vector units add up to
 // 96 % of the first launch's time and 87 % of the second's: what is left is
 // waiting at the barriers and for LDS, with the two waves a SIMD that registers and LDS allow.
 #include <math.h>
