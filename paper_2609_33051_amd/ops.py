@@ -241,7 +241,7 @@ def norm(x: Tensor, weight: Tensor, eps: float, *, group: int | None = None, res
         if scales is None:
             scales, a.ld_scales = x.new_empty((-(-N // 128), M), dtype=_F32), M
         else:
-            a.ld_scales = max(M, _rows("scales", scales, -(-N // 128), M, dev))
+            a.ld_scales = _rows("scales", scales, -(-N // 128), M, dev)
         a.scales = scales.data_ptr()
     elif scales is not None:
         raise ValueError("scales without an 8-bit output")
@@ -254,8 +254,9 @@ def norm(x: Tensor, weight: Tensor, eps: float, *, group: int | None = None, res
 def _rows(name: str, x: Tensor, rows: int, columns: int, dev: int) -> int:
     """The row stride of a float32 matrix of scales."""
     if (x.dim() != 2 or x.shape[0] != rows or x.shape[1] != columns or x.dtype is not _F32 or x.get_device() != dev
-            or x.stride(1) != 1 and columns > 1):
-        raise ValueError(f"{name}: a {_F32} tensor [{rows}][{columns}] with contiguous rows on cuda:{dev} is needed, not {_said(x)}")
+            or x.stride(1) != 1 and columns > 1 or x.stride(0) < columns and rows > 1):
+        raise ValueError(f"{name}: a {_F32} tensor [{rows}][{columns}] with contiguous rows that do not overlap on cuda:{dev} is needed, "
+                         f"not {_said(x)}")
     return x.stride(0) if rows > 1 else columns
 
 
@@ -280,7 +281,7 @@ def matmul_fp8(a: Tensor, a_scale: Tensor, w: Tensor, w_scale: Tensor, *, out_dt
     if workspace is None and need:
         workspace = a.new_empty(need, dtype=torch.uint8)
     rc = lib.sketchssm_matmul_fp8(M, N, K, a.data_ptr(), _matrix("a", a, (M, K), F8, dev), a_scale.data_ptr(),
-                                  max(M, _rows("a_scale", a_scale, kb, M, dev)), w.data_ptr(), _matrix("w", w, (N, K), F8, dev),
+                                  _rows("a_scale", a_scale, kb, M, dev), w.data_ptr(), _matrix("w", w, (N, K), F8, dev),
                                   _flat("w_scale", w_scale, (-(-N // 128), kb), _F32, dev), _IO[t], out.data_ptr(),
                                   out.stride(0) if M > 1 else N, *_space(workspace, dev), _stream(dev))
     if rc:

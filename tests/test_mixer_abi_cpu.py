@@ -217,3 +217,16 @@ def test_struct_sizes_match_c():
     """The ctypes mirror of skssm_norm_args has the C layout (offsets of its last fields, natural alignment)."""
     assert ctypes.sizeof(B.NormArgs) % 8 == 0 and B.NormArgs.eps.offset == 32 and B.NormArgs.x.offset == 40
     assert B.NormArgs.ld_scales.offset == ctypes.sizeof(B.NormArgs) - 8
+
+
+@pytest.mark.parametrize("rows,columns", [(2, 8), (3, 1), (5, 100)])
+def test_scale_rows_that_overlap_are_refused(rows, columns):
+    """Rows of scales that share memory (broadcast, or a stride below their length): a stride
+    of the row's length in their place would leave the array."""
+    one = torch.ones((1, columns))
+    for x in (one.expand(rows, columns), torch.ones(rows * columns).as_strided((rows, columns), (columns - 1, 1))):
+        with pytest.raises(ValueError, match="scales"):
+            ops._rows("scales", x, rows, columns, -1)
+    assert ops._rows("scales", torch.ones((rows, columns + 3))[:, :columns], rows, columns, -1) == columns + 3
+    assert ops._rows("scales", one, 1, columns, -1) >= columns
+    assert ops._rows("scales", torch.ones((rows, 0)), rows, 0, -1) >= 0
