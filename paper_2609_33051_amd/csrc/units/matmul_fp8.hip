@@ -70,13 +70,12 @@ template <int RUN> __device__ __forceinline__ int key_w(int row) { return (row &
 // 16 (4) bytes a lane from base + at into LDS, the wave's 64 lanes one after the other
 // from `lds`.  In assembly, as the compiler would wait for every such load before the next
 // LDS read, whatever it reads; the caller waits (vmcnt) before the barrier that
-// publishes a stage.  No register is written but M0, which nothing else here reads
-// (gfx950's LDS instructions do not).
+// publishes a stage.  The load takes M0 one wait state after it is written.
 __device__ __forceinline__ void to_lds16(const void* base, uint32_t at, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(at), "s"(base) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(at), "s"(base) : "memory", "m0");
 }
 __device__ __forceinline__ void to_lds4(const void* base, uint32_t at, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds), "v"(at), "s"(base) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds), "v"(at), "s"(base) : "memory", "m0");
 }
 __device__ __forceinline__ uint32_t lds_address(const void* p) {
   return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p;

@@ -1,0 +1,37 @@
+"""The machine code of the kernels built here, where correctness hangs on it:
+a scalar write of M0 and a load into LDS that takes its address from M0 need one
+wait state between them, which the compiler does not add inside assembly text."""
+import os
+import re
+import subprocess
+
+import pytest
+
+from paper_2609_33051_amd import build
+from test_kernel_resources import _code_objects
+
+OBJDUMP = os.path.join(os.path.dirname(os.path.realpath(build.HIPCC)), "..", "llvm", "bin", "llvm-objdump")
+
+
+@pytest.fixture(scope="module")
+def listing(tmp_path_factory):
+    """The instructions of the code object that holds the 8-bit products."""
+    if not os.path.exists(OBJDUMP):
+        pytest.skip("no llvm-objdump")
+    if not os.path.exists(build.LIB):
+        build.build()
+    for elf in _code_objects(open(build.LIB, "rb").read()):
+        if b"matmul_tile_kernel" in elf:
+            f = tmp_path_factory.mktemp("code") / "matmul.elf"
+            f.write_bytes(elf)
+            text = subprocess.run([OBJDUMP, "-d", "--no-show-raw-insn", f], capture_output=True, text=True, check=True).stdout
+            return [line.split("//")[0].strip() for line in text.split("\n") if re.match(r"^\s+[a-z]", line)]
+    pytest.fail("no code object holds the 8-bit products")
+
+
+def test_m0_is_settled_before_a_load_into_lds(listing):
+    loads = [i for i, x in enumerate(listing) if re.match(r"(global|buffer)_load_lds_|buffer_load_\w+ .*\blds\b", x)]
+    assert len(loads) > 100
+    for i in loads:
+        assert not re.match(r"s_\w+ m0,", listing[i - 1]), f"{listing[i - 1]} / {listing[i]}"
+        assert any(re.match(r"s_\w+ m0,", x) for x in listing[i - 4:i]), listing[i - 4:i + 1]
