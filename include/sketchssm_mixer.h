@@ -85,7 +85,8 @@ int sketchssm_conv_token(const skssm_config* cfg, int32_t groups, int32_t width,
  * sketchssm_update(q = NULL) can follow.  y [T][heads*dv] io may not overlap
  * the inputs.  The state and every sum are fp32; with bf16 io the products
  * inside a chunk of tokens take bf16 operands (the decayed scores and the state
- * as read by C_t are rounded to nearest), while what enters the state keeps 24 bits.
+ * as read by C_t are rounded to nearest), while what enters the state keeps 24 bits and D x_t
+ * is fp32.
  * Row strides of x, b, c and y are less than 2^24.  A value that is not finite stays in its
  * head (x, dt) or group (b, c) and its sequence; within its chunk of 64 tokens it may
  * reach the outputs of tokens before it.

@@ -386,11 +386,11 @@ __global__ __launch_bounds__(256, sizeof(IO) == 2 ? 2 : 1) void scan_kernel(Scan
   //   kLeft   dt_s 2^{g_L - g_s}            kEnd   g_L
   // LOCAL keeps kLeft and kEnd.
   auto record = [&](int head, int chunk) { return gates + (head * 4 + chunk) * (LOCAL ? kLocalRecord : kRecord); };
-  float Dh[HEADS], A2[HEADS], bias[HEADS];
+  const float D = !LOCAL && a.D ? a.D[h] : 0.f;
+  float A2[HEADS], bias[HEADS];
 #pragma unroll
   for (int q = 0; q < HEADS; ++q) {
     const int hh = h0 + min(q, heads - 1);
-    Dh[q] = !LOCAL && a.D ? a.D[hh] : 0.f;
     A2[q] = a.A[hh] * 1.44269504f;
     bias[q] = a.dt_bias ? a.dt_bias[hh] : 0.f;
   }
@@ -436,8 +436,8 @@ __global__ __launch_bounds__(256, sizeof(IO) == 2 ? 2 : 1) void scan_kernel(Scan
   };
 
   // the lane's places in the tiles: rows i of B and C by 32 channels (scores), rows c32 of C by 16
-  // channels and of M, columns of B and x
-  uint32_t row16[KT][FR::kRow], row32[2 * KT][FR::kRow], mrow[4][FR::kRow], bcol[KT][FR::kCols], xcol[FR::kCols];
+  // channels, of M and of x, columns of B and x
+  uint32_t row16[KT][FR::kRow], row32[2 * KT][FR::kRow], mrow[4][FR::kRow], xrow[2][FR::kRow], bcol[KT][FR::kCols], xcol[FR::kCols];
 #pragma unroll
   for (int kt = 0; kt < KT; ++kt) {
     FR::template row_at<K>(row16[kt], i, 32 * kt + 8 * g);
@@ -447,6 +447,8 @@ __global__ __launch_bounds__(256, sizeof(IO) == 2 ? 2 : 1) void scan_kernel(Scan
   }
 #pragma unroll
   for (int st = 0; st < 4; ++st) FR::template row_at<kChunk>(mrow[st], c32, 16 * st + 8 * h32);
+#pragma unroll
+  for (int j = 0; j < 2; ++j) FR::template row_at<kValues>(xrow[j], c32, 32 * wave + 16 * j + 8 * h32);
   FR::template cols_at<kValues>(xcol, lane, 32 * wave);
   char* const lmh = lm + hl * TM::kBytes;
   const uint32_t oy = (uint32_t)((c32 * a.ldy + vbase + 8 * h32) * sizeof(IO));
@@ -480,7 +482,7 @@ __global__ __launch_bounds__(256, sizeof(IO) == 2 ? 2 : 1) void scan_kernel(Scan
 
     if constexpr (!LOCAL) {
       // scores of tiles (w, st): tokens t (place i) of tile w against s of tile st <= w, with
-      // decay and step, as rows of M; D on the diagonal.  The ten tiles by wave:
+      // decay and step, as rows of M.  The ten tiles by wave:
       // its diagonal one, then 0: (1,0), 1: (2,1), 2: (3,1), 3: (3,2), then (2,0) and (3,0), each
       // head by a wave of its own where there are two.  (What a missing second head finds in
       // its record is never stored.)
@@ -505,7 +507,7 @@ __global__ __launch_bounds__(256, sizeof(IO) == 2 ? 2 : 1) void scan_kernel(Scan
             for (int e = 0; e < 4; ++e) {
               const int o = 4 * g + e - i;  // s - t
               f[e] = m[e] * __builtin_amdgcn_exp2f((th - h4[e]) + (tl - l4[e]));
-              f[e] = (o > 0 ? 0.f : f[e]) + (o == 0 ? Dh[q] : 0.f);
+              if (o > 0) f[e] = 0.f;
             }
           } else {
             const float et = __builtin_amdgcn_exp2f(r[kLocal + 16 * tw + i]) * r[kSkip + (tw - ts == 1 ? 0 : tw - ts == 3 ? 3 : ts + 1)];
@@ -552,6 +554,16 @@ __global__ __launch_bounds__(256, sizeof(IO) == 2 ? 2 : 1) void scan_kernel(Scan
         const float et = rec[kGate + 32 * tt + c32];
 #pragma unroll
         for (int r = 0; r < 16; ++r) y[tt][r] *= et;
+      }
+      if (a.D) {  // in fp32: on the scores' diagonal it would be rounded with them
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const auto x = __builtin_bit_cast(Raw<IO, 8>, FR::row(lx, xrow[j], 2 * tt * ROW * kValues));
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[tt][8 * j + e] = fmaf(D, x.get(e), y[tt][8 * j + e]);
+          }
       }
       lds_barrier();
       const int n = mine ? s.p1 - p : 0;

@@ -1,0 +1,92 @@
+"""What the mixer layer's operators keep in 32 bits, held to it.
+
+Bounds are derived from counts of operations and unit roundoffs (2^-24, and 2^-8
+for a value stored in bf16).  A scan's decays are products of softplus, step and
+exponent, each a few units off, over the tokens a term survives."""
+import pytest
+import torch
+
+import mixer_reference as R
+from paper_2609_33051_amd import binding as B
+from paper_2609_33051_amd import ops
+
+pytestmark = pytest.mark.gpu
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+def case(*a):
+    print("[case]", *a, flush=True)
+
+
+def rnd(seed):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return lambda shape, dtype=torch.float32, scale=1.0: (torch.randn(shape, device="cuda", generator=g) * scale).to(dtype)
+
+
+def scan_inputs(seed, lengths, H, G, K, V, io, dt_shift=-4.0, initial=True):
+    dt, r, T = DT[io], rnd(seed), sum(lengths)
+    a = dict(x=r((T, H * V), dt), b=r((T, G * K), dt), c=r((T, G * K), dt), dt=r((T, -(-H // 8) * 8), dt)[:, :H], dt_bias=r((H,)) + dt_shift,
+             A=-torch.exp(r((H,))), D=r((H,)))
+    return a, r((len(lengths), H, V, K)) if initial else None
+
+
+def run_scan(a, S, lengths, H, G, K, V, io):
+    cfg = B.make_config("mamba2", len(lengths), H, K, V, 16, 16, io)
+    return ops.scan(cfg, G, a["x"], a["b"], a["c"], a["dt"], a["dt_bias"], a["A"], D=a["D"], offsets=R.offsets(lengths),
+                    S=None if S is None else R.tiles(S).contiguous())
+
+
+def definition(a, S, lengths, H, G):
+    c = {k: v.cpu() for k, v in a.items()}
+    return R.scan(c["x"], c["b"], c["c"], c["dt"], c["dt_bias"], c["A"], c["D"], lengths, None if S is None else S.cpu(), H, G)
+
+
+def skip_terms(a, H):
+    """|D x| of every output"""
+    x = a["x"].cpu().double()
+    return (x.reshape(x.shape[0], H, -1) * a["D"].cpu().double()[:, None]).abs().reshape(x.shape)
+
+
+# ---- scan: the skip term
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+@pytest.mark.parametrize("H,G,K,V", [(2, 1, 64, 64), (6, 2, 128, 64), (3, 3, 128, 128)])
+def test_scan_skip_is_not_rounded(io, H, G, K, V):
+    """D between two bf16 values and steps of nothing: y is D x rounded once, by its own type.
+    The operands that are rounded to bf16 belong to the other terms alone."""
+    case("scan skip", io, H, G, K, V)
+    lengths = [70, 1, 130]
+    a, S = scan_inputs(H + K, lengths, H, G, K, V, io, dt_shift=-40.0, initial=False)
+    a["D"] = torch.linspace(1.5039, 1.9961, H, device="cuda")  # a bf16's neighbours here lie 2^-7 apart
+    y, _ = run_scan(a, S, lengths, H, G, K, V, io)
+    want, mag, _, _ = definition(a, S, lengths, H, G)
+    skip = skip_terms(a, H)
+    R.close(y.cpu(), want, (mag - skip) * 0.01 + skip * 4 * R.U32 + want.abs() * R.unit(DT[io]), "y")
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+@pytest.mark.parametrize("lengths", [[700], [1, 90, 0, 255]])
+def test_scan_rounds_only_what_the_state_and_scores_take(io, lengths):
+    """Ordinary steps and a large D: the operands' 2^-8 is of the recurrence's terms, not of D x."""
+    case("scan terms", io, lengths)
+    H, G, K, V = 4, 2, 128, 64
+    a, S = scan_inputs(sum(lengths), lengths, H, G, K, V, io)
+    a["D"] = a["D"] * 40.0
+    y, _ = run_scan(a, S, lengths, H, G, K, V, io)
+    want, mag, _, _ = definition(a, S, lengths, H, G)
+    skip = skip_terms(a, H)
+    acc = (sum(lengths) + 64) * R.U32 + 100 * 2.0 ** -22
+    op = 1.02 * R.U16 if io == "bf16" else 0.0
+    R.close(y.cpu(), want, (mag - skip) * (op + acc) + skip * (4 * R.U32 + acc) + want.abs() * R.unit(DT[io]) + 1e-30, "y")
+
+
+def test_prompt_and_token_apply_the_same_skip():
+    """The decode path adds D x in fp32 in front of the gated norm; the scan's own D does the same."""
+    case("scan skip and norm skip")
+    lengths, H, G, K, V = [50], 4, 1, 64, 64
+    a, S = scan_inputs(3, lengths, H, G, K, V, "bf16", dt_shift=-40.0, initial=False)
+    a["D"] = torch.tensor([1.5039, 0.7519, 1.9961, 3.0078], device="cuda")
+    y, _ = run_scan(a, S, lengths, H, G, K, V, "bf16")
+    want = (a["x"].float().reshape(50, H, V) * a["D"][:, None]).reshape(50, H * V)
+    assert float((y.float() - want).norm() / want.norm()) < 2.0 ** -9  # rms of one rounding: 2^-8 / sqrt(3) at the most, less over a binade
