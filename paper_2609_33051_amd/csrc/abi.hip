@@ -79,6 +79,7 @@ int check_ring(const skssm_config* c, const skssm_ring* r, bool derived_f, bool 
 
 int launched(int rc, const char* what) {
   if (rc == -2) return fail(SKSSM_EUNSUPPORTED, "%s: no kernel compiled for this shape", what);
+  if (rc == -3) return fail(SKSSM_EUNSUPPORTED, "%s: too large for one launch (2^32 threads)", what);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return fail(SKSSM_EHIP, "%s: %s", what, hipGetErrorString(e));
   g_err[0] = '\0';

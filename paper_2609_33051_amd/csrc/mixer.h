@@ -45,6 +45,11 @@ __device__ __forceinline__ float softplus(float r) {
   return fmaf(2.f * z, t, fmaxf(r, 0.f));
 }
 
+// What a launch can hold: fewer than 2^32 threads.  A call whose launches do not all fit makes none and returns -3.
+inline bool fits(int64_t workgroups, int threads) { return workgroups * threads < (int64_t)1 << 32; }
+// Whether the launches so far were taken: one that follows from them is not made where they were not.
+inline bool taken() { return hipPeekAtLastError() == hipSuccess; }
+
 struct ConvArgs {
   Sequences seq;
   int C;                  // channels

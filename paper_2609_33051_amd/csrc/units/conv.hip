@@ -184,12 +184,12 @@ int launch_conv_rows(const ConvArgs& a, bool apart, hipStream_t s) {
   constexpr int CH = 16 / sizeof(IO);
   const int cols = (a.C / CH + 63) / 64, tiles = (a.seq.tokens + ROWS - 1) / ROWS;
   const int states = a.state_out ? a.seq.batch : 0, with = apart ? 0 : states;
-  const unsigned first = (unsigned)cols * (unsigned)((tiles + with + kDown - 1) / kDown);
-  if (first) hipLaunchKernelGGL((conv_kernel<IO, W, SILU, ROWS>), dim3(first), dim3(64 * kDown), 0, s, a, cols, tiles, with);
+  const int64_t first = cols * (((int64_t)tiles + with + kDown - 1) / kDown), then = apart ? cols * (((int64_t)states + kDown - 1) / kDown) : 0;
+  if (!fits(first, 64 * kDown) || !fits(then, 64 * kDown)) return -3;
+  if (first) hipLaunchKernelGGL((conv_kernel<IO, W, SILU, ROWS>), dim3((unsigned)first), dim3(64 * kDown), 0, s, a, cols, tiles, with);
   // the new states in place of the old ones: after the outputs, which read those
-  if (apart && states)
-    hipLaunchKernelGGL((conv_kernel<IO, W, SILU, ROWS>), dim3((unsigned)cols * (unsigned)((states + kDown - 1) / kDown)), dim3(64 * kDown), 0, s,
-                       a, cols, 0, states);
+  if (then && taken())
+    hipLaunchKernelGGL((conv_kernel<IO, W, SILU, ROWS>), dim3((unsigned)then), dim3(64 * kDown), 0, s, a, cols, 0, states);
   return 0;
 }
 

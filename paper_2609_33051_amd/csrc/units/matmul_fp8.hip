@@ -298,14 +298,16 @@ __global__ __launch_bounds__(256) void matmul_join_kernel(MatmulArgs p, int spli
 }
 
 template <typename OUT, int BM, int BN, int WM, int WN, int STAGES>
-void launch_tiles(const MatmulArgs& p, int splits, hipStream_t s) {
+int launch_tiles(const MatmulArgs& p, int splits, hipStream_t s) {
   const int mt = (p.M + BM - 1) / BM, nt = (p.N + BN - 1) / BN;
+  if (!fits((int64_t)mt * nt, 64 * WM * WN)) return -3;
   hipLaunchKernelGGL((matmul_tile_kernel<OUT, BM, BN, WM, WN, STAGES>), dim3((unsigned)mt * (unsigned)nt, (unsigned)splits), dim3(64 * WM * WN), 0,
                      s, p, mt, nt);
-  if (splits > 1) {
+  if (splits > 1 && taken()) {  // (of fewer tiles than the card runs at once)
     const size_t quads = (size_t)p.M * ((p.N + 3) / 4);
     hipLaunchKernelGGL((matmul_join_kernel<OUT>), dim3((unsigned)((quads + 255) / 256)), dim3(256), 0, s, p, splits);
   }
+  return 0;
 }
 
 // Which tiles, and over how many workgroups the K axis is split.
@@ -355,9 +357,10 @@ int launch_matmul(const MatmulArgs& p, hipStream_t s) {
   MatmulArgs q = p;
   if constexpr (sizeof(OUT) == 2) {
     if (plan.wide) {
+      if (plan.rest && !fits((int64_t)((p.M + 127) / 128) * ((p.N - plan.wide + 63) / 64), 256)) return -3;  // (128 x 64, the most tiles)
       q.N = std::min(p.N, plan.wide);
-      launch_tiles<OUT, 256, 256, 4, 2, 2>(q, 1, s);
-      if (!plan.rest) return 0;
+      const int rc = launch_tiles<OUT, 256, 256, 4, 2, 2>(q, 1, s);
+      if (rc || !plan.rest || !taken()) return rc;
       q.N = p.N - plan.wide;
       q.w = p.w + (size_t)plan.wide * p.ldw;
       q.sw = p.sw + (size_t)(plan.wide / 128) * ((p.K + 127) / 128);
@@ -365,10 +368,10 @@ int launch_matmul(const MatmulArgs& p, hipStream_t s) {
     }
   }
   switch (plan.rest) {
-    case 1: launch_tiles<OUT, 128, 128, 2, 2, 2>(q, plan.splits, s); return 0;
-    case 2: launch_tiles<OUT, 128, 64, 2, 2, 3>(q, plan.splits, s); return 0;
-    case 3: launch_tiles<OUT, 64, 64, 2, 2, 3>(q, plan.splits, s); return 0;
-    case 4: launch_tiles<OUT, 32, 64, 2, 2, 4>(q, plan.splits, s); return 0;
+    case 1: return launch_tiles<OUT, 128, 128, 2, 2, 2>(q, plan.splits, s);
+    case 2: return launch_tiles<OUT, 128, 64, 2, 2, 3>(q, plan.splits, s);
+    case 3: return launch_tiles<OUT, 64, 64, 2, 2, 3>(q, plan.splits, s);
+    case 4: return launch_tiles<OUT, 32, 64, 2, 2, 4>(q, plan.splits, s);
     default: return -2;
   }
 }

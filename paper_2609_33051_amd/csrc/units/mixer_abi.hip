@@ -13,7 +13,6 @@ using skssm::overlap;
 namespace {
 
 constexpr int64_t kMaxTokens = (int64_t)1 << 30;
-constexpr int64_t kMaxGrid = (int64_t)1 << 30;  // workgroups of a launch
 
 int elem(int dtype) { return dtype == SKSSM_F32 ? 4 : dtype == SKSSM_BF16 ? 2 : 1; }
 
@@ -80,8 +79,6 @@ int sketchssm_conv(const skssm_conv_config* cfg, int32_t batch, int64_t tokens, 
     return fail(SKSSM_EINVAL, "%s: an output overlaps x or a state", what);
   if (state_in != state_out && overlap(state_in, ns, state_out, ns))
     return fail(SKSSM_EINVAL, "%s: the states overlap without being the same", what);
-  const int64_t cols = ((int64_t)C * e / 16 + 255) / 256;
-  if (cols * (tokens / 8 + batch + 1) > kMaxGrid) return fail(SKSSM_EUNSUPPORTED, "%s: too many channels times tokens for one launch", what);
   skssm::ConvArgs a{};
   a.seq = sequences(batch, tokens, offsets);
   a.C = C;
@@ -233,7 +230,7 @@ int sketchssm_norm(const skssm_norm_args* args, void* stream) {
   if (p.group > 32768) return fail(SKSSM_EUNSUPPORTED, "%s: group of %d columns: at most 32768", what, p.group);
   if (fp8 && p.group != p.columns && p.group % 128)
     return fail(SKSSM_EUNSUPPORTED, "%s: a group of %d columns cuts blocks of 128", what, p.group);
-  if (p.rows > kMaxTokens || p.rows * (p.columns / p.group) > kMaxGrid) return fail(SKSSM_EUNSUPPORTED, "%s: too many rows for one launch", what);
+  if (p.rows > kMaxTokens) return fail(SKSSM_EUNSUPPORTED, "%s: %lld rows: at most 2^30", what, (long long)p.rows);
   if (!(p.eps >= 0.f)) return fail(SKSSM_EINVAL, "%s: eps must be >= 0", what);
   if (p.residual && p.gate) return fail(SKSSM_EINVAL, "%s: residual and gate exclude each other", what);
   if (p.residual_out && !p.residual) return fail(SKSSM_EINVAL, "%s: residual_out without residual", what);
@@ -313,7 +310,7 @@ int sketchssm_matmul_fp8(int64_t M, int32_t N, int32_t K, const void* a, int64_t
   const char* what = "sketchssm_matmul_fp8";
   if (M < 0 || N < 1 || K < 1) return fail(SKSSM_EINVAL, "%s: sizes %lld x %d x %d", what, (long long)M, N, K);
   if (K % 16) return fail(SKSSM_EUNSUPPORTED, "%s: K = %d is not a multiple of 16", what, K);
-  if (M > kMaxTokens || N > kMaxTokens || ((M + 127) / 128) * ((N + 127) / 128) > kMaxGrid) return fail(SKSSM_EUNSUPPORTED, "%s: M x N too large for one launch", what);
+  if (M > kMaxTokens || N > kMaxTokens) return fail(SKSSM_EUNSUPPORTED, "%s: M = %lld, N = %d: at most 2^30", what, (long long)M, N);
   if (out_dtype != SKSSM_F32 && out_dtype != SKSSM_BF16) return fail(SKSSM_EINVAL, "%s: unknown out_dtype %d", what, out_dtype);
   int rc;
   if ((rc = check_stride(what, "a", lda, K, 1)) || (rc = check_stride(what, "w", ldw, K, 1))) return rc;

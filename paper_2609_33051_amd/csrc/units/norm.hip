@@ -111,6 +111,14 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(NormArgs a) {
   }
 }
 
+template <typename TX, typename IO, bool FP8, int FORM, int THREADS, int NV>
+int launch_norm(const NormArgs& a, hipStream_t s) {
+  const int64_t workgroups = (int64_t)a.rows * (a.columns / a.group);
+  if (!fits(workgroups, THREADS)) return -3;
+  hipLaunchKernelGGL((norm_kernel<TX, IO, FP8, FORM, THREADS, NV>), dim3((unsigned)workgroups), dim3(THREADS), 0, s, a);
+  return 0;
+}
+
 // Threads and 8-column pieces a thread, by the group's width.  8192 rows with the residual into
 // 8 bits, bf16 (us; the best copy moves 6.4 TB/s): 1024 columns 11.7, 2048 23.2 to 25 (5.0 TB/s; 256
 // threads 26.4), 4096 46.6 (5.0), 8192 90 (5.2; 1024 threads 92.8); 16384 columns of
@@ -119,17 +127,15 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(NormArgs a) {
 // they gain where nothing is used again soon and lose where it is, and a norm's output is.
 template <typename TX, typename IO, bool FP8, int FORM>
 int launch_norm(const NormArgs& a, hipStream_t s) {
-  const dim3 grid((unsigned)a.rows * (unsigned)(a.columns / a.group));
   const int n = a.group;
-  if (n <= 512) hipLaunchKernelGGL((norm_kernel<TX, IO, FP8, FORM, 64, 1>), grid, dim3(64), 0, s, a);
-  else if (n <= 1024) hipLaunchKernelGGL((norm_kernel<TX, IO, FP8, FORM, 64, 2>), grid, dim3(64), 0, s, a);
-  else if (n <= 2048) hipLaunchKernelGGL((norm_kernel<TX, IO, FP8, FORM, 128, 2>), grid, dim3(128), 0, s, a);
-  else if (n <= 4096) hipLaunchKernelGGL((norm_kernel<TX, IO, FP8, FORM, 256, 2>), grid, dim3(256), 0, s, a);
-  else if (n <= 8192) hipLaunchKernelGGL((norm_kernel<TX, IO, FP8, FORM, 256, 4>), grid, dim3(256), 0, s, a);
-  else if (n <= 16384) hipLaunchKernelGGL((norm_kernel<TX, IO, FP8, FORM, 512, 4>), grid, dim3(512), 0, s, a);
-  else if (n <= 32768) hipLaunchKernelGGL((norm_kernel<TX, IO, FP8, FORM, 1024, 4>), grid, dim3(1024), 0, s, a);
-  else return -2;
-  return 0;
+  if (n <= 512) return launch_norm<TX, IO, FP8, FORM, 64, 1>(a, s);
+  if (n <= 1024) return launch_norm<TX, IO, FP8, FORM, 64, 2>(a, s);
+  if (n <= 2048) return launch_norm<TX, IO, FP8, FORM, 128, 2>(a, s);
+  if (n <= 4096) return launch_norm<TX, IO, FP8, FORM, 256, 2>(a, s);
+  if (n <= 8192) return launch_norm<TX, IO, FP8, FORM, 256, 4>(a, s);
+  if (n <= 16384) return launch_norm<TX, IO, FP8, FORM, 512, 4>(a, s);
+  if (n <= 32768) return launch_norm<TX, IO, FP8, FORM, 1024, 4>(a, s);
+  return -2;
 }
 
 template <typename TX, typename IO, bool FP8>

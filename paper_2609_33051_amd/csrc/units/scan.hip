@@ -669,9 +669,11 @@ int launch_scan(const ScanArgs& a, hipStream_t s) {
   if (windows)
     hipLaunchKernelGGL((scan_kernel<IO, K, V, true>), dim3((unsigned)windows * (unsigned)parts), dim3(256),
                        2 * (local + heads * 4 * kLocalRecord * sizeof(float)), s, a, seg, false);
+  // (batch times heads is less than 2^23, windows times parts at most 512: every launch fits)
+  if (windows && !taken()) return 0;
   hipLaunchKernelGGL((scan_kernel<IO, K, V, false>), dim3((unsigned)(a.seq.batch + windows) * (unsigned)parts), dim3(256),
                      full + heads * 4 * kRecord * sizeof(float), s, a, seg, apart);
-  if (apart) hipLaunchKernelGGL(scan_states_kernel, dim3((unsigned)windows * (unsigned)a.H), dim3(256), 0, s, a, seg, V * K);
+  if (apart && taken()) hipLaunchKernelGGL(scan_states_kernel, dim3((unsigned)windows * (unsigned)a.H), dim3(256), 0, s, a, seg, V * K);
   return 0;
 }
 

@@ -230,3 +230,27 @@ def test_scale_rows_that_overlap_are_refused(rows, columns):
     assert ops._rows("scales", torch.ones((rows, columns + 3))[:, :columns], rows, columns, -1) == columns + 3
     assert ops._rows("scales", one, 1, columns, -1) >= columns
     assert ops._rows("scales", torch.ones((rows, 0)), rows, 0, -1) >= 0
+
+
+@cpu_only
+def test_launches_of_too_many_threads_are_refused(lib):
+    """A launch holds fewer than 2^32 threads: sizes past that are refused before any launch, by the
+    kernel's own workgroups (64 threads of a norm's narrow group, 256 of a convolution's or a product's tiles)."""
+    def refused(rc):
+        return rc == -2 and "one launch" in B.sketchssm_last_error()
+    far = lambda k: (k + 1) << 44  # noqa: E731
+    # a norm by groups of 64 columns, 8192 columns: a workgroup of 64 threads a group
+    for kw in (dict(rows=1 << 19, columns=8192, group=64), dict(rows=1 << 23, columns=8192, group=64), dict(rows=1 << 26, columns=64, group=64),
+               dict(rows=1 << 22, columns=32768, group=32768)):
+        n = kw["columns"]
+        for out in (dict(out_dtype=1, scales=None), dict(scales=far(4), ld_scales=kw["rows"])) if n == kw["group"] else (dict(out_dtype=1, scales=None),):
+            assert refused(lib.sketchssm_norm(norm_args(**kw, **out, ldx=n, ld_out=n, x=far(1), weight=far(2), out=far(3)), None)), (kw, out)
+    # a convolution: 64 lanes of 16 bytes a column of workgroups, 48 tokens a workgroup, and its states
+    arrays = dict(x=far(1), taps=far(2), bias=far(3), s_in=far(4), s_out=far(5), y=far(6))
+    assert refused(conv(lib, C=8, T=1 << 30, ldx=8, ldy=8, off=None, batch=1, **arrays))
+    assert refused(conv(lib, C=8, T=0, ldx=8, ldy=8, batch=1 << 26, **arrays))
+    assert refused(conv(lib, C=8, T=0, ldx=8, ldy=8, batch=1 << 26, **{**arrays, "s_in": far(5)}))
+    assert refused(conv(lib, C=1 << 23, T=1 << 16, ldx=1 << 23, ldy=1 << 23, batch=1, **arrays))
+    # a product of one row and 2^30 columns: 2^24 tiles of 64 columns
+    assert refused(matmul(lib, M=1, N=1 << 30, K=16, lda=16, ldw=16, ldsa=1, out=0, ldy=1 << 30, a=far(1), sa=far(2), w=far(3), sw=far(4), y=far(5),
+                          ws=far(6)))
