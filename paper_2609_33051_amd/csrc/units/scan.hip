@@ -645,6 +645,7 @@ int scan_segment(const Sequences& q, int parts) {
   int64_t seg = ((int64_t)q.tokens * parts + want - 1) / want;
   const int64_t joined = (int64_t)sqrt(8.0 * q.tokens);
   if (seg < joined) seg = joined;
+  if (seg > q.tokens) seg = q.tokens;  // (as much: none is split)
   return (int)(seg <= kGates / 2 ? (seg + kChunk - 1) / kChunk * kChunk : (seg + kGates - 1) / kGates * kGates);
 }
 // Windows that may hold a later segment's start; none where no sequence is split.

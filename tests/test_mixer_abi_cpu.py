@@ -254,3 +254,12 @@ def test_launches_of_too_many_threads_are_refused(lib):
     # a product of one row and 2^30 columns: 2^24 tiles of 64 columns
     assert refused(matmul(lib, M=1, N=1 << 30, K=16, lda=16, ldw=16, ldsa=1, out=0, ldy=1 << 30, a=far(1), sa=far(2), w=far(3), sw=far(4), y=far(5),
                           ws=far(6)))
+
+
+def test_scan_workspace_of_many_heads_and_tokens(lib):
+    """The shares of 2^30 tokens and 2^22 heads pass 32 bits: no sequence is split, and nothing is divided by their remainder."""
+    for heads, T in ((1 << 22, 1 << 30), (1 << 13, 1 << 30), ((1 << 22) - 1, (1 << 30) - 1), (1 << 10, 1 << 30), (513, 1 << 20)):
+        c = B.make_config("mamba2", 1, heads, 128, 64, 16, 16, "bf16")
+        assert lib.sketchssm_scan_workspace(c, heads, T) == 0, (heads, T)
+    c = B.make_config("mamba2", 1, 2, 128, 64, 16, 16, "bf16")
+    assert lib.sketchssm_scan_workspace(c, 1, 1 << 30) > 0
