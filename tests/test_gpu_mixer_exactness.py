@@ -90,3 +90,36 @@ def test_prompt_and_token_apply_the_same_skip():
     y, _ = run_scan(a, S, lengths, H, G, K, V, "bf16")
     want = (a["x"].float().reshape(50, H, V) * a["D"][:, None]).reshape(50, H * V)
     assert float((y.float() - want).norm() / want.norm()) < 2.0 ** -9  # rms of one rounding: 2^-8 / sqrt(3) at the most, less over a binade
+
+
+# ---- 8-bit products whose K axis is split
+
+
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+@pytest.mark.parametrize("M,N,K", [(5, 130, 8208), (77, 513, 4112), (40, 17, 6160), (77, 4096, 8192), (1, 256, 16400), (16, 1028, 2064),
+                                   (64, 66, 4096), (200, 384, 8080), (33, 1, 12304)])
+def test_matmul_split(M, N, K, out):
+    """Parts of unequal length, a short last block, N that is no multiple of four, more than two parts; an output
+    between guard columns, a workspace of the size asked for, NaN before the call, with a guard behind it."""
+    case("matmul split", M, N, K, out)
+    r = rnd(M + N + K)
+    kb, nb = -(-K // 128), -(-N // 128)
+    f8 = lambda shape: r(shape, scale=130.0).clamp(-448, 448).to(ops.F8)  # noqa: E731
+    a, w = f8((M, K)), f8((N, K))
+    sa, sw = torch.exp(r((kb, M))), torch.exp(r((nb, kb)))
+    need = B.load().sketchssm_matmul_fp8_workspace(M, N, K)
+    assert need >= 2 * M * N * 4  # the split is taken
+    space = torch.full((need // 4 + 64,), float("nan"), device="cuda")
+    space[need // 4:] = 3.0
+    y, mag, top = R.matmul(a, sa, w, sw)
+    bound = (128 + K / 128 + 8) * R.U32 * mag
+    if out == "bf16":
+        bound = bound + top * 2.0 ** -11 + y.abs() * R.U16
+    for ld in (N, N + 3, -(-N // 16) * 16 + 16):
+        wide = torch.full((M, ld), 5.0, dtype=DT[out], device="cuda")
+        ops.matmul_fp8(a, sa, w, sw, out=wide[:, :N], workspace=space[:need // 4])
+        R.close(wide[:, :N], y, bound, f"y, rows of {ld}")
+        assert bool((wide[:, N:] == 5.0).all()) and bool((space[need // 4:] == 3.0).all())
+    again = torch.empty((M, N), dtype=DT[out], device="cuda")
+    ops.matmul_fp8(a, sa, w, sw, out=again)
+    assert torch.equal(again, wide[:, :N])  # parts are joined in order
