@@ -123,3 +123,41 @@ def test_matmul_split(M, N, K, out):
     again = torch.empty((M, N), dtype=DT[out], device="cuda")
     ops.matmul_fp8(a, sa, w, sw, out=again)
     assert torch.equal(again, wide[:, :N])  # parts are joined in order
+
+
+# ---- the state's 24 bits, and heads shared out over the XCDs
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+@pytest.mark.parametrize("H,G,K,V", [(2, 1, 64, 64), (4, 2, 128, 64), (3, 3, 128, 128)])
+@pytest.mark.parametrize("lengths", [[64], [37, 0, 20], [130, 5]])
+def test_scan_state_keeps_24_bits(io, H, G, K, V, lengths):
+    """Slow decays, so that every token's share of the state lasts: the state is as close as fp32 sums are, value by
+    value and in the norm (two bf16 parts of x dt 2^{..} are 2e-6 off in the norm)."""
+    case("scan state", io, H, G, K, V, lengths)
+    a, S = scan_inputs(H + K + sum(lengths), lengths, H, G, K, V, io, initial=False)
+    a["A"] = a["A"] * 0.1
+    _, St = run_scan(a, S, lengths, H, G, K, V, io)
+    _, _, want, mag = definition(a, S, lengths, H, G)
+    acc = (sum(lengths) + 64) * R.U32 + 100 * 2.0 ** -22
+    R.close(St.cpu(), R.tiles(want), R.tiles(mag) * acc + 1e-30, "S")
+    n = [i for i, k in enumerate(lengths) if k]
+    got, ref = St.cpu().double()[n], R.tiles(want)[n]
+    assert float((got - ref).norm() / ref.norm()) < 1e-6
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+@pytest.mark.parametrize("H,G,K,V", [(16, 8, 128, 64), (32, 2, 128, 64), (16, 8, 64, 64), (8, 8, 128, 128), (24, 8, 64, 64)])
+def test_scan_heads_over_the_dies(io, H, G, K, V):
+    """Parts of heads in multiples of eight, which are dealt out in runs; with later segments."""
+    case("scan heads", io, H, G, K, V)
+    lengths = [260, 3, 0, 150]
+    assert B.load().sketchssm_scan_workspace(B.make_config("mamba2", 4, H, K, V, 16, 16, io), G, sum(lengths)) > 0
+    a, S = scan_inputs(H + G + K, lengths, H, G, K, V, io)
+    y, St = run_scan(a, S, lengths, H, G, K, V, io)
+    wy, my, wS, mS = definition(a, S, lengths, H, G)
+    skip = skip_terms(a, H)
+    acc = (sum(lengths) + 64) * R.U32 + 100 * 2.0 ** -22
+    op = 1.02 * R.U16 if io == "bf16" else 0.0
+    R.close(y.cpu(), wy, (my - skip) * (op + acc) + skip * (4 * R.U32 + acc) + wy.abs() * R.unit(DT[io]) + 1e-30, "y")
+    R.close(St.cpu(), R.tiles(wS), R.tiles(mS) * acc + 1e-30, "S")
