@@ -68,7 +68,7 @@ __device__ __forceinline__ Raw<IO, 16 / sizeof(IO)> conv_row(const Taps<IO, W>& 
 #pragma unroll
   for (int i = 0; i < CH; i += 2) {
     float a = k.sum(win, i), b = k.sum(win, i + 1);
-    if constexpr (SILU) { a *= sigmoid(a); b *= sigmoid(b); }
+    if constexpr (SILU) { a *= sigmoid<IO>(a); b *= sigmoid<IO>(b); }
     set_pair<IO, CH>(y, i, a, b);
   }
   return y;

@@ -55,7 +55,7 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(NormArgs a) {
       float t = rx[v].get(i);
       if constexpr (FORM == RESIDUAL) t += r1[v].get(i);
       if constexpr (FORM == GATED_SKIP) t = fmaf(d, r2[v].get(i), t);
-      if constexpr (FORM >= GATED) { const float z = r1[v].get(i); t *= z * sigmoid(z); }
+      if constexpr (FORM >= GATED) { const float z = r1[v].get(i); t *= z * sigmoid<IO>(z); }
       u[v][i] = in ? t : 0.f;
       ss = fmaf(u[v][i], u[v][i], ss);
     }

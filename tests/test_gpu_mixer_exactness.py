@@ -161,3 +161,43 @@ def test_scan_heads_over_the_dies(io, H, G, K, V):
     op = 1.02 * R.U16 if io == "bf16" else 0.0
     R.close(y.cpu(), wy, (my - skip) * (op + acc) + skip * (4 * R.U32 + acc) + wy.abs() * R.unit(DT[io]) + 1e-30, "y")
     R.close(St.cpu(), R.tiles(wS), R.tiles(mS) * acc + 1e-30, "S")
+
+
+# ---- exponentials of the gates
+
+
+def test_step_sizes_are_fp32():
+    """softplus of a step down to 2^-100 and less, without a bias (whose sum would be rounded first): its exponential is
+    within 2 units (1 ulp) of the instruction and 2 of its argument's low part, the reciprocal within 2, the series, its
+    factors and the last sum within 6; log decay adds a product."""
+    case("softplus")
+    Bt, H, K, V, W = 512, 8, 64, 64, 4
+    r = torch.linspace(-84.0, 84.0, Bt * H, device="cuda").reshape(Bt, H)
+    C = H * V + 2 * K
+    z = lambda *s: torch.zeros(s, device="cuda")  # noqa: E731
+    cfg = B.make_config("mamba2", Bt, H, K, V, 16, W, "f32")
+    rk, rv, rb, rl, q, A = z(Bt, H, W, K), z(Bt, H, W, V), z(Bt, H, W), z(Bt, H, W), z(Bt, H, K), -torch.linspace(0.5, 8.0, H, device="cuda")
+    ops.conv_token(cfg, 1, z(Bt, C), z(C, 4), None, z(Bt, 3, C), r, None, A, B.make_ring(k=rk, v=rv, beta=rb, log_decay=rl), 1, q)
+    want = torch.log1p(torch.exp(r.double())).where(r < 0, r.double() + torch.log1p(torch.exp(-r.double())))
+    R.close(rb[:, :, 1], want, want * 12 * R.U32, "beta")
+    R.close(rl[:, :, 1], want * A.double(), (want * A.double()).abs() * 13 * R.U32, "log decay")
+    assert float(((rb[:, :, 1] - want) / want).square().mean().sqrt()) < 2 * R.U32
+
+
+def test_silu_is_fp32():
+    """The convolution's and the gate's silu in fp32, to |z| = 80: z sigma(z) of an exact z, its exponential within 4
+    units, the sum, the reciprocal and two products within 6; where sigma is less than 2^-126 nothing is asked."""
+    case("silu")
+    n = 1 << 14
+    x = torch.linspace(-80.0, 80.0, n, device="cuda").reshape(n // 64, 64)
+    taps = torch.zeros((64, 4), device="cuda")
+    taps[:, 3] = 1.0
+    y, _ = ops.conv(x, taps)
+    z = x.double()
+    want = z / (1 + torch.exp(-z))
+    R.close(y, want, want.abs() * 10 * R.U32, "conv")
+    one = torch.ones((n // 64, 64), device="cuda")
+    out, _, _ = ops.norm(one, torch.ones(64, device="cuda"), 1e-30, gate=x, group=8)
+    u = want.reshape(-1, 8, 8)
+    y = (u / (u.square().mean(-1, keepdim=True) + 1e-30).sqrt()).reshape(x.shape)
+    R.close(out, y, y.abs() * 32 * R.U32, "norm")
