@@ -47,7 +47,7 @@ typedef struct {
  * width-1 inputs of state and sequence together, so an empty sequence keeps
  * its state; it may be state_in itself.  taps [channels][width] and bias
  * [channels] (may be NULL) are fp32; sums are fp32.  y may not overlap x or
- * the states.
+ * the states, and neither y nor state_out taps, bias or offsets.
  */
 int sketchssm_conv(const skssm_conv_config* cfg, int32_t batch, int64_t tokens, const int32_t* offsets, const void* x,
                    int64_t ldx, const float* taps, const float* bias, const void* state_in, void* state_out, void* y,
@@ -65,7 +65,7 @@ int sketchssm_conv(const skssm_conv_config* cfg, int32_t batch, int64_t tokens, 
  *     (heads / groups consecutive heads each),
  *     ring.beta = softplus(dt + dt_bias), ring.log_decay = beta A
  * with dt [batch][heads] (io, row stride lddt, aligned to its element only) and
- * dt_bias, A [heads] fp32 (dt_bias may be NULL).  x and dt may not overlap what is written.
+ * dt_bias, A [heads] fp32 (dt_bias may be NULL).  No input but the state may overlap what is written.
  */
 int sketchssm_conv_token(const skssm_config* cfg, int32_t groups, int32_t width, const void* x, int64_t ldx,
                          const float* taps, const float* bias, void* state, const void* dt, int64_t lddt,
@@ -82,8 +82,8 @@ int sketchssm_conv_token(const skssm_config* cfg, int32_t groups, int32_t width,
  * batch, heads, dk, dv and io_dtype (kind SKSSM_MAMBA2; its rank is not used).
  * S_in (NULL: zero) and S_out are states in the tile-major layout of
  * sketchssm.h, S_out may be S_in; an empty sequence's state is passed on, so
- * sketchssm_update(q = NULL) can follow.  y [T][heads*dv] io may not overlap
- * the inputs.  The state and every sum are fp32; with bf16 io the products
+ * sketchssm_update(q = NULL) can follow.  y [T][heads*dv] io, S_out and the
+ * workspace may not overlap the inputs (but S_in).  The state and every sum are fp32; with bf16 io the products
  * inside a chunk of tokens take bf16 operands (the decayed scores and the state
  * as read by C_t are rounded to nearest), while what enters the state keeps 24 bits and D x_t
  * is fp32.

@@ -26,6 +26,15 @@ int check_stride(const char* what, const char* name, int64_t ld, int64_t row, in
 // Bytes from the first to past the last element of `rows` rows.
 size_t span(int64_t rows, int64_t ld, int64_t row, int e) { return rows > 0 ? (size_t)(((rows - 1) * ld + row) * e) : 0; }
 
+// Arrays by address and bytes (NULL or 0 bytes: none); whether one of the first overlaps one of the second.
+struct Range { const void* p; size_t n; };
+template <size_t N, size_t M> bool any_overlap(const Range (&a)[N], const Range (&b)[M]) {
+  for (const Range& x : a)
+    for (const Range& y : b)
+      if (x.n && y.n && overlap(x.p, x.n, y.p, y.n)) return true;
+  return false;
+}
+
 int check_packed(const char* what, int batch, int64_t tokens, const int32_t* offsets) {
   if (batch < 1) return fail(SKSSM_EINVAL, "%s: batch must be >= 1", what);
   if (tokens < 0 || tokens > kMaxTokens)
@@ -77,6 +86,9 @@ int sketchssm_conv(const skssm_conv_config* cfg, int32_t batch, int64_t tokens, 
   const size_t nx = span(tokens, ldx, C, e), ny = span(tokens, ldy, C, e), ns = (size_t)batch * (w - 1) * C * e;
   if (overlap(y, ny, x, nx) || overlap(y, ny, state_in, ns) || overlap(y, ny, state_out, ns) || overlap(state_out, ns, x, nx))
     return fail(SKSSM_EINVAL, "%s: an output overlaps x or a state", what);
+  const Range outs[] = {{y, ny}, {state_out, ns}};
+  const Range parameters[] = {{taps, (size_t)C * w * 4}, {bias, (size_t)C * 4}, {offsets, ((size_t)batch + 1) * 4}};
+  if (any_overlap(outs, parameters)) return fail(SKSSM_EINVAL, "%s: an output overlaps taps, bias or offsets", what);
   if (state_in != state_out && overlap(state_in, ns, state_out, ns))
     return fail(SKSSM_EINVAL, "%s: the states overlap without being the same", what);
   skssm::ConvArgs a{};
@@ -115,11 +127,13 @@ int sketchssm_conv_token(const skssm_config* cfg, int32_t groups, int32_t width,
   if ((rc = check_stride(what, "x", ldx, C, e))) return rc;
   if (lddt < H) return fail(SKSSM_EINVAL, "%s: dt stride %lld is less than %lld heads", what, (long long)lddt, (long long)H);
   const size_t items = (size_t)B * H, W = (size_t)cfg->window;
-  const struct { const void* p; size_t n; } out[6] = {{ring->k, items * W * cfg->dk * e}, {ring->v, items * W * cfg->dv * e},
+  const Range out[6] = {{ring->k, items * W * cfg->dk * e}, {ring->v, items * W * cfg->dv * e},
       {ring->beta, items * W * 4}, {ring->log_decay, items * W * 4}, {q, items * cfg->dk * e}, {state, (size_t)B * (width - 1) * C * e}};
   for (const auto& o : out)
     if (overlap(o.p, o.n, x, span(B, ldx, C, e)) || overlap(o.p, o.n, dt, span(B, lddt, H, e)))
       return fail(SKSSM_EINVAL, "%s: x or dt overlaps what is written", what);
+  const Range parameters[] = {{taps, (size_t)C * width * 4}, {bias, (size_t)C * 4}, {dt_bias, (size_t)H * 4}, {A, (size_t)H * 4}};
+  if (any_overlap(out, parameters)) return fail(SKSSM_EINVAL, "%s: taps, bias, dt_bias or A overlaps what is written", what);
   for (int i = 0; i < 6; ++i)
     for (int j = 0; j < i; ++j)
       if (overlap(out[i].p, out[i].n, out[j].p, out[j].n)) return fail(SKSSM_EINVAL, "%s: the arrays that are written overlap", what);
@@ -180,14 +194,12 @@ int sketchssm_scan(const skssm_config* cfg, int32_t groups, int64_t tokens, cons
   if (need && (!workspace || workspace_bytes < need))
     return fail(SKSSM_EINVAL, "%s: workspace of %zu bytes, %zu needed", what, workspace ? workspace_bytes : (size_t)0, need);
   const size_t states = (size_t)cfg->batch * HV * cfg->dk * 4;
-  const struct { const void* p; size_t n; } in[4] = {{x, span(tokens, ldx, HV, e)}, {b, span(tokens, ldb, GK, e)},
-      {c, span(tokens, ldc, GK, e)}, {dt, span(tokens, lddt, H, e)}};
-  const struct { const void* p; size_t n; } out[3] = {{y, span(tokens, ldy, HV, e)}, {S_out, states}, {workspace, need}};
-  for (const auto& o : out) {
-    for (const auto& p : in)
-      if (overlap(o.p, o.n, p.p, p.n)) return fail(SKSSM_EINVAL, "%s: an output overlaps an input", what);
+  const Range in[] = {{x, span(tokens, ldx, HV, e)}, {b, span(tokens, ldb, GK, e)}, {c, span(tokens, ldc, GK, e)}, {dt, span(tokens, lddt, H, e)},
+      {offsets, ((size_t)cfg->batch + 1) * 4}, {dt_bias, (size_t)H * 4}, {A, (size_t)H * 4}, {D, (size_t)H * 4}};
+  const Range out[] = {{y, span(tokens, ldy, HV, e)}, {S_out, states}, {workspace, need}};
+  if (any_overlap(out, in)) return fail(SKSSM_EINVAL, "%s: an output overlaps an input", what);
+  for (const Range& o : out)
     if (o.p != S_out && overlap(o.p, o.n, S_in, states)) return fail(SKSSM_EINVAL, "%s: an output overlaps S_in", what);
-  }
   if (overlap(y, out[0].n, S_out, states) || overlap(workspace, need, S_out, states) || overlap(workspace, need, y, out[0].n))
     return fail(SKSSM_EINVAL, "%s: the outputs overlap", what);
   if (S_in != S_out && overlap(S_in, states, S_out, states))
@@ -270,6 +282,9 @@ int sketchssm_norm(const skssm_norm_args* args, void* stream) {
     const bool same = x.p == p.residual_out && x.ld == p.ld_residual_out && x.dtype == p.io_dtype;
     if (!same && overlap(p.residual_out, nr, x.p, x.n)) return fail(SKSSM_EINVAL, "%s: residual_out overlaps an input", what);
   }
+  const Range outs[] = {{p.out, no}, {fp8 ? p.scales : nullptr, ns}, {p.residual_out, nr}};
+  const Range parameters[] = {{p.weight, (size_t)n * 4}, {p.D, p.D ? (size_t)(n / p.skip_width) * 4 : 0}};
+  if (any_overlap(outs, parameters)) return fail(SKSSM_EINVAL, "%s: an output overlaps weight or D", what);
   if (overlap(p.out, no, p.residual_out, nr) || (fp8 && (overlap(p.out, no, p.scales, ns) || overlap(p.residual_out, nr, p.scales, ns))))
     return fail(SKSSM_EINVAL, "%s: the outputs overlap", what);
   if (M == 0) return fail(SKSSM_OK, "%s", "");  // nothing to do: no launch, no error
@@ -326,10 +341,9 @@ int sketchssm_matmul_fp8(int64_t M, int32_t N, int32_t K, const void* a, int64_t
     return fail(SKSSM_EINVAL, "%s: workspace of %zu bytes, %zu needed", what, workspace ? workspace_bytes : (size_t)0, need);
   const int64_t kb = ((int64_t)K + 127) / 128, nb = ((int64_t)N + 127) / 128;
   const size_t ny = span(M, ldy, N, elem(out_dtype));
-  const struct { const void* p; size_t n; } in[4] = {{a, span(M, lda, K, 1)}, {w, span(N, ldw, K, 1)},
-      {a_scale, span(kb, ld_ascale, M, 4)}, {w_scale, (size_t)(nb * kb * 4)}};
-  for (const auto& p : in)
-    if (overlap(y, ny, p.p, p.n) || overlap(workspace, need, p.p, p.n)) return fail(SKSSM_EINVAL, "%s: y or workspace overlaps an input", what);
+  const Range in[] = {{a, span(M, lda, K, 1)}, {w, span(N, ldw, K, 1)}, {a_scale, span(kb, ld_ascale, M, 4)}, {w_scale, (size_t)(nb * kb * 4)}};
+  const Range out[] = {{y, ny}, {workspace, need}};
+  if (any_overlap(out, in)) return fail(SKSSM_EINVAL, "%s: y or workspace overlaps an input", what);
   if (overlap(y, ny, workspace, need)) return fail(SKSSM_EINVAL, "%s: y overlaps workspace", what);
   if (M == 0) return fail(SKSSM_OK, "%s", "");  // nothing to do: no launch, no error
   skssm::MatmulArgs p{};

@@ -263,3 +263,31 @@ def test_scan_workspace_of_many_heads_and_tokens(lib):
         assert lib.sketchssm_scan_workspace(c, heads, T) == 0, (heads, T)
     c = B.make_config("mamba2", 1, 2, 128, 64, 16, 16, "bf16")
     assert lib.sketchssm_scan_workspace(c, 1, 1 << 30) > 0
+
+
+@cpu_only
+def test_outputs_over_parameters_are_refused(lib):
+    """No output may lie over an array that other workgroups still read: taps, biases, offsets, A, D, weights."""
+    def refused(rc):
+        return rc == -1 and "overlap" in B.sketchssm_last_error()
+    # convolution: y [64][1024] bf16, new states [2][3][1024] bf16
+    for p in (dict(taps=at(7) + 1024), dict(bias=at(7) + 1024), dict(off=at(7) + 1024), dict(taps=at(6)), dict(bias=at(6) + 64), dict(off=at(6) + 64)):
+        assert refused(conv(lib, **p)), p
+    # one token: the ring's slots, q and the state
+    for where in (at(4), at(7), at(8), at(9), at(10), at(11)):
+        for name in ("taps", "bias", "dt_bias", "A"):
+            assert refused(token(lib, **{name: where})), (name, where)
+    # scan: y, S_out (and, where there is one, the workspace)
+    for where in (at(7), at(8)):
+        for name in ("off", "bias", "A", "D"):
+            assert refused(scan(lib, **{name: where})), (name, where)
+    need = lib.sketchssm_scan_workspace(cfg(batch=1), 4, 1 << 16)
+    for name in ("off", "bias", "A", "D"):
+        assert refused(scan(lib, c=cfg(batch=1), T=1 << 16, ws=at(20), nws=need, **{name: at(20) + 64})), name
+    # norm: the output, its scales and the residual's sum
+    res = dict(residual=at(5), ld_residual=512, residual_out=at(9), ld_residual_out=512)
+    gate = dict(gate=at(6), ld_gate=512, skip=at(7), ld_skip=512, skip_head=64, skip_width=64)
+    for where in (at(3), at(4), at(9)):
+        assert refused(lib.sketchssm_norm(norm_args(weight=where, **res), None)), where
+    for where in (at(3), at(4)):
+        assert refused(lib.sketchssm_norm(norm_args(D=where, **gate), None)), where
