@@ -9,7 +9,8 @@ call into libsketchssm.so.  Tensors are on the current device; matrices are
 read where they lie as long as their rows are contiguous (any row stride of
 whole 16-byte pieces).  Outputs and workspaces are allocated where the caller
 gives none.  A tensor of the wrong type, shape, device or layout raises
-ValueError; what the library itself refuses raises SketchSSMError.
+ValueError; what the library itself refuses raises SketchSSMError.  Results
+carry no gradient history: there is no backward pass.
 
 Types: io is bfloat16 or float32; parameters (taps, biases, weights, A, D) and
 scales are float32, 8-bit values torch.float8_e4m3fn, offsets int32.
@@ -84,9 +85,13 @@ def _device(x: Tensor) -> int:
 
 def _offsets(offsets: Tensor | None, batch: int | None, dev: int) -> tuple[int, int | None]:
     """(sequences, address of their offsets or None)"""
+    if batch is not None and batch < 1:
+        raise ValueError(f"a batch of {batch}")
     if offsets is None:
         return (1 if batch is None else batch), None
     n = offsets.numel() - 1
+    if n < 1:
+        raise ValueError(f"offsets: {n + 1} entries, one more than the sequences are needed")
     if batch is not None and batch != n:
         raise ValueError(f"offsets of {n} sequences for a batch of {batch}")
     return n, _flat("offsets", offsets, (n + 1,), torch.int32, dev)
@@ -212,7 +217,7 @@ def norm(x: Tensor, weight: Tensor, eps: float, *, group: int | None = None, res
         out_dtype = t
     f8 = out_dtype is F8
     io = _IO.get
-    a = B.NormArgs(M, N, group or N, io(x.dtype, -1), io(t, -1), B.E4M3 if f8 else io(out_dtype, -1), 0, eps, x.data_ptr(),
+    a = B.NormArgs(M, N, N if group is None else group, io(x.dtype, -1), io(t, -1), B.E4M3 if f8 else io(out_dtype, -1), 0, eps, x.data_ptr(),
                    _matrix("x", x, (M, N), x.dtype, dev))
     a.weight = _flat("weight", weight, (N,), _F32, dev)
     if residual is not None:

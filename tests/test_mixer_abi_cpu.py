@@ -291,3 +291,27 @@ def test_outputs_over_parameters_are_refused(lib):
         assert refused(lib.sketchssm_norm(norm_args(weight=where, **res), None)), where
     for where in (at(3), at(4)):
         assert refused(lib.sketchssm_norm(norm_args(D=where, **gate), None)), where
+
+
+def test_ops_refuse_counts_below_one(monkeypatch):
+    """No group of no columns (it was taken for all of them), no batch below one, no offsets without an entry."""
+    with pytest.raises(ValueError, match="offsets"):
+        ops._offsets(torch.zeros(0, dtype=torch.int32), None, -1)
+    for batch in (0, -1):
+        with pytest.raises(ValueError, match="batch"):
+            ops._offsets(None, batch, -1)
+    assert ops._offsets(None, None, -1) == (1, None) and ops._offsets(None, 5, -1) == (5, None)
+    # norm, as far as the call into the library: its group as it was given
+    seen = []
+
+    class Library:
+        def sketchssm_norm(self, a, stream):
+            seen.append(a.group)
+            return 0
+    monkeypatch.setattr(ops, "_device", lambda x: -1)
+    monkeypatch.setattr(ops, "_stream", lambda dev: 0)
+    monkeypatch.setattr(B, "_lib", Library())
+    x, w = torch.zeros((2, 64)), torch.ones(64)
+    for group in (None, 0, 32):
+        ops.norm(x, w, 1e-5, group=group)
+    assert seen == [64, 0, 32]  # (the library refuses 0)
