@@ -1,6 +1,7 @@
-"""The machine code of the kernels built here, where correctness hangs on it:
+"""The machine code of the kernels built here, where correctness or speed hangs on it:
 a scalar write of M0 and a load into LDS that takes its address from M0 need one
-wait state between them, which the compiler does not add inside assembly text."""
+wait state between them, which the compiler does not add inside assembly text;
+and a kernel past its line of registers loses a wave per SIMD."""
 import os
 import re
 import subprocess
@@ -8,7 +9,7 @@ import subprocess
 import pytest
 
 from paper_2609_33051_amd import build
-from test_kernel_resources import _code_objects
+from test_kernel_resources import _code_objects, kernels  # noqa: F401
 
 OBJDUMP = os.path.join(os.path.dirname(os.path.realpath(build.HIPCC)), "..", "llvm", "bin", "llvm-objdump")
 
@@ -35,3 +36,14 @@ def test_m0_is_settled_before_a_load_into_lds(listing):
     for i in loads:
         assert not re.match(r"s_\w+ m0,", listing[i - 1]), f"{listing[i - 1]} / {listing[i]}"
         assert any(re.match(r"s_\w+ m0,", x) for x in listing[i - 4:i]), listing[i - 4:i + 1]
+
+
+# waves a SIMD (512 registers in eights) that the kernels' figures hang on: the scan's bf16 workgroups come two a CU
+@pytest.mark.parametrize("kernel,most", [
+    (r"scan_kernel<unsigned short, .*", 256), (r"scan_kernel<float, .*", 512), (r"matmul_tile_kernel<.*", 256),
+    (r"conv_kernel<.*", 128), (r"conv_token_kernel<.*", 128), (r"norm_kernel<.*", 128)])
+def test_mixer_kernel_registers(kernels, kernel, most):
+    found = {n: v for n, v in kernels.items() if re.fullmatch(kernel, n)}
+    assert found
+    for name, (regs, spilled) in found.items():
+        assert regs <= most and spilled == 0, (name, regs, spilled)
