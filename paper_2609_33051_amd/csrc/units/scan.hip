@@ -27,6 +27,7 @@
 // the matrix units'), 37 prompts of 12000 tokens 211 us.  Matrix and vector units add up to
 // 96 % of the first launch's time and 87 % of the second's: what is left is
 // waiting at the barriers and for LDS, with the two waves a SIMD that registers and LDS allow.
+#include <limits.h>
 #include <math.h>
 
 #include <type_traits>
@@ -230,22 +231,18 @@ __device__ __forceinline__ double lane_of(double x, int lane) {
 }
 
 // The sequence that is `rank`-th by length, longest first: workgroups start in this order, so
-// that the card does not wait for a long sequence that began last.  (37 prompts of 0 to
-// 1214 tokens, 128 heads: 218 -> 211 us.)  Each workgroup of 256 threads counts for itself, a thread
-// a sequence; of more than 256 one is little of the whole.
-__device__ __forceinline__ int by_length(const Sequences& q, int rank, int* lds, int tid) {
-  if (!q.offsets || q.batch < 2 || q.batch > 256) return rank;
-  const int length = tid < q.batch ? q.start(tid + 1) - q.start(tid) : 0;
-  lds[tid] = length;
-  lds_barrier();
+// that the card does not wait for a long sequence that began last.  Every wave counts for itself, a
+// lane a sequence; for 64 sequences at the most, of three chunks on average: shorter ones
+// leave nothing to wait for, and counting (over 256 sequences in 6 us a workgroup) is a large part of them.
+// 128 heads of 128 x 64, uneven lengths, by packed order / by length (us): 37 sequences of 324 tokens on average
+// 219 / 212, 16 of 200 85 / 82, 8 of 1000 160 / 163; with a count over all of up to 256: 100 of 400 613 / 609, of 200
+// 352 / 363, of 80 199 / 220, 256 of 30 440 / 572, 37 of 100 91 / 94.
+__device__ __forceinline__ int by_length(const Sequences& q, int rank, int lane) {
+  if (!q.offsets || q.batch < 2 || q.batch > 64 || q.tokens < 3 * kChunk * q.batch) return rank;
+  const int length = lane < q.batch ? q.start(lane + 1) - q.start(lane) : INT_MIN;
   int before = 0;
-  for (int b = 0; b < q.batch; ++b) {
-    const int other = lds[b];
-    before += other > length || (other == length && b < tid);
-  }
-  if (tid < q.batch && before == rank) lds[256] = tid;
-  lds_barrier();
-  return __builtin_amdgcn_readfirstlane(lds[256]);
+  for (int b = 0; b < q.batch; ++b) before += __builtin_amdgcn_readlane(length, b) + (b < lane) > length;
+  return __builtin_ctzll(__ballot(lane < q.batch && before == rank));
 }
 
 // LOCAL: the state part alone, over the segment before the slot's (first launch).
@@ -278,7 +275,7 @@ __global__ __launch_bounds__(256, sizeof(IO) == 2 ? 2 : 1) void scan_kernel(Scan
     s.p0 -= seg;
     --s.k;
   } else if (slot < a.seq.batch) {
-    s.first(a.seq, by_length(a.seq, slot, reinterpret_cast<int*>(lds), tid), seg);
+    s.first(a.seq, by_length(a.seq, slot, lane), seg);
   } else if (!s.later(a.seq, slot - a.seq.batch + 1, seg)) {
     return;
   }

@@ -201,3 +201,18 @@ def test_silu_is_fp32():
     u = want.reshape(-1, 8, 8)
     y = (u / (u.square().mean(-1, keepdim=True) + 1e-30).sqrt()).reshape(x.shape)
     R.close(out, y, y.abs() * 32 * R.U32, "norm")
+
+
+@pytest.mark.parametrize("lengths", [[(97 * i) % 400 for i in range(64)], [(89 * i) % 400 for i in range(65)], [192] * 3, [0, 600, 0, 600, 1, 600],
+                                     [575, 1], [1, 575], [191, 192, 192]])
+def test_scan_orders_sequences_by_length(lengths):
+    """Every sequence is scanned once where workgroups start longest first: ties, empty ones, both sides of the rule."""
+    case("scan order", len(lengths), sum(lengths))
+    H, G, K, V = 2, 1, 64, 64
+    a, S = scan_inputs(len(lengths), lengths, H, G, K, V, "bf16")
+    y, St = run_scan(a, S, lengths, H, G, K, V, "bf16")
+    wy, my, wS, mS = definition(a, S, lengths, H, G)
+    skip = skip_terms(a, H)
+    acc = (max(lengths) + 64) * R.U32 + 100 * 2.0 ** -22
+    R.close(y.cpu(), wy, (my - skip) * (1.02 * R.U16 + acc) + skip * (4 * R.U32 + acc) + wy.abs() * R.U16 + 1e-30, "y")
+    R.close(St.cpu(), R.tiles(wS), R.tiles(mS) * acc + 1e-30, "S")
