@@ -326,7 +326,9 @@ int launch_tiles(const MatmulArgs& p, int splits, hipStream_t s) {
 //     64 x 18560 x 4096     -   25.2    22.1   17.1   19.3
 //      1 x 18560 x 4096     -      -       -   16.0   15.1     (weights straight into registers: 19.5)
 // so: the largest tiles of which there is one for each CU, but for 256 x 256, of which a
-// round of all CUs has to be full -- what is left over goes to smaller ones.
+// round of all CUs has to be full -- what is left over goes to smaller ones -- and half a tile's rows
+// have to be there: 131072 x 4096, of 1 / 64 / 100 / 128 / 129 rows, 256 x 256: 142 / 147 / 152 / 154 / 152, without:
+// 98 / 117 / 139 / 142 / -.
 // K split (not / by 2 / by 4): 77 x 4096 x 8192, 64x64: 23.7 / 17.5 / 15.5; 16 x 4096 x 8192 23.1 / 16.0 / 11.4; 16 x
 // 4096 x 4096 12.1 / 10.4 / 9.6; 200 x 2048 x 4096 13.8 / 13.2 / 13.6; 100 x 2048 x 2048 8.1 / 8.7 / 8.7: over what fills the
 // CUs in parts of 8 blocks at least, or twice that in parts of 16.
@@ -334,7 +336,7 @@ struct MatmulPlan { int wide, rest, splits; };
 MatmulPlan matmul_plan(int M, int N, int K, bool narrow) {  // M, N, K >= 1
   constexpr int64_t cus = 256;
   auto tiles = [&](int bm, int bn, int n) { return (int64_t)((M + bm - 1) / bm) * ((n + bn - 1) / bn); };
-  if (narrow && tiles(256, 256, N) >= cus) {
+  if (narrow && M > 128 && tiles(256, 256, N) >= cus) {
     const int64_t all = tiles(256, 256, N), rounds = all / cus, over = all % cus;
     if (over == 0 || over > cus / 2) return {(N + 255) / 256 * 256, 0, 1};
     const int64_t rows = (M + 255) / 256, columns = rounds * cus / rows;

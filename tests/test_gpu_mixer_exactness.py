@@ -216,3 +216,19 @@ def test_scan_orders_sequences_by_length(lengths):
     acc = (max(lengths) + 64) * R.U32 + 100 * 2.0 ** -22
     R.close(y.cpu(), wy, (my - skip) * (1.02 * R.U16 + acc) + skip * (4 * R.U32 + acc) + wy.abs() * R.U16 + 1e-30, "y")
     R.close(St.cpu(), R.tiles(wS), R.tiles(mS) * acc + 1e-30, "S")
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 66000, 144), (64, 65540, 128), (65, 65601, 272), (128, 65536, 256), (129, 65536, 256), (257, 40001, 144)])
+def test_matmul_of_few_rows_and_many_columns(M, N, K):
+    """A vocabulary's columns for a decode batch: both sides of the rule that gives the widest tiles to more rows."""
+    case("matmul columns", M, N, K)
+    r = rnd(M + N)
+    kb, nb = -(-K // 128), -(-N // 128)
+    f8 = lambda shape: r(shape, scale=130.0).clamp(-448, 448).to(ops.F8)  # noqa: E731
+    a, w = f8((M, K)), f8((N, K))
+    sa, sw = torch.exp(r((kb, M))), torch.exp(r((nb, kb)))
+    y = ops.matmul_fp8(a, sa, w, sw)
+    rows = torch.tensor(sorted({0, M // 2, M - 1}), device="cuda")
+    want, mag, top = R.matmul(a.float()[rows].to(ops.F8), sa[:, rows], w, sw)
+    R.close(y[rows], want, (128 + K / 128 + 4) * R.U32 * mag + top * 2.0 ** -11 + want.abs() * R.U16, "bf16")
+    assert bool(torch.isfinite(y).all())
