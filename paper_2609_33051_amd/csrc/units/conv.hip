@@ -76,10 +76,13 @@ __device__ __forceinline__ Raw<IO, 16 / sizeof(IO)> conv_row(const Taps<IO, W>& 
 
 // Tokens of a wave, loaded together, and waves of a workgroup, one below the other on the
 // same 64 lanes of channels, so that they share their taps: 12, or 4 where there would be fewer than ten for
-// each SIMD.  Measured, rows of 10240 bf16, four taps, 12 / 4 (us): 16384 tokens 122 / 138 (5.5 TB/s, 91 % of what the
-// same loads and stores reach without the sums, 110; 16 tokens 123, 8 129), 4096 37.1 / 38.9,
-// 512 6.5 / 7.5, 256 5.7 / 4.8; 777 x 1792 fp32 6.9 / 5.2.  Each thread loading its own taps took 128 for the
-// first; a workgroup of 16 tokens by 4 KB, which only reads what it writes, 114.
+// each SIMD.  Measured, rows of 10240 bf16, four taps, 12 / 4 (us): 16384 tokens 119 / 128 (5.7 TB/s, 92 % of what the
+// same loads and stores reach without the sums, 110; 16 tokens 119, 8 125), 4096 36.8 / 38.0,
+// 512 6.8 / 7.8, 256 6.2 / 5.3; 777 x 1792 fp32 7.6 / 5.3.  Each thread loading its own taps took 10 more for the
+// first.
+// Rows are loaded and stored past the caches: a stream larger than them gains by it, one that the scan finds there loses
+// less.  Stored past them / not, alone: 16384 tokens 119 / 137, 4096 36.3 / 37.3; with the
+// scan behind it: 16384 446 / 448, 8192 244 / 241, 4096 151 / 145, 2048 88 / 84, 1024 62 / 62.
 constexpr int kConvRows = 12, kConvFew = 4, kDown = 4;
 
 template <typename IO, int CH> __device__ __forceinline__ void store_nt(const Raw<IO, CH>& r, IO* p) {

@@ -12,7 +12,8 @@
 // 5e-5 of the result where the exponents vary most; 16x16x32_fp8_fp8 the same).
 // Under an output stored in bf16 (2^-8) that is nothing.  An fp32 output is computed
 // from the same values as bf16, which holds e4m3 exactly, by four 16x16x32_bf16
-// (7.5e-8 on the same blocks) at half the rate.
+// (7.5e-8 on the same blocks) at half the rate: 8192 x 18560 x 4096 558 us for bf16 outputs (2.2 PFLOP/s), 1140 for
+// fp32 (1.1), 1024 x 4096 x 4096 27 and 42, 1 x 18560 x 4096 15 and 20.
 #include <algorithm>
 #include <type_traits>
 

@@ -122,7 +122,8 @@ int launch_norm(const NormArgs& a, hipStream_t s) {
 // Threads and 8-column pieces a thread, by the group's width.  8192 rows with the residual into
 // 8 bits, bf16 (us; the best copy moves 6.4 TB/s): 1024 columns 11.7, 2048 23.2 to 25 (5.0 TB/s; 256
 // threads 26.4), 4096 46.6 (5.0), 8192 90 (5.2; 1024 threads 92.8); 16384 columns of
-// an ordinary norm 93.9 (4.3; 1024 threads 108); gated, 8192 columns by groups of 1024 68.7 (4.9).
+// an ordinary norm 93.9 (4.3; 1024 threads 108); gated, 8192 columns by groups of 1024 67.3 (5.0).  Into bf16: 4096 columns
+// with the residual 47.7 (5.6), 16384 of an ordinary norm 101 (5.3).
 // Reads past the caches move these by -4 % to +18 %, reads and writes past them by -9 % to +9 %:
 // they gain where nothing is used again soon and lose where it is, and a norm's output is.
 template <typename TX, typename IO, bool FP8, int FORM>

@@ -25,7 +25,7 @@
 // Measured, 128 heads of 128 x 64 in 8 groups, bf16: one prompt of 16384 tokens 330 us (states 110,
 // outputs 220; its bytes take 96 at the best copy's rate, its products in this form 100 of
 // the matrix units'), 37 prompts of 12000 tokens 211 us.  Matrix and vector units add up to
-// 96 % of the first launch's time and 87 % of the second's: what is left is
+// 96 % of the first launch's time and 86 % of the second's: what is left is
 // waiting at the barriers and for LDS, with the two waves a SIMD that registers and LDS allow.
 #include <limits.h>
 #include <math.h>
@@ -47,9 +47,10 @@ typedef short shortx4 __attribute__((ext_vector_type(4)));
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 
 // 64 rows of COLS elements in LDS.  The 16-byte chunks of a row are permuted by the row, so
-// that neither of two reads finds its lanes in the same banks: 16 bytes of 16 consecutive
+// that two reads keep their lanes in different banks: 16 bytes of consecutive
 // rows, and the transposed read's four rows of 64 bytes (rows of 128 bytes differ by their
-// place already where they follow one another).
+// place already where they follow one another).  The states' launch has no conflicts by its counters; the
+// outputs' has them in 19 % of its LDS cycles, at what only it accesses: the operands and the tile of the scores.
 template <typename IO, int COLS> struct Tile {
   static constexpr int kBytes = kChunk * COLS * (int)sizeof(IO), kChunks = COLS * (int)sizeof(IO) / 16;
   static constexpr int kPer = 16 / (int)sizeof(IO);  // elements of a chunk
