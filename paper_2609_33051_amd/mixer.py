@@ -38,11 +38,14 @@ class Mamba2Mixer:
     this order, taps [C][w], conv_bias [C] (or None), dt_bias, A and D [H]
     (A < 0), out_norm [H V], out_proj [hidden][H V].  The projections are
     quantised here.  omega and coef are the sketch's, and the other sketch
-    arguments those of SketchSSMLayer."""
+    arguments those of SketchSSMLayer.  The gated norm's groups (H V / G columns
+    each, where G > 1) are whole blocks of 128, hidden and H V multiples of 16.
+    Shapes that do not fit raise ValueError here, before a prompt moves any state."""
 
     def __init__(self, weights: dict, batch: int, heads: int, groups: int, dk: int, dv: int, rank: int, window: int,
                  omega: Tensor, coef: Tensor, io: str = "bf16", eps: float = 1e-5, device="cuda", **sketch):
         dev = torch.device(device)
+        self._check(weights, heads, groups, dk, dv)
         f32 = lambda n: None if weights.get(n) is None else weights[n].to(dev, torch.float32).contiguous()  # noqa: E731
         self.batch, self.heads, self.groups, self.dk, self.dv, self.eps = batch, heads, groups, dk, dv, eps
         self.dtype = torch.bfloat16 if io == "bf16" else torch.float32
@@ -55,6 +58,25 @@ class Mamba2Mixer:
         self.layer = SketchSSMLayer("mamba2", batch, heads, dk, dv, rank, window, io, device, omega=omega, coef=coef, **sketch)
         self.conv_state = torch.zeros((batch, self.taps.shape[1] - 1, self.channels), dtype=self.dtype, device=dev)
         self.q = torch.empty((batch, heads, dk), dtype=self.dtype, device=dev)
+
+    @staticmethod
+    def _check(weights: dict, heads: int, groups: int, dk: int, dv: int) -> None:
+        if groups < 1 or heads % groups:
+            raise ValueError(f"{groups} groups do not divide {heads} heads")
+        HV, C = heads * dv, heads * dv + 2 * groups * dk
+        if groups > 1 and HV // groups % 128:
+            raise ValueError(f"{groups} groups of {HV // groups} columns cut the output norm's blocks of 128")
+        hidden = weights["in_proj"].shape[1]
+        if hidden % 16 or HV % 16:
+            raise ValueError(f"hidden size {hidden} and {HV} values: multiples of 16 are projected in 8 bits")
+        for name, shape in (("in_proj", (HV + C + heads, hidden)), ("out_proj", (weights["out_proj"].shape[0], HV)), ("norm", (hidden,)),
+                            ("out_norm", (HV,)), ("conv_bias", (C,)), ("dt_bias", (heads,)), ("A", (heads,)), ("D", (heads,))):
+            w = weights.get(name)
+            if w is not None and w.shape != shape:
+                raise ValueError(f"{name}: {list(w.shape)}, not {list(shape)}")
+        taps = weights["taps"].shape
+        if len(taps) != 2 or taps[0] != C or not 2 <= taps[1] <= 4:
+            raise ValueError(f"taps: {list(taps)}, not [{C}][2 to 4]")
 
     def _project_in(self, x: Tensor, residual: Tensor):
         u, s, residual = ops.norm(x, self.norm, self.eps, residual=residual, out_dtype=ops.F8)
