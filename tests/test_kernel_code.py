@@ -47,3 +47,18 @@ def test_mixer_kernel_registers(kernels, kernel, most):
     assert found
     for name, (regs, spilled) in found.items():
         assert regs <= most and spilled == 0, (name, regs, spilled)
+
+
+def test_the_loads_bases_are_settled_too(listing):
+    """A scalar register that a vector instruction writes is read by a memory instruction five wait states later at the earliest."""
+    for i, x in enumerate(listing):
+        if "_load_lds_" not in x:
+            continue
+        pair = {int(n) for n in re.search(r"s\[(\d+):(\d+)\]", x).groups()}
+        states = 0
+        for y in reversed(listing[max(0, i - 5):i]):
+            written = re.match(r"v_\w+ s(?:\[(\d+):(\d+)\]|(\d+)),", y)
+            if written and states < 5:
+                assert not pair & {int(n) for n in written.groups() if n}, f"{y} / {x}"
+            wait = re.match(r"s_nop (\d+)", y)
+            states += int(wait.group(1)) + 1 if wait else 1
