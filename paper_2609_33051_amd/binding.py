@@ -32,6 +32,10 @@ MIXER_FUNCTIONS = ("sketchssm_conv", "sketchssm_conv_token", "sketchssm_scan", "
                    "sketchssm_matmul_fp8", "sketchssm_matmul_fp8_workspace")
 E4M3 = 2
 
+# include/sketchssm_attention.h: a softmax attention layer's operators (ops.py takes tensors)
+ATTENTION_FUNCTIONS = ("sketchssm_cache_bytes", "sketchssm_rotary", "sketchssm_cache_append", "sketchssm_cache_read",
+                       "sketchssm_attention", "sketchssm_attention_workspace")
+
 
 class SketchSSMError(RuntimeError):
     def __init__(self, status: int, message: str):
@@ -76,6 +80,32 @@ class NormArgs(ctypes.Structure):
                    ("skip", ctypes.c_void_p), ("ld_skip", ctypes.c_int64), ("skip_head", ctypes.c_int64),
                    ("D", ctypes.c_void_p), ("weight", ctypes.c_void_p), ("out", ctypes.c_void_p),
                    ("ld_out", ctypes.c_int64), ("scales", ctypes.c_void_p), ("ld_scales", ctypes.c_int64)]
+
+
+class Cache(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p)] + [(name, ctypes.c_int32) for name in ("pages", "kv_heads", "page", "dim")]
+
+
+class NewTokens(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_int64), ("offsets", ctypes.c_void_p), ("lengths", ctypes.c_void_p), ("table", ctypes.c_void_p),
+                ("ld_table", ctypes.c_int64), ("batch", ctypes.c_int32), ("columns", ctypes.c_int32)]
+
+
+class Rotation(ctypes.Structure):
+    _fields_ = [("angles", ctypes.c_void_p), ("positions", ctypes.c_void_p)] + [
+        (name, ctypes.c_int32) for name in ("places", "rotated", "interleaved")]
+
+
+class AppendArgs(ctypes.Structure):
+    _fields_ = [("io_dtype", ctypes.c_int32), ("heads", ctypes.c_int32)] + [
+        f for x, ld in (("k", "ldk"), ("v", "ldv"), ("q", "ldq"), ("q_out", "ld_qout"))
+        for f in ((x, ctypes.c_void_p), (ld, ctypes.c_int64), (x.replace("_", "") + "_head", ctypes.c_int64))]
+
+
+class AttentionArgs(ctypes.Structure):
+    _fields_ = [("io_dtype", ctypes.c_int32), ("out_dtype", ctypes.c_int32), ("heads", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("q", ctypes.c_void_p), ("ldq", ctypes.c_int64), ("q_head", ctypes.c_int64), ("out", ctypes.c_void_p), ("ld_out", ctypes.c_int64),
+                ("scales", ctypes.c_void_p), ("ld_scales", ctypes.c_int64), ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)]
 
 
 _lib = None
@@ -123,6 +153,16 @@ def load(path: str | None = None):
     lib.sketchssm_scan_workspace.argtypes = [cfgp, i32, i64]
     lib.sketchssm_matmul_fp8_workspace.argtypes = [i64, i32, i32]
     lib.sketchssm_scan_workspace.restype = lib.sketchssm_matmul_fp8_workspace.restype = size
+    cachep, tokp, rotp = ctypes.POINTER(Cache), ctypes.POINTER(NewTokens), ctypes.POINTER(Rotation)
+    lib.sketchssm_rotary.argtypes = [i32, i64, i32, i32, rotp, P, i64, i64, P, i64, i64, P]
+    lib.sketchssm_cache_append.argtypes = [cachep, tokp, rotp, ctypes.POINTER(AppendArgs), P]
+    lib.sketchssm_cache_read.argtypes = [cachep, tokp, i32, P, P, P]
+    lib.sketchssm_attention.argtypes = [cachep, tokp, ctypes.POINTER(AttentionArgs), P]
+    for f in ("sketchssm_rotary", "sketchssm_cache_append", "sketchssm_cache_read", "sketchssm_attention"):
+        getattr(lib, f).restype = ctypes.c_int
+    lib.sketchssm_cache_bytes.argtypes = [cachep]
+    lib.sketchssm_attention_workspace.argtypes = [cachep, i32, i32, i64, i32]
+    lib.sketchssm_cache_bytes.restype = lib.sketchssm_attention_workspace.restype = size
     _lib = lib
     return lib
 

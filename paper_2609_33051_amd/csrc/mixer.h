@@ -65,6 +65,16 @@ __device__ __forceinline__ float softplus(float r) {
   return fmaf(2.f * z, t, fmaxf(r, 0.f));
 }
 
+// Largest of a row's 16 values, by their bits: magnitudes order as integers, NaN above all.
+__device__ __forceinline__ uint32_t row_max16(uint32_t x) {
+  auto step = [](uint32_t v, uint32_t w) { return v > w ? v : w; };
+  x = step(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0xB1, 0xF, 0xF, true));
+  x = step(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x4E, 0xF, 0xF, true));
+  x = step(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x141, 0xF, 0xF, true));
+  x = step(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x140, 0xF, 0xF, true));
+  return x;
+}
+
 // What a launch can hold: fewer than 2^32 threads.  A call whose launches do not all fit makes none and returns -3.
 inline bool fits(int64_t workgroups, int threads) { return workgroups * threads < (int64_t)1 << 32; }
 // Whether the launches so far were taken: one that follows from them is not made where they were not.

@@ -1,0 +1,668 @@
+// Attention of the new tokens over a paged cache in 4 bits.
+//
+// A wave holds QT tiles of 16 query rows (a row is one head of one new token; the heads that share a key
+// head lie together) and goes over the keys 32 at a time:
+//     S^T = K Q^T, P^T = 2^(c S^T - m), O^T += V^T P^T      (16 x 16 x 32 matrix products)
+// Both products take the cache as their left operand, so that a query row is one column, one lane in each of
+// the wave's four rows of lanes: the running maximum and every weight are a lane's own, and P^T comes out of
+// the first product in the registers in which the second one takes it (the order in which the 32
+// keys are summed is free, and the cache's records hold the values in the order it leaves).  Nothing passes
+// through LDS.  A row of ones beside V^T sums the weights as the products see them.
+//
+// The maximum that the weights are taken over moves only where a score is past it by more than 2^8; until
+// then nothing is rescaled.
+#include <type_traits>
+
+#include "../attention.h"
+
+namespace skssm {
+
+namespace {
+
+constexpr int kWaves = 4, kThreads = 64 * kWaves;
+constexpr int kStep = 32;         // keys a step
+constexpr int kShare = 1024;      // workgroups that a split is made for: four a CU
+constexpr int kLeast = kWaves;    // steps a workgroup takes at least: one a wave
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+__device__ __forceinline__ floatx4 mfma(bf16x8 a, bf16x8 b, floatx4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+
+// N consecutive words of a record, 4-byte aligned at least (8 where N is even).
+template <int N> struct Words {
+  uint32_t w[N];
+  __device__ __forceinline__ void load(const uint8_t* p) {
+    typedef uint32_t w2 __attribute__((ext_vector_type(2), aligned(8)));
+    typedef uint32_t w3 __attribute__((ext_vector_type(3), aligned(4)));
+    typedef uint32_t w4 __attribute__((ext_vector_type(4), aligned(8)));
+    if constexpr (N == 3) {
+      const w3 t = *reinterpret_cast<const w3*>(p);
+      w[0] = t.x; w[1] = t.y; w[2] = t.z;
+    } else {
+#pragma unroll
+      for (int i = 0; i + 4 <= N; i += 4) {
+        const w4 t = *reinterpret_cast<const w4*>(p + 4 * i);
+        w[i] = t.x; w[i + 1] = t.y; w[i + 2] = t.z; w[i + 3] = t.w;
+      }
+      if constexpr (N % 4 == 2) {
+        const w2 t = *reinterpret_cast<const w2*>(p + 4 * (N - 2));
+        w[N - 2] = t.x; w[N - 1] = t.y;
+      }
+    }
+  }
+};
+
+// Byte i of w as the exponent of an fp32 number.  The conversions take their scale's exponent and nothing else of it.
+template <int N> __device__ __forceinline__ float exponent(const Words<N>& w, int i) {
+  const uint32_t x = w.w[i >> 2];
+  return __uint_as_float((i & 3) == 3 ? x >> 1 : x << (23 - 8 * (i & 3)));
+}
+
+__device__ __forceinline__ uint32_t two(uint32_t w, float scale, int byte) {
+  switch (byte) {
+    case 0: return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0));
+    case 1: return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1));
+    case 2: return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2));
+    default: return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3));
+  }
+}
+
+// One record of 16 tokens as a lane (r = lane % 16, a = lane / 16) takes it: channels a D/4 .. of token r's key,
+// bytes r of every block of the values of tokens 4 a .. 4 a + 3.
+template <int D> struct Tile {
+  static constexpr int N = D / 32;
+  Words<N> k, v, vs;
+  uint32_t ks[2];  // exponents of the key's blocks that the channels lie in
+  __device__ __forceinline__ void load(const uint8_t* rec, int lane, uint32_t bad) {
+    const int r = lane & 15, a = lane >> 4;
+    k.load(rec + r * (D / 2) + a * (D / 8));
+    v.load(rec + 8 * D + lane * (D / 8));
+    vs.load(rec + 16 * D + D / 2 + a * (D / 8));
+    const uint8_t* e = rec + 16 * D + r * N;
+    const int g = a * (D / 4) / 32;
+    ks[0] = e[g] | bad;
+    if constexpr (D != 64 && D != 128) ks[1] = e[g + 1 < N ? g + 1 : g] | bad;
+  }
+  // The key's 8 channels a D/4 + 8 j ..
+  __device__ __forceinline__ bf16x8 key(int j, int lane) const {
+    uint32_t e = ks[0];
+    if constexpr (D == 256) e = j < 4 ? ks[0] : ks[1];
+    if constexpr (D == 96 || D == 192) {
+      const int c = (lane >> 4) * (D / 4);
+      e = (c + 8 * j) / 32 == c / 32 ? ks[0] : ks[1];
+    }
+    const float s = __uint_as_float(e << 23);
+    const uint4 t = make_uint4(two(k.w[j], s, 0), two(k.w[j], s, 1), two(k.w[j], s, 2), two(k.w[j], s, 3));
+    return __builtin_bit_cast(bf16x8, t);
+  }
+};
+
+// Channels 32 g + r and 32 g + r + 16 of the values of eight tokens, four of each record.
+template <int D> __device__ __forceinline__ void values(const Tile<D>& x, const Tile<D>& y, int g, bf16x8& lo, bf16x8& hi) {
+  constexpr int N = D / 32;
+  uint32_t c[8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    c[i] = two(x.v.w[g], exponent(x.vs, i * N + g), i);
+    c[i + 4] = two(y.v.w[g], exponent(y.vs, i * N + g), i);
+  }
+  uint32_t l[4], h[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    l[i] = __builtin_amdgcn_perm(c[2 * i + 1], c[2 * i], 0x05040100u);
+    h[i] = __builtin_amdgcn_perm(c[2 * i + 1], c[2 * i], 0x07060302u);
+  }
+  lo = __builtin_bit_cast(bf16x8, make_uint4(l[0], l[1], l[2], l[3]));
+  hi = __builtin_bit_cast(bf16x8, make_uint4(h[0], h[1], h[2], h[3]));
+}
+
+// Eight fp32 values as bf16, or as three parts that keep their 24 bits.
+template <int PARTS> __device__ __forceinline__ void parts(const float (&x)[8], bf16x8 (&out)[PARTS]) {
+  float r[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) r[i] = x[i];
+#pragma unroll
+  for (int p = 0; p < PARTS; ++p) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      w[i] = bf16_pack2(r[2 * i], r[2 * i + 1]);
+      if (p + 1 < PARTS) { r[2 * i] -= bf16_lo(w[i]); r[2 * i + 1] -= bf16_hi(w[i]); }
+    }
+    out[p] = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
+  }
+}
+
+__device__ __forceinline__ float across_rows_max(float x) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  const auto h = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(h[0]), __uint_as_float(h[1]));
+}
+
+// Weights 2^(c (s - m)) of scores s under a maximum m, c = scale log2 e.  EXACT: to fp32's last places, with what c's own
+// rounding leaves out; otherwise the product c m is rounded, by the same for every weight of a row.
+template <bool EXACT> struct Weight {
+  float c, low;
+  __device__ __forceinline__ explicit Weight(float scale) {
+    c = scale * 1.44269504f;
+    low = EXACT ? fmaf(scale, 1.92596299e-8f, fmaf(scale, 1.44269504f, -c)) : 0.f;
+  }
+  __device__ __forceinline__ float under(float m) const { return m == -INFINITY ? 0.f : EXACT ? m : m * c; }  // -inf: nothing seen yet
+  __device__ __forceinline__ float operator()(float s, float under) const {
+    if constexpr (EXACT) {
+      const float d = s - under, x = fmaf(d, c, d * low);
+      return __builtin_amdgcn_exp2f(d == -INFINITY ? d : x);
+    } else {
+      return __builtin_amdgcn_exp2f(fmaf(s, c, -under));
+    }
+  }
+  // What sums under the maximum m are multiplied by under a larger one.
+  __device__ __forceinline__ float from(float m, float to) const { return m == to ? 1.f : (*this)(m, under(to)); }
+};
+
+// ---- what a workgroup takes
+
+// Rows of a sequence's new tokens (tiles of ROWS) and the keys that they can see.
+struct Extent { int first, n, length, tiles, steps; };
+template <int ROWS> __device__ __forceinline__ Extent extent(const AttentionArgs& a, int b) {
+  Extent e;
+  e.first = a.tok.seq.start(b);
+  e.n = a.tok.seq.start(b + 1) - e.first;
+  e.n = e.n < 0 ? 0 : e.n;
+  const int length = a.tok.lengths[b];
+  e.length = length < -(1 << 30) ? -(1 << 30) : length < 1 << 30 ? length : 1 << 30;
+  const int most = (a.tok.columns << (a.cache.shift + 4)) + 1;  // one past the table, which reads as NaN
+  const int seen = e.length < 0 ? 0 : e.length < most ? e.length : most;
+  e.tiles = (e.n * a.group + ROWS - 1) / ROWS;
+  e.steps = (seen + kStep - 1) / kStep;
+  return e;
+}
+
+__device__ __forceinline__ int64_t wave_sum64(int64_t x) {
+  for (int d = 1; d < 64; d *= 2) x += __shfl_xor((long long)x, d);
+  return x;
+}
+
+// How a call's rows and keys are shared out where sequences are split: every sequence into pieces of `chunk`
+// steps, so many that all pieces of all heads together are about kShare.
+template <int ROWS> __device__ __forceinline__ int chunk_steps(const AttentionArgs& a) {
+  int64_t total = 0;
+  if (a.tok.seq.batch == 1) {
+    const Extent e = extent<ROWS>(a, 0);
+    total = (int64_t)e.tiles * e.steps;
+  } else {
+    for (int b = threadIdx.x & 63; b < a.tok.seq.batch; b += 64) {
+      const Extent e = extent<ROWS>(a, b);
+      total += (int64_t)e.tiles * e.steps;
+    }
+    total = wave_sum64(total);
+  }
+  const int64_t each = (total * a.cache.heads + kShare - 1) / kShare;
+  const int64_t whole = (each + kWaves - 1) / kWaves * kWaves;
+  return whole < kLeast ? kLeast : (int)(whole < (1 << 26) ? whole : 1 << 26);
+}
+__device__ __forceinline__ int pieces(const Extent& e, int chunk) { return e.steps <= chunk ? 1 : (e.steps + chunk - 1) / chunk; }
+
+// The sequence that holds unit u, with u's place in it; false where there are fewer.
+template <int ROWS> __device__ __forceinline__ bool find(const AttentionArgs& a, int chunk, int u, int& b, int& at) {
+  const int lane = threadIdx.x & 63;
+  int before = 0;
+  for (int b0 = 0; b0 < a.tok.seq.batch; b0 += 64) {
+    int units = 0;
+    if (b0 + lane < a.tok.seq.batch) {
+      const Extent e = extent<ROWS>(a, b0 + lane);
+      units = e.tiles * pieces(e, chunk);
+    }
+    int upto = units;  // inclusive
+    for (int d = 1; d < 64; d *= 2) {
+      const int x = __shfl_up(upto, d);
+      if (lane >= d) upto += x;
+    }
+    const unsigned long long hit = __builtin_amdgcn_ballot_w64(u < before + upto);
+    if (hit) {
+      const int l = __builtin_ctzll(hit);
+      b = b0 + l;
+      at = u - before - __builtin_amdgcn_readlane(upto - units, l);
+      return true;
+    }
+    before += __builtin_amdgcn_readlane(upto, 63);
+  }
+  return false;
+}
+
+// Units of the sequences before b.
+template <int ROWS> __device__ __forceinline__ int units_before(const AttentionArgs& a, int chunk, int b) {
+  int n = 0;
+  for (int i = threadIdx.x & 63; i < b; i += 64) {
+    const Extent e = extent<ROWS>(a, i);
+    n += e.tiles * pieces(e, chunk);
+  }
+  for (int d = 1; d < 64; d *= 2) n += __shfl_xor(n, d);
+  return n;
+}
+
+// ---- outputs
+
+// Eight consecutive channels of a row; 16 lanes of a DPP row hold a block of 128 columns.
+template <typename IO, bool FP8> __device__ __forceinline__ void put(const AttentionArgs& a, int token, int column, const float (&y)[8]) {
+  if constexpr (FP8) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t m = __float_as_uint(y[i]) & 0x7FFFFFFFu;
+      top = m > top ? m : top;
+    }
+    const float most = __uint_as_float(row_max16(top)) / 448.f;
+    const float s = most < 0x1p-64f ? 0x1p-64f : most;  // a NaN stays
+    const float inv = 1.f / s;
+    uint32_t lo = 0, hi = 0;
+    lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[0] * inv, y[1] * inv, lo, false);
+    lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[2] * inv, y[3] * inv, lo, true);
+    hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[4] * inv, y[5] * inv, hi, false);
+    hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[6] * inv, y[7] * inv, hi, true);
+    *reinterpret_cast<uint2*>(static_cast<uint8_t*>(a.out) + (size_t)token * a.ld_out + column) = make_uint2(lo, hi);
+    if ((column & 127) == 0) a.scales[(size_t)(column >> 7) * a.ld_scales + token] = s;
+  } else {
+    IO* dst = static_cast<IO*>(a.out) + (size_t)token * a.ld_out + column;
+    st_elem4(dst, y[0], y[1], y[2], y[3]);
+    st_elem4(dst + 4, y[4], y[5], y[6], y[7]);
+  }
+}
+
+// ---- the kernel
+
+// SPLIT: the workgroup's waves share the keys of one piece of a sequence for one tile of rows; its rows are
+// written where the sequence is one piece, else left in `work` for join_kernel.  Otherwise each wave has
+// a tile of rows of its own and all their keys.
+template <typename IO, int D, int QT, bool SPLIT, bool FP8>
+__global__ __launch_bounds__(kThreads) void attention_kernel(AttentionArgs a) {
+  // bf16 parts of a query and of a weight: what an fp32 result (the scales of an 8-bit output among them) has to keep
+  constexpr int N = D / 32, ROWS = 16 * QT, QP = sizeof(IO) == 2 ? 1 : 3, WP = FP8 ? 3 : QP, PITCH = D + 4;
+  __shared__ float shared[SPLIT ? kWaves * ROWS * PITCH + 2 * kWaves * ROWS : kWaves * 16 * PITCH];
+  const int lane = threadIdx.x & 63, r = lane & 15, kg = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int G = a.cache.heads, h = blockIdx.x % G, u = blockIdx.x / G;
+
+  int b, at, chunk = 1 << 26;
+  if constexpr (SPLIT) {
+    chunk = chunk_steps<ROWS>(a);
+    if (!find<ROWS>(a, chunk, u, b, at)) return;
+  } else {
+    if (!find<ROWS * kWaves>(a, chunk, u, b, at)) return;
+  }
+  const Extent e = extent<ROWS>(a, b);
+  const int count = SPLIT ? pieces(e, chunk) : 1;
+  // the last rows see the most keys: they go first
+  const int tile = SPLIT ? at / count : ((e.tiles + kWaves - 1) / kWaves - 1 - at) * kWaves + wave, piece = SPLIT ? at - tile * count : 0;
+  const int row0 = tile * ROWS, rows = e.n * a.group - row0 < ROWS ? e.n * a.group - row0 : ROWS;
+  if (!SPLIT && rows <= 0) return;
+  const int most = a.tok.columns << (a.cache.shift + 4);
+  auto limit = [&](int row) {  // the last key that a row sees
+    const int place = e.length - e.n + row / a.group;
+    return place < most ? place : most;
+  };
+  const int low = limit(row0), high = limit(row0 + rows - 1);
+  int lim[QT];
+#pragma unroll
+  for (int t = 0; t < QT; ++t) lim[t] = 16 * t + r < rows ? limit(row0 + 16 * t + r) : -1;
+
+  bf16x8 q[QT][N][QP];
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    const int row = row0 + 16 * t + r, i = row / a.group;
+    const bool in = 16 * t + r < rows;
+    const IO* src = static_cast<const IO*>(a.q) + (in ? (size_t)(e.first + i) * a.ldq + (size_t)(h * a.group + row - i * a.group) * a.q_head : 0) + kg * (D / 4);
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      Raw<IO, 8> x;
+      x.zero();
+      if (in) x.load(src + 8 * j);
+      if constexpr (QP == 1) {
+        q[t][j][0] = __builtin_bit_cast(bf16x8, make_uint4(x.w[0], x.w[1], x.w[2], x.w[3]));
+      } else {
+        float f[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) f[k] = x.get(k);
+        parts<QP>(f, q[t][j]);
+      }
+    }
+  }
+
+  const Weight<WP != 1> weight(a.scale);
+  floatx4 o[QT][2 * N], l[QT];
+  float m[QT];
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    m[t] = -INFINITY;
+    l[t] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < 2 * N; ++j) o[t][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+  }
+  const bf16x8 ones = __builtin_bit_cast(bf16x8, make_uint4(0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u));
+
+  const int stride = SPLIT ? kWaves : 1;
+  const int64_t begin = SPLIT ? (int64_t)piece * chunk : 0;
+  const int64_t last = (int64_t)high < 0 ? 0 : high / kStep + 1;
+  const int s1 = (int)(begin + chunk < last ? begin + chunk : last);
+  const int s0 = (int)begin + (SPLIT ? wave : 0);
+
+  struct Pages { int p0, p1; };
+  auto pages = [&](int s) {
+    Pages p;
+    p.p0 = a.tok.page(a.cache, b, 2 * s);
+    p.p1 = kStep * s + 16 <= high ? a.tok.page(a.cache, b, 2 * s + 1) : -2;  // -2: no row sees it
+    return p;
+  };
+  auto load = [&](Tile<D> (&x)[2], int s, const Pages& p) {
+    const uint8_t* r0 = record<D>(a.cache, p.p0 < 0 ? 0 : p.p0, h, 2 * s);
+    const uint8_t* r1 = p.p1 == -2 ? r0 : record<D>(a.cache, p.p1 < 0 ? 0 : p.p1, h, 2 * s + 1);
+    x[0].load(r0, lane, p.p0 < 0 ? 255u : 0u);
+    x[1].load(r1, lane, p.p1 == -1 ? 255u : 0u);
+  };
+  auto compute = [&](Tile<D> (&x)[2], int s) {
+    floatx4 z[QT][2];
+#pragma unroll
+    for (int t = 0; t < QT; ++t) z[t][0] = z[t][1] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const bf16x8 k = x[i].key(j, lane);
+#pragma unroll
+        for (int p = 0; p < QP; ++p)
+#pragma unroll
+          for (int t = 0; t < QT; ++t) z[t][i] = mfma(k, q[t][j][p], z[t][i]);
+      }
+    float w[QT][8];
+#pragma unroll
+    for (int t = 0; t < QT; ++t)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) w[t][i] = z[t][i >> 2][i & 3];
+    const bool edge = kStep * s + kStep - 1 > low;
+    uint32_t spoilt = 0;  // bit i: a value of token i is not a number
+    if (edge) {
+      const int n = e.length < most ? e.length : most + 1;  // keys there are
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int key = kStep * s + (i >> 2) * 16 + kg * 4 + (i & 3);
+        // what lies behind the sequence may be anything, and a NaN among the values may not meet the zero weights of rows that do not see it
+        uint32_t nan = 0;
+#pragma unroll
+        for (int g = 0; g < N; ++g) {
+          const int at = (i & 3) * N + g, sh = 8 * (at & 3);
+          nan |= (x[i >> 2].vs.w[at >> 2] >> sh & 255u) == 255u;
+        }
+        const bool gone = key >= n;
+        spoilt |= gone ? 0u : nan << i;
+        if (gone || nan) {
+#pragma unroll
+          for (int g = 0; g < N; ++g) {
+            const int at = (i & 3) * N + g, sh = 8 * (at & 3);
+            uint32_t& word = x[i >> 2].vs.w[at >> 2];
+            word = (word & ~(255u << sh)) | 127u << sh;
+          }
+        }
+#pragma unroll
+        for (int t = 0; t < QT; ++t) w[t][i] = key <= lim[t] ? w[t][i] : -INFINITY;
+      }
+    }
+    bool past = false;
+    float top[QT];
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+      top[t] = fmaxf(fmaxf(fmaxf(w[t][0], w[t][1]), fmaxf(w[t][2], w[t][3])), fmaxf(fmaxf(w[t][4], w[t][5]), fmaxf(w[t][6], w[t][7])));
+      past |= top[t] * weight.c > m[t] * weight.c + 8.f;
+    }
+    if (__builtin_amdgcn_ballot_w64(past)) {
+#pragma unroll
+      for (int t = 0; t < QT; ++t) {
+        const float to = fmaxf(m[t], across_rows_max(top[t]));
+        const float f = weight.from(m[t], to);
+        m[t] = to;
+        l[t] *= f;
+#pragma unroll
+        for (int j = 0; j < 2 * N; ++j) o[t][j] *= f;
+      }
+    }
+    bf16x8 p[QT][WP];
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+      const float under = weight.under(m[t]);
+      float f[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) f[i] = weight(w[t][i], under);
+      if (edge && spoilt) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = (spoilt >> i & 1) && w[t][i] != -INFINITY ? __builtin_nanf("") : f[i];
+      }
+      parts<WP>(f, p[t]);
+    }
+#pragma unroll
+    for (int k = 0; k < WP; ++k)
+#pragma unroll
+      for (int t = 0; t < QT; ++t) l[t] = mfma(ones, p[t][k], l[t]);
+#pragma unroll
+    for (int g = 0; g < N; ++g) {
+      bf16x8 lo, hi;
+      values<D>(x[0], x[1], g, lo, hi);
+#pragma unroll
+      for (int k = 0; k < WP; ++k)
+#pragma unroll
+        for (int t = 0; t < QT; ++t) {
+          o[t][2 * g] = mfma(lo, p[t][k], o[t][2 * g]);
+          o[t][2 * g + 1] = mfma(hi, p[t][k], o[t][2 * g + 1]);
+        }
+    }
+  };
+
+  if (s0 < s1) {
+    Tile<D> now[2], next[2];
+    load(now, s0, pages(s0));
+    Pages p = pages(s0 + stride < s1 ? s0 + stride : s0);
+    for (int s = s0; s < s1; s += stride) {
+      // the last round loads what it has again: loads under a condition would be waited for
+      const int s2 = s + stride < s1 ? s + stride : s, s3 = s2 + stride < s1 ? s2 + stride : s2;
+      load(next, s2, p);
+      p = pages(s3);
+      compute(now, s);
+      now[0] = next[0];
+      now[1] = next[1];
+    }
+  }
+
+  if constexpr (SPLIT) {
+    float* so = shared;                               // [waves][ROWS][PITCH]
+    float* sm = shared + kWaves * ROWS * PITCH;       // [waves][ROWS] maxima, then sums
+    float* sl = sm + kWaves * ROWS;
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+      const int row = wave * ROWS + 16 * t + r;
+#pragma unroll
+      for (int j = 0; j < 2 * N; ++j) *reinterpret_cast<floatx4*>(so + row * PITCH + 16 * j + 4 * kg) = o[t][j];
+      if (kg == 0) { sm[row] = m[t]; sl[row] = l[t][0]; }
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < rows * (D / 8); i += kThreads) {
+      const int row = i / (D / 8), c = (i - row * (D / 8)) * 8;
+      float to = -INFINITY, sum = 0.f, y[8] = {};
+#pragma unroll
+      for (int k = 0; k < kWaves; ++k) to = fmaxf(to, sm[k * ROWS + row]);
+#pragma unroll
+      for (int k = 0; k < kWaves; ++k) {
+        const float mk = sm[k * ROWS + row], f = weight.from(mk, to);
+        sum = fmaf(f, sl[k * ROWS + row], sum);
+        Vec<8> v;
+        v.load(so + (k * ROWS + row) * PITCH + c);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) y[j] = fmaf(f, v.e[j], y[j]);
+      }
+      if (count == 1) {
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) y[j] *= inv;
+        const int tok = (row0 + row) / a.group;
+        put<IO, FP8>(a, e.first + tok, (h * a.group + row0 + row - tok * a.group) * D + c, y);
+      } else {
+        float* slot = a.work + (size_t)blockIdx.x * (ROWS * (D + 2));
+        st_elem4(slot + row * D + c, y[0], y[1], y[2], y[3]);
+        st_elem4(slot + row * D + c + 4, y[4], y[5], y[6], y[7]);
+        if (c == 0) {
+          slot[ROWS * D + row] = to;
+          slot[ROWS * D + ROWS + row] = sum;
+        }
+      }
+    }
+  } else {
+    float* so = shared + wave * 16 * PITCH;  // a tile of this wave's
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+      const float inv = l[t][0] == 0.f ? 0.f : 1.f / l[t][0];
+#pragma unroll
+      for (int j = 0; j < 2 * N; ++j) *reinterpret_cast<floatx4*>(so + r * PITCH + 16 * j + 4 * kg) = o[t][j] * inv;
+      wave_lds_sync();
+      const int left = rows - 16 * t < 16 ? rows - 16 * t : 16;
+      for (int i = lane; i < left * (D / 8); i += 64) {
+        const int row = i / (D / 8), c = (i - row * (D / 8)) * 8;
+        Vec<8> v;
+        v.load(so + row * PITCH + c);
+        const int at_row = row0 + 16 * t + row, tok = at_row / a.group;
+        put<IO, FP8>(a, e.first + tok, (h * a.group + at_row - tok * a.group) * D + c, v.e);
+      }
+      wave_lds_sync();
+    }
+  }
+}
+
+// Joins the pieces of a split sequence: a workgroup has one head of one token (two heads where they
+// share a block of 128 columns), its groups of lanes take the pieces in turn.
+template <typename IO, int D, int QT, bool FP8> __global__ __launch_bounds__(kThreads) void join_kernel(AttentionArgs a) {
+  constexpr int ROWS = 16 * QT, HEADS = FP8 && D == 64 ? 2 : 1, LANES = HEADS * D / 8, GROUPS = kThreads / LANES;
+  __shared__ float so[GROUPS][LANES * 8], sm[GROUPS][HEADS], sl[GROUPS][HEADS];
+  const int per = a.H / HEADS, t = blockIdx.x / per, head = (blockIdx.x - t * per) * HEADS;
+  const int b = a.tok.seq.of(t);
+  const Extent e = extent<ROWS>(a, b);
+  if (t < e.first || t >= e.first + e.n) return;
+  const int chunk = chunk_steps<ROWS>(a), count = pieces(e, chunk);
+  if (count == 1) return;
+  const int base = units_before<ROWS>(a, chunk, b), G = a.cache.heads, h = head / a.group;
+  const int group = threadIdx.x / LANES, lane = threadIdx.x - group * LANES, c = lane * 8 % D, mine = lane * 8 / D;
+  const int row = (t - e.first) * a.group + head + mine - h * a.group, tile = row / ROWS, in = row - tile * ROWS;
+  const Weight<sizeof(IO) == 4 || FP8> weight(a.scale);
+  float to = -INFINITY, sum = 0.f, y[8] = {};
+  if (group < GROUPS) {
+    for (int k = group; k < count && base + tile * count + k < a.units; k += GROUPS) {
+      const float* slot = a.work + ((size_t)(base + tile * count + k) * G + h) * (ROWS * (D + 2));
+      const float mk = slot[ROWS * D + in], lk = slot[ROWS * D + ROWS + in];
+      Vec<8> v;
+      v.load(slot + in * D + c);
+      const float next = fmaxf(to, mk);
+      const float f = weight.from(to, next), g = weight.from(mk, next);
+      to = next;
+      sum = fmaf(sum, f, lk * g);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) y[j] = fmaf(y[j], f, v.e[j] * g);
+    }
+    float4* dst = reinterpret_cast<float4*>(&so[group][lane * 8]);
+    dst[0] = make_float4(y[0], y[1], y[2], y[3]);
+    dst[1] = make_float4(y[4], y[5], y[6], y[7]);
+    if (c == 0) { sm[group][mine] = to; sl[group][mine] = sum; }
+  }
+  __syncthreads();
+  if (group == 0) {
+    const int groups = count < GROUPS ? count : GROUPS;
+    to = -INFINITY;
+    for (int k = 0; k < groups; ++k) to = fmaxf(to, sm[k][mine]);
+    sum = 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) y[j] = 0.f;
+    for (int k = 0; k < groups; ++k) {
+      const float g = weight.from(sm[k][mine], to);
+      sum = fmaf(g, sl[k][mine], sum);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) y[j] = fmaf(g, so[k][lane * 8 + j], y[j]);
+    }
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) y[j] *= inv;
+    put<IO, FP8>(a, t, (head + mine) * D + c, y);
+  }
+}
+
+// ---- the host's side
+
+// Tiles of `rows` rows that a call has at most, whatever its offsets are.
+int64_t most_tiles(int batch, int tokens, int group, int rows) {
+  const int64_t whole = (int64_t)tokens * group / rows + batch, apart = (int64_t)tokens * ((group + rows - 1) / rows);
+  return whole < apart ? whole : apart;
+}
+// Splits keys: tiles of query rows too few to fill the chip, 256 rows a workgroup.
+bool splits(int batch, int tokens, int group, int G) { return ((int64_t)tokens * group / 256 + batch / 4) * G < 256; }
+int split_tiles(int batch, int tokens, int group) { return (int64_t)tokens * group <= (int64_t)16 * batch ? 1 : 2; }
+// Tiles of rows a wave can hold: the queries, the sums and two steps of the cache have to fit 512 registers.
+constexpr int most_tiles_held(size_t io, int D) { return io == 4 ? (D > 128 ? 1 : 2) : D > 128 ? 2 : 4; }
+// Pieces there can be at most.
+int64_t most_units(int batch, int tokens, int group, int G, int QT) { return (kShare + G - 1) / G + most_tiles(batch, tokens, group, 16 * QT); }
+// Whether a sequence can be more than one piece.
+bool joins(int columns, int page) { return (int64_t)columns * page > kLeast * kStep; }
+
+template <typename IO, int D, bool FP8> int launch(const AttentionArgs& a, hipStream_t s) {
+  const int batch = a.tok.seq.batch, tokens = a.tok.seq.tokens, G = a.cache.heads;
+  if (splits(batch, tokens, a.group, G)) {
+    auto run = [&](auto qt) {
+      constexpr int QT = decltype(qt)::value;
+      const int64_t units = most_units(batch, tokens, a.group, G, QT), workgroups = units * G;
+      const int64_t rows = (int64_t)tokens * a.H / (FP8 && D == 64 ? 2 : 1);
+      const bool join = joins(a.tok.columns, 16 << a.cache.shift);
+      if (!fits(workgroups, kThreads) || (join && !fits(rows, kThreads))) return -3;
+      AttentionArgs b = a;
+      b.units = (int)units;
+      hipLaunchKernelGGL((attention_kernel<IO, D, QT, true, FP8>), dim3((unsigned)workgroups), dim3(kThreads), 0, s, b);
+      if (join && taken()) hipLaunchKernelGGL((join_kernel<IO, D, QT, FP8>), dim3((unsigned)rows), dim3(kThreads), 0, s, b);
+      return 0;
+    };
+    if constexpr (most_tiles_held(sizeof(IO), D) > 1)
+      if (split_tiles(batch, tokens, a.group) == 2) return run(std::integral_constant<int, 2>{});
+    return run(std::integral_constant<int, 1>{});
+  }
+  constexpr int QT = most_tiles_held(sizeof(IO), D);
+  const int64_t workgroups = most_tiles(batch, tokens, a.group, 16 * QT * kWaves) * G;
+  if (!fits(workgroups, kThreads)) return -3;
+  hipLaunchKernelGGL((attention_kernel<IO, D, QT, false, FP8>), dim3((unsigned)workgroups), dim3(kThreads), 0, s, a);
+  return 0;
+}
+
+template <typename IO, int D> int launch(const AttentionArgs& a, bool fp8, hipStream_t s) {
+  if constexpr (D == 96 || D == 192) {
+    return fp8 ? -2 : launch<IO, D, false>(a, s);
+  } else {
+    return fp8 ? launch<IO, D, true>(a, s) : launch<IO, D, false>(a, s);
+  }
+}
+
+template <int D> int launch(const AttentionArgs& a, int io, bool fp8, hipStream_t s) {
+  return io == 0 ? launch<float, D>(a, fp8, s) : launch<bf16_t, D>(a, fp8, s);
+}
+
+}  // namespace
+
+int run_attention(const AttentionArgs& a, int D, int io, bool fp8, void* stream) {
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  switch (D) {
+    case 64: return launch<64>(a, io, fp8, s);
+    case 96: return launch<96>(a, io, fp8, s);
+    case 128: return launch<128>(a, io, fp8, s);
+    case 192: return launch<192>(a, io, fp8, s);
+    case 256: return launch<256>(a, io, fp8, s);
+  }
+  return -2;
+}
+
+size_t attention_workspace(int batch, int tokens, int H, int G, int D, int columns, int page) {
+  const int group = H / G;
+  if (!splits(batch, tokens, group, G) || !joins(columns, page)) return 0;
+  const int QT = split_tiles(batch, tokens, group);  // of one tile a wave (wide heads in fp32) there are more, each half as large
+  return (size_t)most_units(batch, tokens, group, G, QT) * G * (16 * QT) * (D + 2) * 4;
+}
+
+}  // namespace skssm

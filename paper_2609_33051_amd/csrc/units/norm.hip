@@ -11,16 +11,6 @@ namespace skssm {
 
 enum NormForm { PLAIN = 0, RESIDUAL = 1, GATED = 2, GATED_SKIP = 3 };
 
-// Largest of a row's 16 values, by their bits: magnitudes order as integers, NaN above all.
-__device__ __forceinline__ uint32_t row_max16(uint32_t x) {
-  auto step = [](uint32_t v, uint32_t w) { return v > w ? v : w; };
-  x = step(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0xB1, 0xF, 0xF, true));
-  x = step(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x4E, 0xF, 0xF, true));
-  x = step(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x141, 0xF, 0xF, true));
-  x = step(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x140, 0xF, 0xF, true));
-  return x;
-}
-
 template <typename TX, typename IO, bool FP8, int FORM, int THREADS, int NV>
 __global__ __launch_bounds__(THREADS) void norm_kernel(NormArgs a) {
   const int groups = a.columns / a.group, row = blockIdx.x / groups, g = blockIdx.x - row * groups, tid = threadIdx.x;

@@ -2,7 +2,9 @@
 tensors (include/sketchssm_mixer.h through `binding`): the short causal
 convolution and the selective scan of packed prompts, one token of every
 request into the decode path's replay buffer, root-mean-square norms that end
-in 8 bits, and products of 8-bit matrices.
+in 8 bits, and products of 8-bit matrices.  And those of a softmax attention
+layer between mixer layers (include/sketchssm_attention.h): rotary positions,
+a paged cache of keys and values in 4 bits, attention over it.
 
 torch supplies device memory and the current stream; every computation is a
 call into libsketchssm.so.  Tensors are on the current device; matrices are
@@ -292,3 +294,191 @@ def matmul_fp8(a: Tensor, a_scale: Tensor, w: Tensor, w_scale: Tensor, *, out_dt
     if rc:
         B._check(rc)
     return out
+
+
+# ---- the softmax attention layer's operators
+
+
+def _heads(name: str, x: Tensor, shape: tuple, dtype, dev: int) -> tuple[int, int]:
+    """(token stride, head stride) of an array [T][heads][dim] whose channels are contiguous."""
+    if x.shape != shape or x.dtype is not dtype or x.get_device() != dev:
+        raise ValueError(f"{name}: a {dtype} tensor {list(shape)} on cuda:{dev} is needed, not {_said(x)}")
+    T, H, D = shape
+    t, h, c = x.stride()
+    if c != 1 or H > 1 and h < D:
+        raise ValueError(f"{name}: its heads are not contiguous or overlap ({_said(x)})")
+    if H == 1:
+        h = -(-D // 16) * 16  # one head: any stride
+    row = (H - 1) * h + D
+    if T > 1 and t < row:
+        raise ValueError(f"{name}: its rows overlap ({_said(x)})")
+    return (t if T > 1 else -(-row // 16) * 16), h
+
+
+def _rotation(angles: Tensor, positions: Tensor | None, interleaved: bool, tokens: int, dev: int) -> B.Rotation:
+    if angles.dim() != 2:
+        raise ValueError("rotation [places][rotated] is needed")
+    return B.Rotation(_flat("rotation", angles, angles.shape, _F32, dev), _flat("positions", positions, (tokens,), torch.int32, dev),
+                      angles.shape[0], angles.shape[1], 1 if interleaved else 0)
+
+
+def rotary(x: Tensor, rotation: Tensor, positions: Tensor | None = None, *, interleaved: bool = False, out: Tensor | None = None) -> Tensor:
+    """x [T][heads][dim] io with the leading channels of every head rotated in
+    pairs: (i, i + R / 2), or (2 i, 2 i + 1) if interleaved.  rotation
+    [places][R] holds each place's cosines and then its sines
+    (`attention.rotary_angles` makes one); positions [T] int32 names each
+    token's row (None: row t).  A position outside the table turns into NaN.
+    `out` may be x."""
+    dev = _device(x)
+    io = _io(x)
+    if x.dim() != 3:
+        raise ValueError("x [T][heads][dim] is needed")
+    T, H, D = x.shape
+    if out is None:
+        out = x.new_empty((T, H, D))
+    rc = (B._lib or B.load()).sketchssm_rotary(io, T, H, D, _rotation(rotation, positions, interleaved, T, dev), x.data_ptr(),
+                                               *_heads("x", x, x.shape, x.dtype, dev), out.data_ptr(), *_heads("out", out, x.shape, x.dtype, dev),
+                                               _stream(dev))
+    if rc:
+        B._check(rc)
+    return out
+
+
+def new_cache(pages: int, kv_heads: int, page: int, dim: int, device="cuda") -> Tensor:
+    """An empty cache of keys and values in 4 bits: [pages][kv_heads][page / 16][17 dim] bytes
+    (records of 16 tokens of a head, as include/sketchssm_attention.h lays them out)."""
+    if not (B._lib or B.load()).sketchssm_cache_bytes(B.Cache(None, pages, kv_heads, page, dim)):
+        raise B.SketchSSMError(-2, B.sketchssm_last_error())
+    return torch.zeros((pages, kv_heads, page // 16, 17 * dim), dtype=torch.uint8, device=device)
+
+
+def _cache(cache: Tensor, dev: int) -> B.Cache:
+    if cache.dim() != 4 or cache.shape[3] % 17:
+        raise ValueError(f"cache: [pages][kv_heads][page / 16][17 dim] bytes are needed, not {_said(cache)}")
+    P, G, n, D = cache.shape
+    return B.Cache(_flat("cache", cache, cache.shape, torch.uint8, dev), P, G, 16 * n, D // 17)
+
+
+def _tokens(table: Tensor, lengths: Tensor, tokens: int, offsets: Tensor | None, dev: int) -> B.NewTokens:
+    n, off = _offsets(offsets, lengths.numel(), dev)
+    if table.dim() != 2 or table.dtype is not torch.int32 or table.get_device() != dev or table.shape[0] != n or table.stride(1) != 1 and table.shape[1] > 1:
+        raise ValueError(f"table: an int32 tensor [{n}][columns] with contiguous rows on cuda:{dev} is needed, not {_said(table)}")
+    return B.NewTokens(tokens, off, _flat("lengths", lengths, (n,), torch.int32, dev), table.data_ptr(),
+                       table.stride(0) if n > 1 else table.shape[1], n, table.shape[1])
+
+
+def cache_append(cache: Tensor, table: Tensor, lengths: Tensor, k: Tensor, v: Tensor, *, offsets: Tensor | None = None,
+                 rotation: Tensor | None = None, positions: Tensor | None = None, interleaved: bool = False, q: Tensor | None = None,
+                 q_out: Tensor | None = None) -> Tensor | None:
+    """The new tokens' keys and values k, v [T][kv_heads][dim] io into the
+    cache, in 4 bits; keys are rotated first (`rotation`, as in `rotary`; by
+    their place in the sequence unless `positions` names rows), and so are the
+    queries q [T][heads][dim] where given: q_out (a new tensor; it may be q).
+
+    Sequence b's new tokens are rows offsets[b] .. offsets[b+1]-1 (None: T /
+    batch each), its lengths[b] tokens end with them, and its places page j ..
+    page (j + 1) - 1 are in page table[b][j] of the cache.  lengths, table and
+    offsets are int32.  A token whose place is below 0 (lengths[b] less than
+    its new tokens) is a padding row and not appended; one whose page is not
+    in the cache is not written.  Sequences may not share a page that is written."""
+    dev = _device(k)
+    io = _io(k)
+    c = _cache(cache, dev)
+    if k.dim() != 3:
+        raise ValueError("k [T][kv_heads][dim] is needed")
+    T, t = k.shape[0], k.dtype
+    shape = (T, c.kv_heads, c.dim)
+    a = B.AppendArgs(io, 0, k.data_ptr(), *_heads("k", k, shape, t, dev), v.data_ptr(), *_heads("v", v, shape, t, dev))
+    if q is not None:
+        if q.dim() != 3:
+            raise ValueError("q [T][heads][dim] is needed")
+        if rotation is None:
+            raise ValueError("q without a rotation")
+        shape = (T, q.shape[1], c.dim)
+        if q_out is None:
+            q_out = q.new_empty(shape)
+        a.heads = q.shape[1]
+        a.q, a.ldq, a.q_head = q.data_ptr(), *_heads("q", q, shape, t, dev)
+        a.q_out, a.ld_qout, a.qout_head = q_out.data_ptr(), *_heads("q_out", q_out, shape, t, dev)
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    rot = None if rotation is None else _rotation(rotation, positions, interleaved, T, dev)
+    if rot is None and positions is not None:
+        raise ValueError("positions without a rotation")
+    rc = (B._lib or B.load()).sketchssm_cache_append(c, _tokens(table, lengths, T, offsets, dev), rot, a, _stream(dev))
+    if rc:
+        B._check(rc)
+    return q_out
+
+
+def cache_read(cache: Tensor, table: Tensor, lengths: Tensor, tokens: int, *, offsets: Tensor | None = None, dtype=torch.bfloat16,
+               k: Tensor | None = None, v: Tensor | None = None) -> tuple[Tensor, Tensor]:
+    """What the cache holds for its sequences' last tokens (`tokens` in all,
+    indexed as in cache_append): (k, v) [tokens][kv_heads][dim], rotated keys and
+    values as the 4 bits stand for them (bfloat16 holds them exactly).  Rows of
+    places below 0 are 0, of pages that are not in the cache NaN."""
+    dev = _device(cache)
+    c = _cache(cache, dev)
+    if dtype not in _IO:
+        raise ValueError(f"{dtype}: bfloat16 or float32 is written")
+    shape = (tokens, c.kv_heads, c.dim)
+    if k is None:
+        k = cache.new_empty(shape, dtype=dtype)
+    if v is None:
+        v = cache.new_empty(shape, dtype=dtype)
+    rc = (B._lib or B.load()).sketchssm_cache_read(c, _tokens(table, lengths, tokens, offsets, dev), _IO[dtype], _flat("k", k, shape, dtype, dev),
+                                                   _flat("v", v, shape, dtype, dev), _stream(dev))
+    if rc:
+        B._check(rc)
+    return k, v
+
+
+def attention(cache: Tensor, table: Tensor, lengths: Tensor, q: Tensor, *, offsets: Tensor | None = None, scale: float | None = None,
+              out: Tensor | None = None, out_dtype=None, scales: Tensor | None = None,
+              workspace: Tensor | None = None) -> tuple[Tensor, Tensor | None]:
+    """Causal softmax attention of the new tokens' queries q [T][heads][dim] io
+    over their sequences in the cache (tokens, table and lengths as in
+    cache_append, which comes first): (out [T][heads][dim], scales).  heads /
+    kv_heads consecutive heads share a key head; scale is dim^-1/2 unless given.
+    out_dtype None: the io type; F8: blocks of 128 columns over their scale,
+    scales [heads dim / 128][T] (what matmul_fp8 reads).  Padding rows are 0."""
+    dev = _device(q)
+    io = _io(q)
+    c = _cache(cache, dev)
+    if q.dim() != 3:
+        raise ValueError("q [T][heads][dim] is needed")
+    T, H, D = q.shape
+    if D != c.dim:
+        raise ValueError(f"q has heads of {D} channels, the cache of {c.dim}")
+    if out_dtype is None:
+        out_dtype = q.dtype
+    f8 = out_dtype is F8
+    a = B.AttentionArgs(io, B.E4M3 if f8 else _IO.get(out_dtype, -1), H, D ** -0.5 if scale is None else scale, q.data_ptr(),
+                        *_heads("q", q, q.shape, q.dtype, dev))
+    if out is None:
+        out, a.ld_out = q.new_empty((T, H, D), dtype=out_dtype), H * D
+    else:
+        a.ld_out, head = _heads("out", out, q.shape, out_dtype, dev)
+        if head != D and H > 1:
+            raise ValueError(f"out: its heads are not contiguous ({_said(out)})")
+    a.out = out.data_ptr()
+    if f8:
+        if H * D % 128:
+            raise ValueError(f"{H} heads of {D} channels are not whole blocks of 128")
+        if scales is None:
+            scales, a.ld_scales = q.new_empty((H * D // 128, T), dtype=_F32), T
+        else:
+            a.ld_scales = _rows("scales", scales, H * D // 128, T, dev)
+        a.scales = scales.data_ptr()
+    elif scales is not None:
+        raise ValueError("scales without an 8-bit output")
+    lib = B._lib or B.load()
+    tok = _tokens(table, lengths, T, offsets, dev)
+    need = lib.sketchssm_attention_workspace(c, H, tok.batch, T, tok.columns)
+    if workspace is None and need:
+        workspace = q.new_empty(need, dtype=torch.uint8)
+    a.workspace, a.workspace_bytes = _space(workspace, dev)
+    rc = lib.sketchssm_attention(c, tok, a, _stream(dev))
+    if rc:
+        B._check(rc)
+    return out, scales
