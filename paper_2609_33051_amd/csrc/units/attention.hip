@@ -19,14 +19,19 @@ namespace skssm {
 
 namespace {
 
+#define INLINE __attribute__((always_inline))
+
 constexpr int kWaves = 4, kThreads = 64 * kWaves;
 constexpr int kStep = 32;         // keys a step
+constexpr float kMost = 65536.f;  // sum of weights from which on the maximum is taken again
 constexpr int kShare = 1024;      // workgroups that a split is made for: four a CU
 constexpr int kLeast = kWaves;    // steps a workgroup takes at least: one a wave
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 __device__ __forceinline__ floatx4 mfma(bf16x8 a, bf16x8 b, floatx4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
 // N consecutive words of a record, 4-byte aligned at least (8 where N is even).
 template <int N> struct Words {
@@ -73,15 +78,17 @@ template <int D> struct Tile {
   static constexpr int N = D / 32;
   Words<N> k, v, vs;
   uint32_t ks[2];  // exponents of the key's blocks that the channels lie in
-  __device__ __forceinline__ void load(const uint8_t* rec, int lane, uint32_t bad) {
+  __device__ __forceinline__ void load_keys(const uint8_t* rec, int lane, uint32_t bad) {
     const int r = lane & 15, a = lane >> 4;
     k.load(rec + r * (D / 2) + a * (D / 8));
-    v.load(rec + 8 * D + lane * (D / 8));
-    vs.load(rec + 16 * D + D / 2 + a * (D / 8));
     const uint8_t* e = rec + 16 * D + r * N;
     const int g = a * (D / 4) / 32;
     ks[0] = e[g] | bad;
     if constexpr (D != 64 && D != 128) ks[1] = e[g + 1 < N ? g + 1 : g] | bad;
+  }
+  __device__ __forceinline__ void load_values(const uint8_t* rec, int lane) {
+    v.load(rec + 8 * D + lane * (D / 8));
+    vs.load(rec + 16 * D + D / 2 + (lane >> 4) * (D / 8));
   }
   // The key's 8 channels a D/4 + 8 j ..
   __device__ __forceinline__ bf16x8 key(int j, int lane) const {
@@ -272,11 +279,17 @@ template <typename IO, bool FP8> __device__ __forceinline__ void put(const Atten
 
 // ---- the kernel
 
+// Tiles of rows that a wave takes at most, and waves a SIMD that its registers are held to.
+constexpr int most_tiles_held(size_t io, int D, bool split) {
+  return io == 4 ? (D > 96 ? 1 : 2) : D == 256 || (split && D == 192) ? 1 : 2;
+}
+constexpr int waves_held(size_t io, int D) { return io == 4 && D == 256 ? 1 : 2; }
+
 // SPLIT: the workgroup's waves share the keys of one piece of a sequence for one tile of rows; its rows are
 // written where the sequence is one piece, else left in `work` for join_kernel.  Otherwise each wave has
 // a tile of rows of its own and all their keys.
 template <typename IO, int D, int QT, bool SPLIT, bool FP8>
-__global__ __launch_bounds__(kThreads) void attention_kernel(AttentionArgs a) {
+__global__ __launch_bounds__(kThreads, waves_held(sizeof(IO), D)) void attention_kernel(AttentionArgs a) {
   // bf16 parts of a query and of a weight: what an fp32 result (the scales of an 8-bit output among them) has to keep
   constexpr int N = D / 32, ROWS = 16 * QT, QP = sizeof(IO) == 2 ? 1 : 3, WP = FP8 ? 3 : QP, PITCH = D + 4;
   __shared__ float shared[SPLIT ? kWaves * ROWS * PITCH + 2 * kWaves * ROWS : kWaves * 16 * PITCH];
@@ -291,14 +304,22 @@ __global__ __launch_bounds__(kThreads) void attention_kernel(AttentionArgs a) {
   } else {
     if (!find<ROWS * kWaves>(a, chunk, u, b, at)) return;
   }
-  const Extent e = extent<ROWS>(a, b);
+  b = uniform(b);
+  at = uniform(at);
+  chunk = uniform(chunk);
+  Extent e = extent<ROWS>(a, b);
+  e.first = uniform(e.first);
+  e.n = uniform(e.n);
+  e.length = uniform(e.length);
+  e.tiles = uniform(e.tiles);
+  e.steps = uniform(e.steps);
   const int count = SPLIT ? pieces(e, chunk) : 1;
   // the last rows see the most keys: they go first
   const int tile = SPLIT ? at / count : ((e.tiles + kWaves - 1) / kWaves - 1 - at) * kWaves + wave, piece = SPLIT ? at - tile * count : 0;
   const int row0 = tile * ROWS, rows = e.n * a.group - row0 < ROWS ? e.n * a.group - row0 : ROWS;
   if (!SPLIT && rows <= 0) return;
   const int most = a.tok.columns << (a.cache.shift + 4);
-  auto limit = [&](int row) {  // the last key that a row sees
+  auto limit = [&](int row) INLINE {  // the last key that a row sees
     const int place = e.length - e.n + row / a.group;
     return place < most ? place : most;
   };
@@ -348,19 +369,33 @@ __global__ __launch_bounds__(kThreads) void attention_kernel(AttentionArgs a) {
   const int s0 = (int)begin + (SPLIT ? wave : 0);
 
   struct Pages { int p0, p1; };
-  auto pages = [&](int s) {
+  auto pages = [&](int s) INLINE {
     Pages p;
     p.p0 = a.tok.page(a.cache, b, 2 * s);
     p.p1 = kStep * s + 16 <= high ? a.tok.page(a.cache, b, 2 * s + 1) : -2;  // -2: no row sees it
     return p;
   };
-  auto load = [&](Tile<D> (&x)[2], int s, const Pages& p) {
-    const uint8_t* r0 = record<D>(a.cache, p.p0 < 0 ? 0 : p.p0, h, 2 * s);
-    const uint8_t* r1 = p.p1 == -2 ? r0 : record<D>(a.cache, p.p1 < 0 ? 0 : p.p1, h, 2 * s + 1);
-    x[0].load(r0, lane, p.p0 < 0 ? 255u : 0u);
-    x[1].load(r1, lane, p.p1 == -1 ? 255u : 0u);
+  struct Records { const uint8_t *r0, *r1; uint32_t b0, b1; };
+  auto records = [&](int s, const Pages& p) INLINE {
+    Records x;
+    x.r0 = record<D>(a.cache, p.p0 < 0 ? 0 : p.p0, h, 2 * s);
+    x.r1 = p.p1 == -2 ? x.r0 : record<D>(a.cache, p.p1 < 0 ? 0 : p.p1, h, 2 * s + 1);
+    x.b0 = p.p0 < 0 ? 255u : 0u;
+    x.b1 = p.p1 == -1 ? 255u : 0u;
+    return x;
   };
-  auto compute = [&](Tile<D> (&x)[2], int s) {
+  auto load_keys = [&](Tile<D> (&x)[2], const Records& r) INLINE {
+    x[0].load_keys(r.r0, lane, r.b0);
+    x[1].load_keys(r.r1, lane, r.b1);
+  };
+  auto load_values = [&](Tile<D> (&x)[2], const Records& r) INLINE {
+    x[0].load_values(r.r0, lane);
+    x[1].load_values(r.r1, lane);
+  };
+  // EDGE: some row does not see all of the step's keys
+  // keys_used, values_used: called once the step's registers are free
+  auto compute = [&](Tile<D> (&x)[2], int s, auto at_edge, auto keys_used, auto values_used) INLINE {
+    constexpr bool EDGE = decltype(at_edge)::value;
     floatx4 z[QT][2];
 #pragma unroll
     for (int t = 0; t < QT; ++t) z[t][0] = z[t][1] = floatx4{0.f, 0.f, 0.f, 0.f};
@@ -374,14 +409,14 @@ __global__ __launch_bounds__(kThreads) void attention_kernel(AttentionArgs a) {
 #pragma unroll
           for (int t = 0; t < QT; ++t) z[t][i] = mfma(k, q[t][j][p], z[t][i]);
       }
+    keys_used();
     float w[QT][8];
 #pragma unroll
     for (int t = 0; t < QT; ++t)
 #pragma unroll
       for (int i = 0; i < 8; ++i) w[t][i] = z[t][i >> 2][i & 3];
-    const bool edge = kStep * s + kStep - 1 > low;
     uint32_t spoilt = 0;  // bit i: a value of token i is not a number
-    if (edge) {
+    if constexpr (EDGE) {
       const int n = e.length < most ? e.length : most + 1;  // keys there are
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
@@ -407,41 +442,46 @@ __global__ __launch_bounds__(kThreads) void attention_kernel(AttentionArgs a) {
         for (int t = 0; t < QT; ++t) w[t][i] = key <= lim[t] ? w[t][i] : -INFINITY;
       }
     }
-    bool past = false;
-    float top[QT];
-#pragma unroll
-    for (int t = 0; t < QT; ++t) {
-      top[t] = fmaxf(fmaxf(fmaxf(w[t][0], w[t][1]), fmaxf(w[t][2], w[t][3])), fmaxf(fmaxf(w[t][4], w[t][5]), fmaxf(w[t][6], w[t][7])));
-      past |= top[t] * weight.c > m[t] * weight.c + 8.f;
-    }
-    if (__builtin_amdgcn_ballot_w64(past)) {
-#pragma unroll
-      for (int t = 0; t < QT; ++t) {
-        const float to = fmaxf(m[t], across_rows_max(top[t]));
-        const float f = weight.from(m[t], to);
-        m[t] = to;
-        l[t] *= f;
-#pragma unroll
-        for (int j = 0; j < 2 * N; ++j) o[t][j] *= f;
-      }
-    }
     bf16x8 p[QT][WP];
-#pragma unroll
-    for (int t = 0; t < QT; ++t) {
+    auto weigh = [&](int t) INLINE {
       const float under = weight.under(m[t]);
       float f[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) f[i] = weight(w[t][i], under);
-      if (edge && spoilt) {
+      if constexpr (EDGE) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) f[i] = (spoilt >> i & 1) && w[t][i] != -INFINITY ? __builtin_nanf("") : f[i];
       }
       parts<WP>(f, p[t]);
+      floatx4 sum = l[t];
+#pragma unroll
+      for (int k = 0; k < WP; ++k) sum = mfma(ones, p[t][k], sum);
+      return sum;
+    };
+    floatx4 sum[QT];
+    bool fine = s != s0;
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+      sum[t] = weigh(t);
+      fine = fine && sum[t][0] <= kMost;
+    }
+    if (__builtin_amdgcn_ballot_w64(!fine)) {
+#pragma unroll
+      for (int t = 0; t < QT; ++t) {
+        float top = m[t];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) top = fmaxf(top, w[t][i]);
+        top = across_rows_max(top);
+        const float f = weight.from(m[t], top);
+        m[t] = top;
+        l[t] *= f;
+#pragma unroll
+        for (int j = 0; j < 2 * N; ++j) o[t][j] *= f;
+        sum[t] = weigh(t);
+      }
     }
 #pragma unroll
-    for (int k = 0; k < WP; ++k)
-#pragma unroll
-      for (int t = 0; t < QT; ++t) l[t] = mfma(ones, p[t][k], l[t]);
+    for (int t = 0; t < QT; ++t) l[t] = sum[t];
 #pragma unroll
     for (int g = 0; g < N; ++g) {
       bf16x8 lo, hi;
@@ -454,20 +494,57 @@ __global__ __launch_bounds__(kThreads) void attention_kernel(AttentionArgs a) {
           o[t][2 * g + 1] = mfma(hi, p[t][k], o[t][2 * g + 1]);
         }
     }
+    values_used();
   };
 
   if (s0 < s1) {
-    Tile<D> now[2], next[2];
-    load(now, s0, pages(s0));
-    Pages p = pages(s0 + stride < s1 ? s0 + stride : s0);
-    for (int s = s0; s < s1; s += stride) {
-      // the last round loads what it has again: loads under a condition would be waited for
-      const int s2 = s + stride < s1 ? s + stride : s, s3 = s2 + stride < s1 ? s2 + stride : s2;
-      load(next, s2, p);
-      p = pages(s3);
-      compute(now, s);
-      now[0] = next[0];
-      now[1] = next[1];
+    const int whole = low < 0 ? 0 : (low + 1) / kStep, end = whole < s1 ? whole : s1;  // steps that every row sees all of
+    // the last round loads what it has again: loads under a condition would be waited for
+    auto after = [&](int s) INLINE { return s + stride < s1 ? s + stride : s; };
+    Tile<D> now[2];
+    Pages p = pages(s0);
+    Records r = records(s0, p);
+    load_keys(now, r);
+    load_values(now, r);
+    p = pages(after(s0));
+    int s = s0;
+    if constexpr (SPLIT) {
+      // a step ahead in registers of its own: the cache comes from memory
+      Tile<D> next[2];
+      auto one = [&](Tile<D> (&x)[2], Tile<D> (&y)[2], auto at_edge) INLINE {
+        const int s2 = after(s);
+        r = records(s2, p);
+        load_keys(y, r);
+        load_values(y, r);
+        p = pages(after(s2));
+        compute(x, s, at_edge, [] {}, [] {});
+        s += stride;
+      };
+      while (s + stride < end) {  // two steps a round, so that the buffers change places without moves
+        one(now, next, std::false_type{});
+        one(next, now, std::false_type{});
+      }
+      if (s < end) {
+        one(now, next, std::false_type{});
+        now[0] = next[0];
+        now[1] = next[1];
+      }
+      while (s < s1) {
+        one(now, next, std::true_type{});
+        now[0] = next[0];
+        now[1] = next[1];
+      }
+    } else {
+      // keys and values of the next step as soon as the registers are free: the cache comes from L2
+      auto one = [&](auto at_edge) INLINE {
+        const int s2 = after(s);
+        r = records(s2, p);
+        p = pages(after(s2));
+        compute(now, s, at_edge, [&]() INLINE { load_keys(now, r); }, [&]() INLINE { load_values(now, r); });
+        s += stride;
+      };
+      while (s < end) one(std::false_type{});
+      while (s < s1) one(std::true_type{});
     }
   }
 
@@ -599,8 +676,6 @@ int64_t most_tiles(int batch, int tokens, int group, int rows) {
 // Splits keys: tiles of query rows too few to fill the chip, 256 rows a workgroup.
 bool splits(int batch, int tokens, int group, int G) { return ((int64_t)tokens * group / 256 + batch / 4) * G < 256; }
 int split_tiles(int batch, int tokens, int group) { return (int64_t)tokens * group <= (int64_t)16 * batch ? 1 : 2; }
-// Tiles of rows a wave can hold: the queries, the sums and two steps of the cache have to fit 512 registers.
-constexpr int most_tiles_held(size_t io, int D) { return io == 4 ? (D > 128 ? 1 : 2) : D > 128 ? 2 : 4; }
 // Pieces there can be at most.
 int64_t most_units(int batch, int tokens, int group, int G, int QT) { return (kShare + G - 1) / G + most_tiles(batch, tokens, group, 16 * QT); }
 // Whether a sequence can be more than one piece.
@@ -621,11 +696,11 @@ template <typename IO, int D, bool FP8> int launch(const AttentionArgs& a, hipSt
       if (join && taken()) hipLaunchKernelGGL((join_kernel<IO, D, QT, FP8>), dim3((unsigned)rows), dim3(kThreads), 0, s, b);
       return 0;
     };
-    if constexpr (most_tiles_held(sizeof(IO), D) > 1)
+    if constexpr (most_tiles_held(sizeof(IO), D, true) > 1)
       if (split_tiles(batch, tokens, a.group) == 2) return run(std::integral_constant<int, 2>{});
     return run(std::integral_constant<int, 1>{});
   }
-  constexpr int QT = most_tiles_held(sizeof(IO), D);
+  constexpr int QT = most_tiles_held(sizeof(IO), D, false);
   const int64_t workgroups = most_tiles(batch, tokens, a.group, 16 * QT * kWaves) * G;
   if (!fits(workgroups, kThreads)) return -3;
   hipLaunchKernelGGL((attention_kernel<IO, D, QT, false, FP8>), dim3((unsigned)workgroups), dim3(kThreads), 0, s, a);
