@@ -74,8 +74,10 @@ struct AttentionArgs {
   size_t ld_out;
   float* scales;
   size_t ld_scales;
-  float* work;     // [units][key heads]: sums, maxima and sums of weights of a tile's rows
-  int units;
+  float* work;     // [share][key heads][2]: a tile's sums, maxima and sums of weights
+  int64_t* plan;   // at the workspace's start (NULL: no tile can be split)
+  int share;       // workgroups of attention_kernel a key head
+  int span;        // pieces of 8 channels a workgroup of join_kernel
 };
 int run_attention(const AttentionArgs& a, int D, int io, bool fp8, void* stream);
 size_t attention_workspace(int batch, int tokens, int H, int G, int D, int columns, int page);

@@ -24,8 +24,7 @@ namespace {
 constexpr int kWaves = 4, kThreads = 64 * kWaves;
 constexpr int kStep = 32;         // keys a step
 constexpr float kMost = 65536.f;  // sum of weights from which on the maximum is taken again
-constexpr int kShare = 1024;      // workgroups that a split is made for: four a CU
-constexpr int kLeast = kWaves;    // steps a workgroup takes at least: one a wave
+constexpr int kCUs = 256;
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
@@ -33,24 +32,29 @@ __device__ __forceinline__ floatx4 mfma(bf16x8 a, bf16x8 b, floatx4 c) { return 
 
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
+template <bool NT, typename T> __device__ __forceinline__ T read(const T* p) {
+  if constexpr (NT) return __builtin_nontemporal_load(p);
+  else return *p;
+}
+
 // N consecutive words of a record, 4-byte aligned at least (8 where N is even).
 template <int N> struct Words {
   uint32_t w[N];
-  __device__ __forceinline__ void load(const uint8_t* p) {
+  template <bool NT> __device__ __forceinline__ void load(const uint8_t* p) {
     typedef uint32_t w2 __attribute__((ext_vector_type(2), aligned(8)));
     typedef uint32_t w3 __attribute__((ext_vector_type(3), aligned(4)));
     typedef uint32_t w4 __attribute__((ext_vector_type(4), aligned(8)));
     if constexpr (N == 3) {
-      const w3 t = *reinterpret_cast<const w3*>(p);
+      const w3 t = read<NT>(reinterpret_cast<const w3*>(p));
       w[0] = t.x; w[1] = t.y; w[2] = t.z;
     } else {
 #pragma unroll
       for (int i = 0; i + 4 <= N; i += 4) {
-        const w4 t = *reinterpret_cast<const w4*>(p + 4 * i);
+        const w4 t = read<NT>(reinterpret_cast<const w4*>(p + 4 * i));
         w[i] = t.x; w[i + 1] = t.y; w[i + 2] = t.z; w[i + 3] = t.w;
       }
       if constexpr (N % 4 == 2) {
-        const w2 t = *reinterpret_cast<const w2*>(p + 4 * (N - 2));
+        const w2 t = read<NT>(reinterpret_cast<const w2*>(p + 4 * (N - 2)));
         w[N - 2] = t.x; w[N - 1] = t.y;
       }
     }
@@ -74,21 +78,20 @@ __device__ __forceinline__ uint32_t two(uint32_t w, float scale, int byte) {
 
 // One record of 16 tokens as a lane (r = lane % 16, a = lane / 16) takes it: channels a D/4 .. of token r's key,
 // bytes r of every block of the values of tokens 4 a .. 4 a + 3.
-template <int D> struct Tile {
+template <int D, bool NT> struct Tile {
   static constexpr int N = D / 32;
   Words<N> k, v, vs;
   uint32_t ks[2];  // exponents of the key's blocks that the channels lie in
-  __device__ __forceinline__ void load_keys(const uint8_t* rec, int lane, uint32_t bad) {
-    const int r = lane & 15, a = lane >> 4;
-    k.load(rec + r * (D / 2) + a * (D / 8));
-    const uint8_t* e = rec + 16 * D + r * N;
-    const int g = a * (D / 4) / 32;
-    ks[0] = e[g] | bad;
-    if constexpr (D != 64 && D != 128) ks[1] = e[g + 1 < N ? g + 1 : g] | bad;
+  // rec is one address for the wave; unsigned offsets of a lane are added to it by the load itself.
+  __device__ __forceinline__ void load_keys(const uint8_t* rec, uint32_t lane, uint32_t bad) {
+    const uint32_t r = lane & 15, a = lane >> 4, g = a * (D / 4) / 32;
+    k.template load<NT>(rec + (r * (D / 2) + a * (D / 8)));
+    ks[0] = rec[16 * D + r * N + g] | bad;
+    if constexpr (D != 64 && D != 128) ks[1] = rec[16 * D + r * N + (g + 1 < N ? g + 1 : g)] | bad;
   }
-  __device__ __forceinline__ void load_values(const uint8_t* rec, int lane) {
-    v.load(rec + 8 * D + lane * (D / 8));
-    vs.load(rec + 16 * D + D / 2 + (lane >> 4) * (D / 8));
+  __device__ __forceinline__ void load_values(const uint8_t* rec, uint32_t lane) {
+    v.template load<NT>(rec + (8 * D + lane * (D / 8)));
+    vs.template load<NT>(rec + (16 * D + D / 2 + (lane >> 4) * (D / 8)));
   }
   // The key's 8 channels a D/4 + 8 j ..
   __device__ __forceinline__ bf16x8 key(int j, int lane) const {
@@ -105,7 +108,7 @@ template <int D> struct Tile {
 };
 
 // Channels 32 g + r and 32 g + r + 16 of the values of eight tokens, four of each record.
-template <int D> __device__ __forceinline__ void values(const Tile<D>& x, const Tile<D>& y, int g, bf16x8& lo, bf16x8& hi) {
+template <int D, bool NT> __device__ __forceinline__ void values(const Tile<D, NT>& x, const Tile<D, NT>& y, int g, bf16x8& lo, bf16x8& hi) {
   constexpr int N = D / 32;
   uint32_t c[8];
 #pragma unroll
@@ -179,75 +182,83 @@ template <int ROWS> __device__ __forceinline__ Extent extent(const AttentionArgs
   e.n = e.n < 0 ? 0 : e.n;
   const int length = a.tok.lengths[b];
   e.length = length < -(1 << 30) ? -(1 << 30) : length < 1 << 30 ? length : 1 << 30;
-  const int most = (a.tok.columns << (a.cache.shift + 4)) + 1;  // one past the table, which reads as NaN
+  const int most = a.tok.columns << (a.cache.shift + 4);
   const int seen = e.length < 0 ? 0 : e.length < most ? e.length : most;
   e.tiles = (e.n * a.group + ROWS - 1) / ROWS;
   e.steps = (seen + kStep - 1) / kStep;
   return e;
 }
 
-__device__ __forceinline__ int64_t wave_sum64(int64_t x) {
-  for (int d = 1; d < 64; d *= 2) x += __shfl_xor((long long)x, d);
-  return x;
-}
-
-// How a call's rows and keys are shared out where sequences are split: every sequence into pieces of `chunk`
-// steps, so many that all pieces of all heads together are about kShare.
-template <int ROWS> __device__ __forceinline__ int chunk_steps(const AttentionArgs& a) {
+// Where a position among the sequences' weights lies: each thread sums the weights of a run of sequences, and
+// `upto` [kThreads] holds the sums up to and with each run.
+template <typename F> __device__ __forceinline__ int64_t lay_out(int batch, F weight, int64_t* upto) {
+  if (batch == 1) return weight(0);
+  __shared__ int64_t waves[kWaves];
+  const int run = (batch + kThreads - 1) / kThreads, tid = threadIdx.x;
+  int64_t x = 0;
+  for (int b = tid * run; b < (tid + 1) * run && b < batch; ++b) x += weight(b);
+  for (int d = 1; d < 64; d *= 2) {
+    const int64_t y = __shfl_up((long long)x, d);
+    x += (tid & 63) >= d ? y : 0;
+  }
+  if ((tid & 63) == 63) waves[tid >> 6] = x;
+  __syncthreads();
   int64_t total = 0;
-  if (a.tok.seq.batch == 1) {
-    const Extent e = extent<ROWS>(a, 0);
-    total = (int64_t)e.tiles * e.steps;
-  } else {
-    for (int b = threadIdx.x & 63; b < a.tok.seq.batch; b += 64) {
-      const Extent e = extent<ROWS>(a, b);
-      total += (int64_t)e.tiles * e.steps;
-    }
-    total = wave_sum64(total);
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    if (w < tid >> 6) x += waves[w];
+    total += waves[w];
   }
-  const int64_t each = (total * a.cache.heads + kShare - 1) / kShare;
-  const int64_t whole = (each + kWaves - 1) / kWaves * kWaves;
-  return whole < kLeast ? kLeast : (int)(whole < (1 << 26) ? whole : 1 << 26);
+  upto[tid] = x;
+  __syncthreads();
+  return total;
 }
-__device__ __forceinline__ int pieces(const Extent& e, int chunk) { return e.steps <= chunk ? 1 : (e.steps + chunk - 1) / chunk; }
-
-// The sequence that holds unit u, with u's place in it; false where there are fewer.
-template <int ROWS> __device__ __forceinline__ bool find(const AttentionArgs& a, int chunk, int u, int& b, int& at) {
-  const int lane = threadIdx.x & 63;
-  int before = 0;
-  for (int b0 = 0; b0 < a.tok.seq.batch; b0 += 64) {
-    int units = 0;
-    if (b0 + lane < a.tok.seq.batch) {
-      const Extent e = extent<ROWS>(a, b0 + lane);
-      units = e.tiles * pieces(e, chunk);
-    }
-    int upto = units;  // inclusive
-    for (int d = 1; d < 64; d *= 2) {
-      const int x = __shfl_up(upto, d);
-      if (lane >= d) upto += x;
-    }
-    const unsigned long long hit = __builtin_amdgcn_ballot_w64(u < before + upto);
+// The sequence that holds position x of the total, and x's place in it.
+template <typename F> __device__ __forceinline__ int seek(int batch, F weight, const int64_t* upto, int64_t x, int64_t& at) {
+  at = x;
+  if (batch == 1) return 0;
+  const int run = (batch + kThreads - 1) / kThreads;
+  int first = 0;
+  for (int j = 0; j < kWaves; ++j) {
+    const unsigned long long hit = __builtin_amdgcn_ballot_w64(upto[64 * j + (threadIdx.x & 63)] > x);
     if (hit) {
-      const int l = __builtin_ctzll(hit);
-      b = b0 + l;
-      at = u - before - __builtin_amdgcn_readlane(upto - units, l);
-      return true;
+      first = 64 * j + __builtin_ctzll(hit);
+      break;
     }
-    before += __builtin_amdgcn_readlane(upto, 63);
   }
-  return false;
+  if (first) at -= upto[first - 1];
+  int b = first * run;
+  while (b + 1 < batch) {
+    const int64_t w = weight(b);
+    if (at < w) break;
+    at -= w;
+    ++b;
+  }
+  at = (int64_t)uniform((int)(at >> 32)) << 32 | (uint32_t)uniform((int)at);
+  return uniform(b);
 }
 
-// Units of the sequences before b.
-template <int ROWS> __device__ __forceinline__ int units_before(const AttentionArgs& a, int chunk, int b) {
-  int n = 0;
-  for (int i = threadIdx.x & 63; i < b; i += 64) {
-    const Extent e = extent<ROWS>(a, i);
-    n += e.tiles * pieces(e, chunk);
-  }
-  for (int d = 1; d < 64; d *= 2) n += __shfl_xor(n, d);
-  return n;
+// a / b of 0 <= a < 2^52, 0 < b, by way of fp64: a quarter of the instructions of a 64-bit division.
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
+  int64_t q = (int64_t)((double)a * __builtin_amdgcn_rcp((double)b));
+  int64_t r = a - q * b;  // rcp is a few units off: q is within a unit or, of large quotients, some
+  while (r < 0) { r += b; --q; }
+  while (r >= b) { r -= b; ++q; }
+  return q;
 }
+
+// Split sequences.  The steps of a tile of rows are counted in rounds, one step of each wave, one round at least. A key head's rounds of all
+// sequences and tiles lie one after the other and are shared out evenly: workgroup u has rounds u each .. of them,
+// whatever tiles they are of.  A tile that one workgroup has whole is written by it; of others it leaves the sums
+// in one of its two slots, the second where the tile begins behind the workgroup's own first round.
+__device__ __forceinline__ int rounds(const Extent& e) { return e.steps <= kWaves ? 1 : (e.steps + kWaves - 1) / kWaves; }
+template <int ROWS> struct Rounds {
+  const AttentionArgs& a;
+  __device__ __forceinline__ int64_t operator()(int b) const {
+    const Extent e = extent<ROWS>(a, b);
+    return (int64_t)e.tiles * rounds(e);
+  }
+};
 
 // ---- outputs
 
@@ -288,7 +299,7 @@ constexpr int waves_held(size_t io, int D) { return io == 4 && D == 256 ? 1 : 2;
 // SPLIT: the workgroup's waves share the keys of one piece of a sequence for one tile of rows; its rows are
 // written where the sequence is one piece, else left in `work` for join_kernel.  Otherwise each wave has
 // a tile of rows of its own and all their keys.
-template <typename IO, int D, int QT, bool SPLIT, bool FP8>
+template <typename IO, int D, int QT, bool SPLIT, bool FP8, bool NT>
 __global__ __launch_bounds__(kThreads, waves_held(sizeof(IO), D)) void attention_kernel(AttentionArgs a) {
   // bf16 parts of a query and of a weight: what an fp32 result (the scales of an 8-bit output among them) has to keep
   constexpr int N = D / 32, ROWS = 16 * QT, QP = sizeof(IO) == 2 ? 1 : 3, WP = FP8 ? 3 : QP, PITCH = D + 4;
@@ -297,29 +308,50 @@ __global__ __launch_bounds__(kThreads, waves_held(sizeof(IO), D)) void attention
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int G = a.cache.heads, h = blockIdx.x % G, u = blockIdx.x / G;
 
-  int b, at, chunk = 1 << 26;
+  __shared__ int64_t upto[kThreads];
+  const int batch = a.tok.seq.batch;
+  const Rounds<ROWS> weight_of{a};
+  auto blocks_of = [&](int b) INLINE { return (int64_t)extent<ROWS * kWaves>(a, b).tiles; };
+  int64_t x = u, x1 = u + 1, each = 1, place = 0, total;
+  int b;
   if constexpr (SPLIT) {
-    chunk = chunk_steps<ROWS>(a);
-    if (!find<ROWS>(a, chunk, u, b, at)) return;
+    total = lay_out(batch, weight_of, upto);
+    each = quotient(total + a.share - 1, a.share);
+    x = u * each;
+    x1 = x + each < total ? x + each : total;
+    if (a.plan && blockIdx.x == 0) {  // for join_kernel
+      if (threadIdx.x == 0) a.plan[0] = each;
+      const int run = (batch + kThreads - 1) / kThreads;
+      int64_t before = batch == 1 || threadIdx.x == 0 ? 0 : upto[threadIdx.x - 1];
+      for (int i = threadIdx.x * run; i < (int)(threadIdx.x + 1) * run && i < batch; ++i) {
+        a.plan[1 + i] = before;
+        before += weight_of(i);
+      }
+    }
+    if (x >= total) return;
+    b = seek(batch, weight_of, upto, x, place);
   } else {
-    if (!find<ROWS * kWaves>(a, chunk, u, b, at)) return;
+    total = lay_out(batch, blocks_of, upto);
+    if (x >= total) return;
+    b = seek(batch, blocks_of, upto, x, place);
   }
-  b = uniform(b);
-  at = uniform(at);
-  chunk = uniform(chunk);
+  // a tile, or a part of one, after the other
+  for (; x < x1;) {
   Extent e = extent<ROWS>(a, b);
   e.first = uniform(e.first);
   e.n = uniform(e.n);
   e.length = uniform(e.length);
   e.tiles = uniform(e.tiles);
   e.steps = uniform(e.steps);
-  const int count = SPLIT ? pieces(e, chunk) : 1;
+  const int all = rounds(e);
   // the last rows see the most keys: they go first
-  const int tile = SPLIT ? at / count : ((e.tiles + kWaves - 1) / kWaves - 1 - at) * kWaves + wave, piece = SPLIT ? at - tile * count : 0;
+  const int tile = SPLIT ? (int)quotient(place, all) : ((e.tiles + kWaves - 1) / kWaves - 1 - (int)place) * kWaves + wave;
+  const int r0 = SPLIT ? (int)(place - (int64_t)tile * all) : 0, r1 = SPLIT && x1 - x < all - r0 ? r0 + (int)(x1 - x) : all;
+  const bool whole_tile = !SPLIT || (r0 == 0 && r1 == all);
   const int row0 = tile * ROWS, rows = e.n * a.group - row0 < ROWS ? e.n * a.group - row0 : ROWS;
   if (!SPLIT && rows <= 0) return;
   const int most = a.tok.columns << (a.cache.shift + 4);
-  auto limit = [&](int row) INLINE {  // the last key that a row sees
+  auto limit = [&](int row) INLINE {  // the last key that a row sees; of keys past the table one, which reads as NaN
     const int place = e.length - e.n + row / a.group;
     return place < most ? place : most;
   };
@@ -363,38 +395,48 @@ __global__ __launch_bounds__(kThreads, waves_held(sizeof(IO), D)) void attention
   const bf16x8 ones = __builtin_bit_cast(bf16x8, make_uint4(0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u));
 
   const int stride = SPLIT ? kWaves : 1;
-  const int64_t begin = SPLIT ? (int64_t)piece * chunk : 0;
-  const int64_t last = (int64_t)high < 0 ? 0 : high / kStep + 1;
-  const int s1 = (int)(begin + chunk < last ? begin + chunk : last);
-  const int s0 = (int)begin + (SPLIT ? wave : 0);
+  const int last = high < 0 ? 0 : high / kStep + 1;
+  const int s1 = SPLIT && r1 < all && r1 * kWaves < last ? r1 * kWaves : last, s0 = SPLIT ? r0 * kWaves + wave : 0;
 
+  // 64 entries of the sequence's row of the table, one a lane: a step's pages are a lane's value, with no load
+  // between a step and the next one's records.
+  const int32_t* row_of_table = a.tok.table + (size_t)b * a.tok.ld_table;
+  int window = 0, entries = 0;
+  auto look = [&](int j) INLINE {
+    window = j;
+    const int at = j + lane;
+    entries = row_of_table[at < a.tok.columns ? at : a.tok.columns - 1];
+    __builtin_amdgcn_s_waitcnt(0x0F70);  // here, where it is rare, and not at every use
+  };
   struct Pages { int p0, p1; };
   auto pages = [&](int s) INLINE {
-    Pages p;
-    p.p0 = a.tok.page(a.cache, b, 2 * s);
-    p.p1 = kStep * s + 16 <= high ? a.tok.page(a.cache, b, 2 * s + 1) : -2;  // -2: no row sees it
-    return p;
+    const int j0 = 2 * s >> a.cache.shift, j1 = (2 * s + 1) >> a.cache.shift;
+    if (j1 - window >= 64) look(j0);
+    return Pages{__builtin_amdgcn_readlane(entries, j0 - window), __builtin_amdgcn_readlane(entries, j1 - window)};
   };
+  using Two = Tile<D, NT>;
   struct Records { const uint8_t *r0, *r1; uint32_t b0, b1; };
   auto records = [&](int s, const Pages& p) INLINE {
+    auto good = [&](int tile, int page) INLINE { return tile >> a.cache.shift < a.tok.columns && (unsigned)page < (unsigned)a.cache.pages; };
+    const bool g0 = good(2 * s, p.p0), g1 = good(2 * s + 1, p.p1), used = kStep * s + 16 <= high;  // whether a row sees the second record
     Records x;
-    x.r0 = record<D>(a.cache, p.p0 < 0 ? 0 : p.p0, h, 2 * s);
-    x.r1 = p.p1 == -2 ? x.r0 : record<D>(a.cache, p.p1 < 0 ? 0 : p.p1, h, 2 * s + 1);
-    x.b0 = p.p0 < 0 ? 255u : 0u;
-    x.b1 = p.p1 == -1 ? 255u : 0u;
+    x.r0 = record<D>(a.cache, g0 ? p.p0 : 0, h, 2 * s);
+    x.r1 = used ? record<D>(a.cache, g1 ? p.p1 : 0, h, 2 * s + 1) : x.r0;
+    x.b0 = g0 ? 0u : 255u;
+    x.b1 = g1 || !used ? 0u : 255u;
     return x;
   };
-  auto load_keys = [&](Tile<D> (&x)[2], const Records& r) INLINE {
+  auto load_keys = [&](Two (&x)[2], const Records& r) INLINE {
     x[0].load_keys(r.r0, lane, r.b0);
     x[1].load_keys(r.r1, lane, r.b1);
   };
-  auto load_values = [&](Tile<D> (&x)[2], const Records& r) INLINE {
+  auto load_values = [&](Two (&x)[2], const Records& r) INLINE {
     x[0].load_values(r.r0, lane);
     x[1].load_values(r.r1, lane);
   };
   // EDGE: some row does not see all of the step's keys
   // keys_used, values_used: called once the step's registers are free
-  auto compute = [&](Tile<D> (&x)[2], int s, auto at_edge, auto keys_used, auto values_used) INLINE {
+  auto compute = [&](Two (&x)[2], int s, auto at_edge, auto keys_used, auto values_used) INLINE {
     constexpr bool EDGE = decltype(at_edge)::value;
     floatx4 z[QT][2];
 #pragma unroll
@@ -485,7 +527,7 @@ __global__ __launch_bounds__(kThreads, waves_held(sizeof(IO), D)) void attention
 #pragma unroll
     for (int g = 0; g < N; ++g) {
       bf16x8 lo, hi;
-      values<D>(x[0], x[1], g, lo, hi);
+      values(x[0], x[1], g, lo, hi);
 #pragma unroll
       for (int k = 0; k < WP; ++k)
 #pragma unroll
@@ -501,22 +543,20 @@ __global__ __launch_bounds__(kThreads, waves_held(sizeof(IO), D)) void attention
     const int whole = low < 0 ? 0 : (low + 1) / kStep, end = whole < s1 ? whole : s1;  // steps that every row sees all of
     // the last round loads what it has again: loads under a condition would be waited for
     auto after = [&](int s) INLINE { return s + stride < s1 ? s + stride : s; };
-    Tile<D> now[2];
-    Pages p = pages(s0);
-    Records r = records(s0, p);
+    Two now[2];
+    look(2 * s0 >> a.cache.shift);
+    Records r = records(s0, pages(s0));
     load_keys(now, r);
     load_values(now, r);
-    p = pages(after(s0));
     int s = s0;
     if constexpr (SPLIT) {
       // a step ahead in registers of its own: the cache comes from memory
-      Tile<D> next[2];
-      auto one = [&](Tile<D> (&x)[2], Tile<D> (&y)[2], auto at_edge) INLINE {
+      Two next[2];
+      auto one = [&](Two (&x)[2], Two (&y)[2], auto at_edge) INLINE {
         const int s2 = after(s);
-        r = records(s2, p);
+        r = records(s2, pages(s2));
         load_keys(y, r);
         load_values(y, r);
-        p = pages(after(s2));
         compute(x, s, at_edge, [] {}, [] {});
         s += stride;
       };
@@ -538,8 +578,7 @@ __global__ __launch_bounds__(kThreads, waves_held(sizeof(IO), D)) void attention
       // keys and values of the next step as soon as the registers are free: the cache comes from L2
       auto one = [&](auto at_edge) INLINE {
         const int s2 = after(s);
-        r = records(s2, p);
-        p = pages(after(s2));
+        r = records(s2, pages(s2));
         compute(now, s, at_edge, [&]() INLINE { load_keys(now, r); }, [&]() INLINE { load_values(now, r); });
         s += stride;
       };
@@ -574,20 +613,31 @@ __global__ __launch_bounds__(kThreads, waves_held(sizeof(IO), D)) void attention
 #pragma unroll
         for (int j = 0; j < 8; ++j) y[j] = fmaf(f, v.e[j], y[j]);
       }
-      if (count == 1) {
+      if (whole_tile) {
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
         for (int j = 0; j < 8; ++j) y[j] *= inv;
         const int tok = (row0 + row) / a.group;
         put<IO, FP8>(a, e.first + tok, (h * a.group + row0 + row - tok * a.group) * D + c, y);
       } else {
-        float* slot = a.work + (size_t)blockIdx.x * (ROWS * (D + 2));
+        float* slot = a.work + ((size_t)blockIdx.x * 2 + (x == u * each ? 0 : 1)) * (ROWS * (D + 2));
         st_elem4(slot + row * D + c, y[0], y[1], y[2], y[3]);
         st_elem4(slot + row * D + c + 4, y[4], y[5], y[6], y[7]);
         if (c == 0) {
           slot[ROWS * D + row] = to;
           slot[ROWS * D + ROWS + row] = sum;
         }
+      }
+    }
+    x += r1 - r0;
+    place += r1 - r0;
+    if (x < x1) {
+      __syncthreads();  // `shared` is written again
+      while (place >= (int64_t)e.tiles * rounds(e) && b + 1 < batch) {  // the next sequence that has rows
+        e = extent<ROWS>(a, ++b);
+        e.tiles = uniform(e.tiles);
+        e.steps = uniform(e.steps);
+        place = 0;
       }
     }
   } else {
@@ -608,61 +658,72 @@ __global__ __launch_bounds__(kThreads, waves_held(sizeof(IO), D)) void attention
       }
       wave_lds_sync();
     }
+    x = x1;
+  }
   }
 }
 
-// Joins the pieces of a split sequence: a workgroup has one head of one token (two heads where they
-// share a block of 128 columns), its groups of lanes take the pieces in turn.
+// Joins what workgroups left of a tile.  A token's rows of a key head are pieces of 8 channels; a workgroup has `span`
+// (a power of two from 16, a block of 128 columns, to 256) of them, and its groups of lanes take the slots in turn.
 template <typename IO, int D, int QT, bool FP8> __global__ __launch_bounds__(kThreads) void join_kernel(AttentionArgs a) {
-  constexpr int ROWS = 16 * QT, HEADS = FP8 && D == 64 ? 2 : 1, LANES = HEADS * D / 8, GROUPS = kThreads / LANES;
-  __shared__ float so[GROUPS][LANES * 8], sm[GROUPS][HEADS], sl[GROUPS][HEADS];
-  const int per = a.H / HEADS, t = blockIdx.x / per, head = (blockIdx.x - t * per) * HEADS;
-  const int b = a.tok.seq.of(t);
+  constexpr int ROWS = 16 * QT;
+  __shared__ float so[kThreads][8], sm[kThreads], sl[kThreads];
+  const int G = a.cache.heads, spans = (a.group * (D / 8) + a.span - 1) / a.span;
+  const int item = blockIdx.x / spans, t = item / G, h = item - t * G, tid = threadIdx.x;
+  const int64_t each = a.plan[0];
+  const int b = uniform(a.tok.seq.of(t));
+  const int64_t before = a.plan[1 + b];
   const Extent e = extent<ROWS>(a, b);
   if (t < e.first || t >= e.first + e.n) return;
-  const int chunk = chunk_steps<ROWS>(a), count = pieces(e, chunk);
-  if (count == 1) return;
-  const int base = units_before<ROWS>(a, chunk, b), G = a.cache.heads, h = head / a.group;
-  const int group = threadIdx.x / LANES, lane = threadIdx.x - group * LANES, c = lane * 8 % D, mine = lane * 8 / D;
-  const int row = (t - e.first) * a.group + head + mine - h * a.group, tile = row / ROWS, in = row - tile * ROWS;
+  const int all = rounds(e), groups = kThreads / a.span, group = tid / a.span;
+  const int piece = (blockIdx.x - item * spans) * a.span + (tid & (a.span - 1)), g = piece / (D / 8), c = (piece - g * (D / 8)) * 8;
+  const int row = (t - e.first) * a.group + g, tile = row / ROWS, in = row - tile * ROWS;
+  const int64_t i0 = before + (int64_t)tile * all, w0 = quotient(i0, each), w1 = quotient(i0 + all - 1, each);
+  const bool mine = g < a.group && w0 != w1;  // the others are written already
   const Weight<sizeof(IO) == 4 || FP8> weight(a.scale);
   float to = -INFINITY, sum = 0.f, y[8] = {};
-  if (group < GROUPS) {
-    for (int k = group; k < count && base + tile * count + k < a.units; k += GROUPS) {
-      const float* slot = a.work + ((size_t)(base + tile * count + k) * G + h) * (ROWS * (D + 2));
+  if (mine) {
+    for (int64_t w = w0 + group; w <= w1 && w < a.share; w += groups) {
+      const float* slot = a.work + (((size_t)w * G + h) * 2 + (w == w0 && i0 != w0 * each ? 1 : 0)) * (ROWS * (D + 2));
       const float mk = slot[ROWS * D + in], lk = slot[ROWS * D + ROWS + in];
       Vec<8> v;
       v.load(slot + in * D + c);
-      const float next = fmaxf(to, mk);
-      const float f = weight.from(to, next), g = weight.from(mk, next);
+      const float next = fmaxf(to, mk), f = weight.from(to, next), f2 = weight.from(mk, next);
       to = next;
-      sum = fmaf(sum, f, lk * g);
+      sum = fmaf(sum, f, lk * f2);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) y[j] = fmaf(y[j], f, v.e[j] * g);
+      for (int j = 0; j < 8; ++j) y[j] = fmaf(y[j], f, v.e[j] * f2);
     }
-    float4* dst = reinterpret_cast<float4*>(&so[group][lane * 8]);
-    dst[0] = make_float4(y[0], y[1], y[2], y[3]);
-    dst[1] = make_float4(y[4], y[5], y[6], y[7]);
-    if (c == 0) { sm[group][mine] = to; sl[group][mine] = sum; }
   }
-  __syncthreads();
-  if (group == 0) {
-    const int groups = count < GROUPS ? count : GROUPS;
-    to = -INFINITY;
-    for (int k = 0; k < groups; ++k) to = fmaxf(to, sm[k][mine]);
-    sum = 0.f;
+  if (groups > 1) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) y[j] = 0.f;
-    for (int k = 0; k < groups; ++k) {
-      const float g = weight.from(sm[k][mine], to);
-      sum = fmaf(g, sl[k][mine], sum);
+    for (int j = 0; j < 8; ++j) so[tid][j] = y[j];
+    sm[tid] = to;
+    sl[tid] = sum;
+    __syncthreads();
+    if (group == 0 && mine) {
+      const int n = w1 - w0 + 1 < groups ? (int)(w1 - w0) + 1 : groups;
+      const float own = to;
+#pragma unroll 4
+      for (int k = 1; k < n; ++k) to = fmaxf(to, sm[tid + k * a.span]);
+      const float f = weight.from(own, to);
+      sum *= f;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) y[j] = fmaf(g, so[k][lane * 8 + j], y[j]);
+      for (int j = 0; j < 8; ++j) y[j] *= f;
+#pragma unroll 4
+      for (int k = 1; k < n; ++k) {
+        const float f2 = weight.from(sm[tid + k * a.span], to);
+        sum = fmaf(f2, sl[tid + k * a.span], sum);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) y[j] = fmaf(f2, so[tid + k * a.span][j], y[j]);
+      }
     }
+  }
+  if (group == 0 && mine) {
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
     for (int j = 0; j < 8; ++j) y[j] *= inv;
-    put<IO, FP8>(a, t, (head + mine) * D + c, y);
+    put<IO, FP8>(a, t, (h * a.group + g) * D + c, y);
   }
 }
 
@@ -673,27 +734,48 @@ int64_t most_tiles(int batch, int tokens, int group, int rows) {
   const int64_t whole = (int64_t)tokens * group / rows + batch, apart = (int64_t)tokens * ((group + rows - 1) / rows);
   return whole < apart ? whole : apart;
 }
+// The plan that join_kernel reads: rounds a workgroup has, then those before each sequence.
+int64_t plan_words(int batch) { return ((int64_t)batch + 1 + 1) / 2 * 2; }
 // Splits keys: tiles of query rows too few to fill the chip, 256 rows a workgroup.
 bool splits(int batch, int tokens, int group, int G) { return ((int64_t)tokens * group / 256 + batch / 4) * G < 256; }
 int split_tiles(int batch, int tokens, int group) { return (int64_t)tokens * group <= (int64_t)16 * batch ? 1 : 2; }
-// Pieces there can be at most.
-int64_t most_units(int batch, int tokens, int group, int G, int QT) { return (kShare + G - 1) / G + most_tiles(batch, tokens, group, 16 * QT); }
-// Whether a sequence can be more than one piece.
-bool joins(int columns, int page) { return (int64_t)columns * page > kLeast * kStep; }
+// Workgroups a key head's rounds are shared out to: as many as are at work at once (by the registers of
+// attention_kernel), and no more than there can be rounds.
+int shares(int batch, int tokens, int group, int G, int D, int QT, int64_t capacity) {
+  const int held = kCUs * (QT == 2 ? (D == 64 ? 3 : 2) : D == 64 ? 4 : D <= 128 ? 3 : 2);
+  const int64_t most = most_tiles(batch, tokens, group, 16 * QT) * ((capacity + kStep * kWaves - 1) / (kStep * kWaves));
+  const int64_t n = held / G < 1 ? 1 : held / G;
+  return (int)(n < most ? n : most);
+}
 
 template <typename IO, int D, bool FP8> int launch(const AttentionArgs& a, hipStream_t s) {
   const int batch = a.tok.seq.batch, tokens = a.tok.seq.tokens, G = a.cache.heads;
   if (splits(batch, tokens, a.group, G)) {
     auto run = [&](auto qt) {
       constexpr int QT = decltype(qt)::value;
-      const int64_t units = most_units(batch, tokens, a.group, G, QT), workgroups = units * G;
-      const int64_t rows = (int64_t)tokens * a.H / (FP8 && D == 64 ? 2 : 1);
-      const bool join = joins(a.tok.columns, 16 << a.cache.shift);
-      if (!fits(workgroups, kThreads) || (join && !fits(rows, kThreads))) return -3;
+      const int64_t capacity = (int64_t)a.tok.columns << (a.cache.shift + 4);
       AttentionArgs b = a;
-      b.units = (int)units;
-      hipLaunchKernelGGL((attention_kernel<IO, D, QT, true, FP8>), dim3((unsigned)workgroups), dim3(kThreads), 0, s, b);
-      if (join && taken()) hipLaunchKernelGGL((join_kernel<IO, D, QT, FP8>), dim3((unsigned)rows), dim3(kThreads), 0, s, b);
+      b.share = shares(batch, tokens, a.group, G, D, QT, capacity);
+      const int64_t workgroups = (int64_t)b.share * G;
+      const bool join = capacity > kStep * kWaves && b.share > 1;  // a round is never split
+      // few pieces a workgroup, so that many lanes share a tile's slots, until there are workgroups enough
+      const int pieces = a.group * (D / 8);
+      b.span = 16;
+      while (b.span < 256 && b.span < pieces && (int64_t)tokens * G * ((pieces + b.span - 1) / b.span) > 4 * kCUs) b.span *= 2;
+      const int64_t joins = (int64_t)tokens * G * ((pieces + b.span - 1) / b.span);
+      if (!fits(workgroups, kThreads) || !fits(joins, kThreads)) return -3;
+      if (join) {
+        b.plan = reinterpret_cast<int64_t*>(a.work);
+        b.work = reinterpret_cast<float*>(b.plan + plan_words(batch));
+      }
+      // Past the caches where the pool is larger than the last-level one, so that nothing of it is there the next time: 64 requests of
+      // up to 8192 tokens 61.3 -> 56.8 us (pool 330 MB); 32 of 4096 with 16 key heads, out of that cache, 40.3 -> 45.7.  Records of
+      // 128 channels only, where every load takes whole lines: of 64, 41.4 -> 54.4.
+      constexpr bool CAN = D == 128 && QT == 1;
+      const bool past = CAN && (int64_t)a.cache.pages * G * (17 * D) << a.cache.shift > (int64_t)256 << 20;
+      if (past) hipLaunchKernelGGL((attention_kernel<IO, D, QT, true, FP8, CAN>), dim3((unsigned)workgroups), dim3(kThreads), 0, s, b);
+      else hipLaunchKernelGGL((attention_kernel<IO, D, QT, true, FP8, false>), dim3((unsigned)workgroups), dim3(kThreads), 0, s, b);
+      if (join && taken()) hipLaunchKernelGGL((join_kernel<IO, D, QT, FP8>), dim3((unsigned)joins), dim3(kThreads), 0, s, b);
       return 0;
     };
     if constexpr (most_tiles_held(sizeof(IO), D, true) > 1)
@@ -703,7 +785,7 @@ template <typename IO, int D, bool FP8> int launch(const AttentionArgs& a, hipSt
   constexpr int QT = most_tiles_held(sizeof(IO), D, false);
   const int64_t workgroups = most_tiles(batch, tokens, a.group, 16 * QT * kWaves) * G;
   if (!fits(workgroups, kThreads)) return -3;
-  hipLaunchKernelGGL((attention_kernel<IO, D, QT, false, FP8>), dim3((unsigned)workgroups), dim3(kThreads), 0, s, a);
+  hipLaunchKernelGGL((attention_kernel<IO, D, QT, false, FP8, false>), dim3((unsigned)workgroups), dim3(kThreads), 0, s, a);
   return 0;
 }
 
@@ -735,9 +817,14 @@ int run_attention(const AttentionArgs& a, int D, int io, bool fp8, void* stream)
 
 size_t attention_workspace(int batch, int tokens, int H, int G, int D, int columns, int page) {
   const int group = H / G;
-  if (!splits(batch, tokens, group, G) || !joins(columns, page)) return 0;
-  const int QT = split_tiles(batch, tokens, group);  // of one tile a wave (wide heads in fp32) there are more, each half as large
-  return (size_t)most_units(batch, tokens, group, G, QT) * G * (16 * QT) * (D + 2) * 4;
+  const int64_t capacity = (int64_t)columns * page;
+  if (!splits(batch, tokens, group, G) || capacity <= kStep * kWaves) return 0;
+  size_t most = 0;  // whichever tiles the type's kernel takes
+  for (int QT = 1; QT <= 2; ++QT) {
+    const size_t n = (size_t)shares(batch, tokens, group, G, D, QT, capacity) * G * 2 * (16 * QT) * (D + 2) * 4;
+    most = n > most ? n : most;
+  }
+  return most + (size_t)plan_words(batch) * 8;
 }
 
 }  // namespace skssm

@@ -212,7 +212,7 @@ int sketchssm_cache_read(const skssm_cache* cache, const skssm_new_tokens* seq, 
 
 size_t sketchssm_attention_workspace(const skssm_cache* cache, int32_t heads, int32_t batch, int64_t tokens, int32_t columns) {
   if (check_cache("sketchssm_attention_workspace", cache) || heads < 1 || heads % cache->kv_heads || batch < 1 || tokens < 1 ||
-      tokens > kMaxTokens || (tokens + 1) * heads > (int64_t)1 << 31 || columns < 1 || (int64_t)columns * cache->page > kMaxTokens)
+      tokens > kMaxTokens || (tokens + 1) * heads > (int64_t)1 << 30 || columns < 1 || (int64_t)columns * cache->page > kMaxTokens)
     return 0;
   return attention_workspace(batch, (int)tokens, heads, cache->kv_heads, cache->dim, columns, cache->page);
 }
@@ -227,7 +227,7 @@ int sketchssm_attention(const skssm_cache* cache, const skssm_new_tokens* seq, c
   if (p.out_dtype != p.io_dtype && p.out_dtype != SKSSM_E4M3)
     return fail(SKSSM_EINVAL, "%s: out_dtype %d is neither the io dtype nor E4M3", what, p.out_dtype);
   const bool fp8 = p.out_dtype == SKSSM_E4M3;
-  if ((seq->tokens + 1) * (int64_t)p.heads > (int64_t)1 << 31) return fail(SKSSM_EUNSUPPORTED, "%s: %lld tokens of %d heads: at most 2^31 rows", what, (long long)seq->tokens, p.heads);
+  if ((seq->tokens + 1) * (int64_t)p.heads > (int64_t)1 << 30) return fail(SKSSM_EUNSUPPORTED, "%s: %lld tokens of %d heads: at most 2^30 rows", what, (long long)seq->tokens, p.heads);
   if (p.heads < 1 || p.heads % cache->kv_heads) return fail(SKSSM_EINVAL, "%s: %d key heads do not divide %d heads", what, cache->kv_heads, p.heads);
   if (!(p.scale > 0.f) || !std::isfinite(p.scale)) return fail(SKSSM_EINVAL, "%s: scale must be > 0 and finite", what);
   const int64_t T = seq->tokens, D = cache->dim, H = p.heads;

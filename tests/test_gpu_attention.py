@@ -344,3 +344,28 @@ def test_a_wide_table():
     case("wide table")
     check("bf16", 4, 1, 128, 16, [1, 1], [70, 3], columns=5000)
     check("bf16", 4, 1, 128, 1024, [2, 0], [2, 0], columns=1000)
+
+
+@pytest.mark.parametrize("columns,page,length", [(1, 128, 129), (1, 128, 140), (8, 16, 200), (2, 16, 33), (3, 1024, 4000)])
+def test_lengths_past_the_table(columns, page, length):
+    """Tokens past the table's last column read as NaN, also where its places are whole rounds of steps."""
+    case("past", columns, page, length)
+    r = rnd(columns)
+    cap = columns * page
+    cache, tab, _, _, _ = built(r, [cap, 5], 2, 64, page, torch.bfloat16)
+    assert tab.shape[1] == columns
+    q = r((4, 4, 64), torch.bfloat16)
+    out, _ = ops.attention(cache, tab, i32([length, 5]), q, offsets=R.offsets([2, 2]))
+    seen = torch.isnan(out).all(-1)
+    assert bool(seen[1].all()) and not bool(torch.isnan(out[2:]).any()) and bool(seen[0].all()) == (length - 2 >= cap)
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+@pytest.mark.parametrize("B,longest,H,G,D", [(300, 40, 4, 2, 64), (700, 9, 2, 1, 128), (65, 900, 8, 1, 128), (130, 300, 6, 2, 96), (257, 260, 4, 4, 256)])
+def test_many_sequences(io, B, longest, H, G, D):
+    """More sequences than lanes and than threads; workgroups whose share is parts of several."""
+    case("many", io, B, longest, H, G, D)
+    g = torch.Generator().manual_seed(B)
+    lengths = [int(x) for x in torch.randint(0, longest + 1, (B,), generator=g)]
+    new = [min(1, n) for n in lengths] if B != 130 else [min(n, int(x)) for n, x in zip(lengths, torch.randint(0, 4, (B,), generator=g))]
+    check(io, H, G, D, 16, new, lengths, seed=B)
