@@ -67,6 +67,10 @@ struct AttentionArgs {
   NewTokens tok;
   Cache cache;
   int H, group;    // query heads, and how many share a key head
+  uint32_t magic, bits;
+  // n / group of 0 <= n < 2^31, with 2^bits >= group, magic = floor(2^32 (2^bits - group) / group) + 1: the product is n (2^bits / group - 1), a
+  // little more, over 2^32.
+  __device__ __forceinline__ int by_group(int n) const { return (int)((__umulhi((uint32_t)n, magic) + (uint32_t)n) >> bits); }
   float scale;
   const void* q;
   size_t ldq, q_head;
@@ -75,7 +79,7 @@ struct AttentionArgs {
   float* scales;
   size_t ld_scales;
   float* work;     // [share][key heads][2]: a tile's sums, maxima and sums of weights
-  int64_t* plan;   // at the workspace's start (NULL: no tile can be split)
+  int* plan;       // at the workspace's start (NULL: no tile can be split)
   int share;       // workgroups of attention_kernel a key head
   int span;        // pieces of 8 channels a workgroup of join_kernel
 };

@@ -191,19 +191,19 @@ template <int ROWS> __device__ __forceinline__ Extent extent(const AttentionArgs
 
 // Where a position among the sequences' weights lies: each thread sums the weights of a run of sequences, and
 // `upto` [kThreads] holds the sums up to and with each run.
-template <typename F> __device__ __forceinline__ int64_t lay_out(int batch, F weight, int64_t* upto) {
+template <typename F> __device__ __forceinline__ int lay_out(int batch, F weight, int* upto) {
   if (batch == 1) return weight(0);
-  __shared__ int64_t waves[kWaves];
+  __shared__ int waves[kWaves];
   const int run = (batch + kThreads - 1) / kThreads, tid = threadIdx.x;
-  int64_t x = 0;
+  int x = 0;
   for (int b = tid * run; b < (tid + 1) * run && b < batch; ++b) x += weight(b);
   for (int d = 1; d < 64; d *= 2) {
-    const int64_t y = __shfl_up((long long)x, d);
+    const int y = __shfl_up(x, d);
     x += (tid & 63) >= d ? y : 0;
   }
   if ((tid & 63) == 63) waves[tid >> 6] = x;
   __syncthreads();
-  int64_t total = 0;
+  int total = 0;
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) {
     if (w < tid >> 6) x += waves[w];
@@ -214,7 +214,7 @@ template <typename F> __device__ __forceinline__ int64_t lay_out(int batch, F we
   return total;
 }
 // The sequence that holds position x of the total, and x's place in it.
-template <typename F> __device__ __forceinline__ int seek(int batch, F weight, const int64_t* upto, int64_t x, int64_t& at) {
+template <typename F> __device__ __forceinline__ int seek(int batch, F weight, const int* upto, int x, int& at) {
   at = x;
   if (batch == 1) return 0;
   const int run = (batch + kThreads - 1) / kThreads;
@@ -229,22 +229,13 @@ template <typename F> __device__ __forceinline__ int seek(int batch, F weight, c
   if (first) at -= upto[first - 1];
   int b = first * run;
   while (b + 1 < batch) {
-    const int64_t w = weight(b);
+    const int w = weight(b);
     if (at < w) break;
     at -= w;
     ++b;
   }
-  at = (int64_t)uniform((int)(at >> 32)) << 32 | (uint32_t)uniform((int)at);
+  at = uniform(at);
   return uniform(b);
-}
-
-// a / b of 0 <= a < 2^52, 0 < b, by way of fp64: a quarter of the instructions of a 64-bit division.
-__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
-  int64_t q = (int64_t)((double)a * __builtin_amdgcn_rcp((double)b));
-  int64_t r = a - q * b;  // rcp is a few units off: q is within a unit or, of large quotients, some
-  while (r < 0) { r += b; --q; }
-  while (r >= b) { r -= b; ++q; }
-  return q;
 }
 
 // Split sequences.  The steps of a tile of rows are counted in rounds, one step of each wave, one round at least. A key head's rounds of all
@@ -254,9 +245,9 @@ __device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
 __device__ __forceinline__ int rounds(const Extent& e) { return e.steps <= kWaves ? 1 : (e.steps + kWaves - 1) / kWaves; }
 template <int ROWS> struct Rounds {
   const AttentionArgs& a;
-  __device__ __forceinline__ int64_t operator()(int b) const {
+  __device__ __forceinline__ int operator()(int b) const {
     const Extent e = extent<ROWS>(a, b);
-    return (int64_t)e.tiles * rounds(e);
+    return e.tiles * rounds(e);
   }
 };
 
@@ -292,7 +283,7 @@ template <typename IO, bool FP8> __device__ __forceinline__ void put(const Atten
 
 // Tiles of rows that a wave takes at most, and waves a SIMD that its registers are held to.
 constexpr int most_tiles_held(size_t io, int D, bool split) {
-  return io == 4 ? (D > 96 ? 1 : 2) : D == 256 || (split && D == 192) ? 1 : 2;
+  return io == 4 ? (D > 96 ? 1 : 2) : D == 256 || (split && D == 192) ? 1 : !split && D == 96 ? 3 : 2;
 }
 constexpr int waves_held(size_t io, int D) { return io == 4 && D == 256 ? 1 : 2; }
 
@@ -308,21 +299,21 @@ __global__ __launch_bounds__(kThreads, waves_held(sizeof(IO), D)) void attention
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int G = a.cache.heads, h = blockIdx.x % G, u = blockIdx.x / G;
 
-  __shared__ int64_t upto[kThreads];
+  __shared__ int upto[kThreads];
   const int batch = a.tok.seq.batch;
   const Rounds<ROWS> weight_of{a};
-  auto blocks_of = [&](int b) INLINE { return (int64_t)extent<ROWS * kWaves>(a, b).tiles; };
-  int64_t x = u, x1 = u + 1, each = 1, place = 0, total;
+  auto blocks_of = [&](int b) INLINE { return extent<ROWS * kWaves>(a, b).tiles; };
+  int x = u, x1 = u + 1, each = 1, place = 0, total;
   int b;
   if constexpr (SPLIT) {
     total = lay_out(batch, weight_of, upto);
-    each = quotient(total + a.share - 1, a.share);
+    each = (int)(((uint32_t)total + a.share - 1) / a.share);
     x = u * each;
-    x1 = x + each < total ? x + each : total;
+    x1 = total - x < each ? total : x + each;
     if (a.plan && blockIdx.x == 0) {  // for join_kernel
       if (threadIdx.x == 0) a.plan[0] = each;
       const int run = (batch + kThreads - 1) / kThreads;
-      int64_t before = batch == 1 || threadIdx.x == 0 ? 0 : upto[threadIdx.x - 1];
+      int before = batch == 1 || threadIdx.x == 0 ? 0 : upto[threadIdx.x - 1];
       for (int i = threadIdx.x * run; i < (int)(threadIdx.x + 1) * run && i < batch; ++i) {
         a.plan[1 + i] = before;
         before += weight_of(i);
@@ -345,14 +336,14 @@ __global__ __launch_bounds__(kThreads, waves_held(sizeof(IO), D)) void attention
   e.steps = uniform(e.steps);
   const int all = rounds(e);
   // the last rows see the most keys: they go first
-  const int tile = SPLIT ? (int)quotient(place, all) : ((e.tiles + kWaves - 1) / kWaves - 1 - (int)place) * kWaves + wave;
-  const int r0 = SPLIT ? (int)(place - (int64_t)tile * all) : 0, r1 = SPLIT && x1 - x < all - r0 ? r0 + (int)(x1 - x) : all;
+  const int tile = SPLIT ? place / all : ((e.tiles + kWaves - 1) / kWaves - 1 - place) * kWaves + wave;
+  const int r0 = SPLIT ? place - tile * all : 0, r1 = SPLIT && x1 - x < all - r0 ? r0 + x1 - x : all;
   const bool whole_tile = !SPLIT || (r0 == 0 && r1 == all);
   const int row0 = tile * ROWS, rows = e.n * a.group - row0 < ROWS ? e.n * a.group - row0 : ROWS;
   if (!SPLIT && rows <= 0) return;
   const int most = a.tok.columns << (a.cache.shift + 4);
   auto limit = [&](int row) INLINE {  // the last key that a row sees; of keys past the table one, which reads as NaN
-    const int place = e.length - e.n + row / a.group;
+    const int place = e.length - e.n + a.by_group(row);
     return place < most ? place : most;
   };
   const int low = limit(row0), high = limit(row0 + rows - 1);
@@ -363,7 +354,7 @@ __global__ __launch_bounds__(kThreads, waves_held(sizeof(IO), D)) void attention
   bf16x8 q[QT][N][QP];
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
-    const int row = row0 + 16 * t + r, i = row / a.group;
+    const int row = row0 + 16 * t + r, i = a.by_group(row);
     const bool in = 16 * t + r < rows;
     const IO* src = static_cast<const IO*>(a.q) + (in ? (size_t)(e.first + i) * a.ldq + (size_t)(h * a.group + row - i * a.group) * a.q_head : 0) + kg * (D / 4);
 #pragma unroll
@@ -459,29 +450,42 @@ __global__ __launch_bounds__(kThreads, waves_held(sizeof(IO), D)) void attention
       for (int i = 0; i < 8; ++i) w[t][i] = z[t][i >> 2][i & 3];
     uint32_t spoilt = 0;  // bit i: a value of token i is not a number
     if constexpr (EDGE) {
-      const int n = e.length < most ? e.length : most + 1;  // keys there are
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const int key = kStep * s + (i >> 2) * 16 + kg * 4 + (i & 3);
-        // what lies behind the sequence may be anything, and a NaN among the values may not meet the zero weights of rows that do not see it
-        uint32_t nan = 0;
 #pragma unroll
-        for (int g = 0; g < N; ++g) {
-          const int at = (i & 3) * N + g, sh = 8 * (at & 3);
-          nan |= (x[i >> 2].vs.w[at >> 2] >> sh & 255u) == 255u;
-        }
-        const bool gone = key >= n;
-        spoilt |= gone ? 0u : nan << i;
-        if (gone || nan) {
+        for (int t = 0; t < QT; ++t) w[t][i] = key <= lim[t] ? w[t][i] : -INFINITY;
+      }
+      // Zero weights may meet nothing but numbers: what lies behind the sequence may be anything, and values that are not
+      // numbers (an exponent of 255) reach the rows that see them by their weights.
+      const int n = e.length < most ? e.length : most + 1;  // keys there are
+      uint32_t any = 0;
+#pragma unroll
+      for (int i = 0; i < 2 * N; ++i) {
+        const uint32_t y = ~x[i / N].vs.w[i % N];
+        any |= (y - 0x01010101u) & ~y & 0x80808080u;  // a byte of y is 0
+      }
+      if (kStep * s + kStep > n || __builtin_amdgcn_ballot_w64(any != 0)) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int key = kStep * s + (i >> 2) * 16 + kg * 4 + (i & 3);
+          uint32_t nan = 0;
 #pragma unroll
           for (int g = 0; g < N; ++g) {
             const int at = (i & 3) * N + g, sh = 8 * (at & 3);
-            uint32_t& word = x[i >> 2].vs.w[at >> 2];
-            word = (word & ~(255u << sh)) | 127u << sh;
+            nan |= (x[i >> 2].vs.w[at >> 2] >> sh & 255u) == 255u;
+          }
+          const bool gone = key >= n;
+          spoilt |= gone ? 0u : nan << i;
+          if (gone || nan) {
+#pragma unroll
+            for (int g = 0; g < N; ++g) {
+              const int at = (i & 3) * N + g, sh = 8 * (at & 3);
+              uint32_t& word = x[i >> 2].vs.w[at >> 2];
+              word = (word & ~(255u << sh)) | 127u << sh;
+            }
           }
         }
-#pragma unroll
-        for (int t = 0; t < QT; ++t) w[t][i] = key <= lim[t] ? w[t][i] : -INFINITY;
       }
     }
     bf16x8 p[QT][WP];
@@ -490,7 +494,7 @@ __global__ __launch_bounds__(kThreads, waves_held(sizeof(IO), D)) void attention
       float f[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) f[i] = weight(w[t][i], under);
-      if constexpr (EDGE) {
+      if (EDGE && __builtin_amdgcn_ballot_w64(spoilt != 0)) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) f[i] = (spoilt >> i & 1) && w[t][i] != -INFINITY ? __builtin_nanf("") : f[i];
       }
@@ -617,7 +621,7 @@ __global__ __launch_bounds__(kThreads, waves_held(sizeof(IO), D)) void attention
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
         for (int j = 0; j < 8; ++j) y[j] *= inv;
-        const int tok = (row0 + row) / a.group;
+        const int tok = a.by_group(row0 + row);
         put<IO, FP8>(a, e.first + tok, (h * a.group + row0 + row - tok * a.group) * D + c, y);
       } else {
         float* slot = a.work + ((size_t)blockIdx.x * 2 + (x == u * each ? 0 : 1)) * (ROWS * (D + 2));
@@ -633,7 +637,7 @@ __global__ __launch_bounds__(kThreads, waves_held(sizeof(IO), D)) void attention
     place += r1 - r0;
     if (x < x1) {
       __syncthreads();  // `shared` is written again
-      while (place >= (int64_t)e.tiles * rounds(e) && b + 1 < batch) {  // the next sequence that has rows
+      while (place >= e.tiles * rounds(e) && b + 1 < batch) {  // the next sequence that has rows
         e = extent<ROWS>(a, ++b);
         e.tiles = uniform(e.tiles);
         e.steps = uniform(e.steps);
@@ -653,7 +657,7 @@ __global__ __launch_bounds__(kThreads, waves_held(sizeof(IO), D)) void attention
         const int row = i / (D / 8), c = (i - row * (D / 8)) * 8;
         Vec<8> v;
         v.load(so + row * PITCH + c);
-        const int at_row = row0 + 16 * t + row, tok = at_row / a.group;
+        const int at_row = row0 + 16 * t + row, tok = a.by_group(at_row);
         put<IO, FP8>(a, e.first + tok, (h * a.group + at_row - tok * a.group) * D + c, v.e);
       }
       wave_lds_sync();
@@ -670,20 +674,20 @@ template <typename IO, int D, int QT, bool FP8> __global__ __launch_bounds__(kTh
   __shared__ float so[kThreads][8], sm[kThreads], sl[kThreads];
   const int G = a.cache.heads, spans = (a.group * (D / 8) + a.span - 1) / a.span;
   const int item = blockIdx.x / spans, t = item / G, h = item - t * G, tid = threadIdx.x;
-  const int64_t each = a.plan[0];
+  const int each = a.plan[0];
   const int b = uniform(a.tok.seq.of(t));
-  const int64_t before = a.plan[1 + b];
+  const int before = a.plan[1 + b];
   const Extent e = extent<ROWS>(a, b);
   if (t < e.first || t >= e.first + e.n) return;
   const int all = rounds(e), groups = kThreads / a.span, group = tid / a.span;
   const int piece = (blockIdx.x - item * spans) * a.span + (tid & (a.span - 1)), g = piece / (D / 8), c = (piece - g * (D / 8)) * 8;
   const int row = (t - e.first) * a.group + g, tile = row / ROWS, in = row - tile * ROWS;
-  const int64_t i0 = before + (int64_t)tile * all, w0 = quotient(i0, each), w1 = quotient(i0 + all - 1, each);
+  const int i0 = before + tile * all, w0 = i0 / each, w1 = (i0 + all - 1) / each;
   const bool mine = g < a.group && w0 != w1;  // the others are written already
   const Weight<sizeof(IO) == 4 || FP8> weight(a.scale);
   float to = -INFINITY, sum = 0.f, y[8] = {};
   if (mine) {
-    for (int64_t w = w0 + group; w <= w1 && w < a.share; w += groups) {
+    for (int w = w0 + group; w <= w1 && w < a.share; w += groups) {
       const float* slot = a.work + (((size_t)w * G + h) * 2 + (w == w0 && i0 != w0 * each ? 1 : 0)) * (ROWS * (D + 2));
       const float mk = slot[ROWS * D + in], lk = slot[ROWS * D + ROWS + in];
       Vec<8> v;
@@ -702,7 +706,7 @@ template <typename IO, int D, int QT, bool FP8> __global__ __launch_bounds__(kTh
     sl[tid] = sum;
     __syncthreads();
     if (group == 0 && mine) {
-      const int n = w1 - w0 + 1 < groups ? (int)(w1 - w0) + 1 : groups;
+      const int n = w1 - w0 + 1 < groups ? w1 - w0 + 1 : groups;
       const float own = to;
 #pragma unroll 4
       for (int k = 1; k < n; ++k) to = fmaxf(to, sm[tid + k * a.span]);
@@ -735,17 +739,25 @@ int64_t most_tiles(int batch, int tokens, int group, int rows) {
   return whole < apart ? whole : apart;
 }
 // The plan that join_kernel reads: rounds a workgroup has, then those before each sequence.
-int64_t plan_words(int batch) { return ((int64_t)batch + 1 + 1) / 2 * 2; }
+int64_t plan_words(int batch) { return ((int64_t)batch + 1 + 3) / 4 * 4; }
 // Splits keys: tiles of query rows too few to fill the chip, 256 rows a workgroup.
 bool splits(int batch, int tokens, int group, int G) { return ((int64_t)tokens * group / 256 + batch / 4) * G < 256; }
-int split_tiles(int batch, int tokens, int group) { return (int64_t)tokens * group <= (int64_t)16 * batch ? 1 : 2; }
 // Workgroups a key head's rounds are shared out to: as many as are at work at once (by the registers of
 // attention_kernel), and no more than there can be rounds.
+int64_t most_rounds(int batch, int tokens, int group, int QT, int64_t capacity) {
+  return most_tiles(batch, tokens, group, 16 * QT) * ((capacity + kStep * kWaves - 1) / (kStep * kWaves));
+}
 int shares(int batch, int tokens, int group, int G, int D, int QT, int64_t capacity) {
   const int held = kCUs * (QT == 2 ? (D == 64 ? 3 : 2) : D == 64 ? 4 : D <= 128 ? 3 : 2);
-  const int64_t most = most_tiles(batch, tokens, group, 16 * QT) * ((capacity + kStep * kWaves - 1) / (kStep * kWaves));
+  const int64_t most = most_rounds(batch, tokens, group, QT, capacity);
   const int64_t n = held / G < 1 ? 1 : held / G;
   return (int)(n < most ? n : most);
+}
+
+// Tiles of rows a wave: two where the sequences' rows fill them and there is more than a few rounds of work for every workgroup; with less,
+// what counts is the time of one.
+int split_tiles(int batch, int tokens, int group, int G, int64_t capacity) {
+  return (int64_t)tokens * group > (int64_t)16 * batch && most_rounds(batch, tokens, group, 2, capacity) * G > 16 * kCUs ? 2 : 1;
 }
 
 template <typename IO, int D, bool FP8> int launch(const AttentionArgs& a, hipStream_t s) {
@@ -763,9 +775,9 @@ template <typename IO, int D, bool FP8> int launch(const AttentionArgs& a, hipSt
       b.span = 16;
       while (b.span < 256 && b.span < pieces && (int64_t)tokens * G * ((pieces + b.span - 1) / b.span) > 4 * kCUs) b.span *= 2;
       const int64_t joins = (int64_t)tokens * G * ((pieces + b.span - 1) / b.span);
-      if (!fits(workgroups, kThreads) || !fits(joins, kThreads)) return -3;
+      if (!fits(workgroups, kThreads) || !fits(joins, kThreads) || most_rounds(batch, tokens, a.group, QT, capacity) >= (int64_t)1 << 30) return -3;
       if (join) {
-        b.plan = reinterpret_cast<int64_t*>(a.work);
+        b.plan = reinterpret_cast<int*>(a.work);
         b.work = reinterpret_cast<float*>(b.plan + plan_words(batch));
       }
       // Past the caches where the pool is larger than the last-level one, so that nothing of it is there the next time: 64 requests of
@@ -779,7 +791,7 @@ template <typename IO, int D, bool FP8> int launch(const AttentionArgs& a, hipSt
       return 0;
     };
     if constexpr (most_tiles_held(sizeof(IO), D, true) > 1)
-      if (split_tiles(batch, tokens, a.group) == 2) return run(std::integral_constant<int, 2>{});
+      if (split_tiles(batch, tokens, a.group, G, (int64_t)a.tok.columns << (a.cache.shift + 4)) == 2) return run(std::integral_constant<int, 2>{});
     return run(std::integral_constant<int, 1>{});
   }
   constexpr int QT = most_tiles_held(sizeof(IO), D, false);
@@ -824,7 +836,7 @@ size_t attention_workspace(int batch, int tokens, int H, int G, int D, int colum
     const size_t n = (size_t)shares(batch, tokens, group, G, D, QT, capacity) * G * 2 * (16 * QT) * (D + 2) * 4;
     most = n > most ? n : most;
   }
-  return most + (size_t)plan_words(batch) * 8;
+  return most + (size_t)plan_words(batch) * 4;
 }
 
 }  // namespace skssm

@@ -257,6 +257,8 @@ int sketchssm_attention(const skssm_cache* cache, const skssm_new_tokens* seq, c
   a.cache = cache_of(cache);
   a.H = p.heads;
   a.group = p.heads / cache->kv_heads;
+  while ((int64_t)1 << a.bits < a.group) ++a.bits;
+  a.magic = (uint32_t)((((uint64_t)1 << 32) * (((uint64_t)1 << a.bits) - a.group)) / a.group + 1);
   a.scale = p.scale;
   a.q = p.q;
   a.ldq = (size_t)p.ldq;
