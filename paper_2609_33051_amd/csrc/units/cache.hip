@@ -157,16 +157,14 @@ __global__ __launch_bounds__(kThreads) void append_kernel(CacheAppendArgs a, int
     }
   };
 
-
-
+  // where the token goes, looked up while the queries are turned
+  const int tile = place >> 4, r = place & 15, D = a.D, blocks = D >> 5;
+  const int page = a.tok.lengths && place >= 0 ? a.tok.page(a.cache, b, tile) : -1;
   heads(a.q, a.ldq, a.q_head, a.H, std::true_type{}, [&](int h, const float (&y)[8]) {
     IO* dst = static_cast<IO*>(a.y) + (size_t)t * a.ldy + (size_t)h * a.y_head + c0;
     st_elem4(dst, y[0], y[1], y[2], y[3]);
     st_elem4(dst + 4, y[4], y[5], y[6], y[7]);
   });
-  if (!a.tok.lengths || place < 0) return;
-  const int tile = place >> 4, r = place & 15, D = a.D, blocks = D >> 5;
-  const int page = a.tok.page(a.cache, b, tile);
   if (page < 0) return;
   const size_t stride = (size_t)(17 * D) << a.cache.shift;  // from head to head
   uint8_t* rec = a.cache.data + (size_t)page * a.cache.heads * stride + (size_t)(tile & ((1 << a.cache.shift) - 1)) * (17 * D);
@@ -213,43 +211,56 @@ template <typename IO> int launch_append(const CacheAppendArgs& a, hipStream_t s
   return a.rot.rotated % 16 ? launch_append<IO, HALVES_ANY>(a, s) : launch_append<IO, HALVES>(a, s);
 }
 
-// A lane owns 8 channels of a token's head.
+// A lane owns 16 channels of a token's head: keys 8 p .. and 8 p + D / 2 .., and the values that eight bytes of a record hold.
 template <typename IO> __global__ __launch_bounds__(kThreads) void read_kernel(ReadArgs a) {
-  const int D = a.D, pieces = D >> 3, blocks = D >> 5, G = a.cache.heads;
+  const int D = a.D, pieces = D >> 4, blocks = D >> 5, G = a.cache.heads;
   const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
   const int64_t item = i / pieces;
-  const int c0 = (int)(i - item * pieces) * 8, t = (int)(item / G), h = (int)(item - (int64_t)t * G);
+  const int p = (int)(i - item * pieces), t = (int)(item / G), h = (int)(item - (int64_t)t * G);
   if (t >= a.tok.seq.tokens) return;
   const int b = a.tok.seq.of(t), first = a.tok.seq.start(b), n = a.tok.seq.start(b + 1) - first;
   if (t < first || t >= first + n) return;
   const int place = a.tok.lengths[b] - n + (t - first), tile = place >> 4, r = place & 15;
   const int page = place < 0 ? 0 : a.tok.page(a.cache, b, tile);
   const uint8_t* rec = a.cache.data + ((((size_t)(page < 0 ? 0 : page) * G + h) << a.cache.shift) + (tile & ((1 << a.cache.shift) - 1))) * (17 * D);
-  auto give = [&](void* out, uint32_t w, uint32_t e) {
+  auto give = [&](void* out, int c0, uint32_t w, uint32_t e) {
     e = page < 0 ? 255 : e;
     const float scale = __uint_as_float(e << 23);
     IO* dst = static_cast<IO*>(out) + ((size_t)t * G + h) * D + c0;
-    uint32_t p[4];
-    p[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0));
-    p[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1));
-    p[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2));
-    p[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3));
+    uint32_t x[4];
+    x[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0));
+    x[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1));
+    x[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2));
+    x[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3));
 #pragma unroll
-    for (int j = 0; j < 4; ++j) p[j] = place < 0 ? 0 : p[j];
+    for (int j = 0; j < 4; ++j) x[j] = place < 0 ? 0 : x[j];
     if constexpr (sizeof(IO) == 2) {
-      *reinterpret_cast<uint4*>(dst) = make_uint4(p[0], p[1], p[2], p[3]);
+      *reinterpret_cast<uint4*>(dst) = make_uint4(x[0], x[1], x[2], x[3]);
     } else {
-      st_elem4(dst, bf16_lo(p[0]), bf16_hi(p[0]), bf16_lo(p[1]), bf16_hi(p[1]));
-      st_elem4(dst + 4, bf16_lo(p[2]), bf16_hi(p[2]), bf16_lo(p[3]), bf16_hi(p[3]));
+      st_elem4(dst, bf16_lo(x[0]), bf16_hi(x[0]), bf16_lo(x[1]), bf16_hi(x[1]));
+      st_elem4(dst + 4, bf16_lo(x[2]), bf16_hi(x[2]), bf16_lo(x[3]), bf16_hi(x[3]));
     }
   };
-  if (a.k) give(a.k, *reinterpret_cast<const uint32_t*>(rec + r * (D >> 1) + (c0 >> 1)), rec[16 * D + r * blocks + (c0 >> 5)]);
-  if (a.v) {
-    const uint8_t* at = rec + 8 * D + (((r >> 2) * 16 + (c0 & 8)) * blocks + (c0 >> 5)) * 4 + (r & 3);
-    uint32_t w = 0;
+  if (a.k) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) w |= (uint32_t)(at[j * blocks * 4] >> (c0 & 16 ? 4 : 0) & 15) << (4 * j);
-    give(a.v, w, rec[16 * D + (D >> 1) + r * blocks + (c0 >> 5)]);
+    for (int j = 0; j < 2; ++j) {
+      const int c0 = 8 * p + j * (D >> 1);
+      give(a.k, c0, *reinterpret_cast<const uint32_t*>(rec + r * (D >> 1) + (c0 >> 1)), rec[16 * D + r * blocks + (c0 >> 5)]);
+    }
+  }
+  if (a.v) {
+    const int g = p >> 1, c = (p & 1) * 8;  // bytes c .. c + 7 of block g
+    const uint8_t* at = rec + 8 * D + (((r >> 2) * 16 + c) * blocks + g) * 4 + (r & 3);
+    uint32_t lo = 0, hi = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const uint32_t x = at[j * blocks * 4];
+      lo |= (x & 15) << (4 * j);
+      hi |= (x >> 4) << (4 * j);
+    }
+    const uint32_t e = rec[16 * D + (D >> 1) + r * blocks + g];
+    give(a.v, 32 * g + c, lo, e);
+    give(a.v, 32 * g + c + 16, hi, e);
   }
 }
 
@@ -262,7 +273,7 @@ int run_append(const CacheAppendArgs& a, int io, void* stream) {
 
 int run_cache_read(const ReadArgs& a, int io, void* stream) {
   hipStream_t s = static_cast<hipStream_t>(stream);
-  const int64_t workgroups = ((int64_t)a.tok.seq.tokens * a.cache.heads * (a.D / 8) + kThreads - 1) / kThreads;
+  const int64_t workgroups = ((int64_t)a.tok.seq.tokens * a.cache.heads * (a.D / 16) + kThreads - 1) / kThreads;
   if (!fits(workgroups, kThreads)) return -3;
   if (io == 0) hipLaunchKernelGGL((read_kernel<float>), dim3((unsigned)workgroups), dim3(kThreads), 0, s, a);
   else hipLaunchKernelGGL((read_kernel<bf16_t>), dim3((unsigned)workgroups), dim3(kThreads), 0, s, a);

@@ -316,10 +316,11 @@ def _heads(name: str, x: Tensor, shape: tuple, dtype, dev: int) -> tuple[int, in
 
 
 def _rotation(angles: Tensor, positions: Tensor | None, interleaved: bool, tokens: int, dev: int) -> B.Rotation:
-    if angles.dim() != 2:
+    shape = angles.shape
+    if len(shape) != 2:
         raise ValueError("rotation [places][rotated] is needed")
-    return B.Rotation(_flat("rotation", angles, angles.shape, _F32, dev), _flat("positions", positions, (tokens,), torch.int32, dev),
-                      angles.shape[0], angles.shape[1], 1 if interleaved else 0)
+    return B.Rotation(_flat("rotation", angles, shape, _F32, dev), _flat("positions", positions, (tokens,), torch.int32, dev), *shape,
+                      1 if interleaved else 0)
 
 
 def rotary(x: Tensor, rotation: Tensor, positions: Tensor | None = None, *, interleaved: bool = False, out: Tensor | None = None) -> Tensor:
@@ -333,12 +334,13 @@ def rotary(x: Tensor, rotation: Tensor, positions: Tensor | None = None, *, inte
     io = _io(x)
     if x.dim() != 3:
         raise ValueError("x [T][heads][dim] is needed")
-    T, H, D = x.shape
+    T, H, D = shape = x.shape
     if out is None:
-        out = x.new_empty((T, H, D))
+        out, t, h = x.new_empty(shape), H * D, D
+    else:
+        t, h = _heads("out", out, shape, x.dtype, dev)
     rc = (B._lib or B.load()).sketchssm_rotary(io, T, H, D, _rotation(rotation, positions, interleaved, T, dev), x.data_ptr(),
-                                               *_heads("x", x, x.shape, x.dtype, dev), out.data_ptr(), *_heads("out", out, x.shape, x.dtype, dev),
-                                               _stream(dev))
+                                               *_heads("x", x, shape, x.dtype, dev), out.data_ptr(), t, h, _stream(dev))
     if rc:
         B._check(rc)
     return out
@@ -355,16 +357,17 @@ def new_cache(pages: int, kv_heads: int, page: int, dim: int, device="cuda") -> 
 def _cache(cache: Tensor, dev: int) -> B.Cache:
     if cache.dim() != 4 or cache.shape[3] % 17:
         raise ValueError(f"cache: [pages][kv_heads][page / 16][17 dim] bytes are needed, not {_said(cache)}")
-    P, G, n, D = cache.shape
-    return B.Cache(_flat("cache", cache, cache.shape, torch.uint8, dev), P, G, 16 * n, D // 17)
+    P, G, n, D = shape = cache.shape
+    return B.Cache(_flat("cache", cache, shape, torch.uint8, dev), P, G, 16 * n, D // 17)
 
 
 def _tokens(table: Tensor, lengths: Tensor, tokens: int, offsets: Tensor | None, dev: int) -> B.NewTokens:
-    n, off = _offsets(offsets, lengths.numel(), dev)
-    if table.dim() != 2 or table.dtype is not torch.int32 or table.get_device() != dev or table.shape[0] != n or table.stride(1) != 1 and table.shape[1] > 1:
+    n = lengths.numel()
+    off = None if offsets is None else _offsets(offsets, n, dev)[1]
+    shape, s = table.shape, table.stride()
+    if len(shape) != 2 or table.dtype is not torch.int32 or table.get_device() != dev or shape[0] != n or s[1] != 1 and shape[1] > 1:
         raise ValueError(f"table: an int32 tensor [{n}][columns] with contiguous rows on cuda:{dev} is needed, not {_said(table)}")
-    return B.NewTokens(tokens, off, _flat("lengths", lengths, (n,), torch.int32, dev), table.data_ptr(),
-                       table.stride(0) if n > 1 else table.shape[1], n, table.shape[1])
+    return B.NewTokens(tokens, off, _flat("lengths", lengths, (n,), torch.int32, dev), table.data_ptr(), s[0] if n > 1 else shape[1], n, shape[1])
 
 
 def cache_append(cache: Tensor, table: Tensor, lengths: Tensor, k: Tensor, v: Tensor, *, offsets: Tensor | None = None,
@@ -395,11 +398,13 @@ def cache_append(cache: Tensor, table: Tensor, lengths: Tensor, k: Tensor, v: Te
         if rotation is None:
             raise ValueError("q without a rotation")
         shape = (T, q.shape[1], c.dim)
+        a.heads = H = q.shape[1]
+        a.q, a.ldq, a.q_head = q.data_ptr(), *_heads("q", q, shape, t, dev)
         if q_out is None:
             q_out = q.new_empty(shape)
-        a.heads = q.shape[1]
-        a.q, a.ldq, a.q_head = q.data_ptr(), *_heads("q", q, shape, t, dev)
-        a.q_out, a.ld_qout, a.qout_head = q_out.data_ptr(), *_heads("q_out", q_out, shape, t, dev)
+            a.q_out, a.ld_qout, a.qout_head = q_out.data_ptr(), H * c.dim, c.dim
+        else:
+            a.q_out, a.ld_qout, a.qout_head = q_out.data_ptr(), *_heads("q_out", q_out, shape, t, dev)
     elif q_out is not None:
         raise ValueError("q_out without q")
     rot = None if rotation is None else _rotation(rotation, positions, interleaved, T, dev)
@@ -422,10 +427,12 @@ def cache_read(cache: Tensor, table: Tensor, lengths: Tensor, tokens: int, *, of
     if dtype not in _IO:
         raise ValueError(f"{dtype}: bfloat16 or float32 is written")
     shape = (tokens, c.kv_heads, c.dim)
-    if k is None:
-        k = cache.new_empty(shape, dtype=dtype)
-    if v is None:
-        v = cache.new_empty(shape, dtype=dtype)
+    if k is None and v is None:
+        k, v = cache.new_empty((2, *shape), dtype=dtype).unbind()
+    elif k is None:
+        k = torch.empty_like(v)
+    elif v is None:
+        v = torch.empty_like(k)
     rc = (B._lib or B.load()).sketchssm_cache_read(c, _tokens(table, lengths, tokens, offsets, dev), _IO[dtype], _flat("k", k, shape, dtype, dev),
                                                    _flat("v", v, shape, dtype, dev), _stream(dev))
     if rc:
