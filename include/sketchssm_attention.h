@@ -11,7 +11,8 @@
  * Heads.  x [tokens][heads][dim] arrays have a token stride (ld*) and a head
  * stride (*_head) in elements, both multiples of 16 bytes and at least what
  * they step over, so that the parts of a projection's output are read where
- * they lie.
+ * they lie.  An array that is written may share no byte with one that is read
+ * but where it is named as the same; it may lie between its rows.
  */
 #ifndef SKETCHSSM_ATTENTION_H
 #define SKETCHSSM_ATTENTION_H

@@ -740,8 +740,12 @@ int64_t most_tiles(int batch, int tokens, int group, int rows) {
 }
 // The plan that join_kernel reads: rounds a workgroup has, then those before each sequence.
 int64_t plan_words(int batch) { return ((int64_t)batch + 1 + 3) / 4 * 4; }
-// Splits keys: tiles of query rows too few to fill the chip, 256 rows a workgroup.
-bool splits(int batch, int tokens, int group, int G) { return ((int64_t)tokens * group / 256 + batch / 4) * G < 256; }
+// Whether keys are split: not where the sequences' rows mostly fill the four waves' tiles of a workgroup, 128 rows, and there
+// are workgroups for twice the CUs.
+bool splits(int batch, int tokens, int group, int G) {
+  const int64_t rows = (int64_t)tokens * group;
+  return rows < (int64_t)64 * batch || rows * G < (int64_t)128 * 2 * kCUs;
+}
 // Workgroups a key head's rounds are shared out to: as many as are at work at once (by the registers of
 // attention_kernel), and no more than there can be rounds.
 int64_t most_rounds(int batch, int tokens, int group, int QT, int64_t capacity) {

@@ -72,6 +72,16 @@ int check_heads(const char* what, const char* name, const void* p, int64_t token
   return SKSSM_OK;
 }
 
+// Whether arrays of T rows share a byte: rows of a and b bytes, lda and ldb bytes apart.  Rows that lie the same distance
+// apart may lie between one another (the parts of a projection's output).
+bool rows_overlap(const void* p, int64_t a, int64_t lda, const void* q, int64_t b, int64_t ldb, int64_t T) {
+  if (T < 1 || !overlap(p, (size_t)((T - 1) * lda + a), q, (size_t)((T - 1) * ldb + b))) return false;
+  if (lda != ldb || T == 1) return true;
+  int64_t d = (int64_t)(reinterpret_cast<uintptr_t>(q) - reinterpret_cast<uintptr_t>(p)) % lda;
+  if (d < 0) d += lda;
+  return d < a || d + b > lda;
+}
+
 Cache cache_of(const skssm_cache* c) {
   Cache o;
   o.data = static_cast<uint8_t*>(c->data);
@@ -122,7 +132,8 @@ int sketchssm_rotary(int32_t io_dtype, int64_t tokens, int32_t heads, int32_t di
   const Range out[] = {{y, ny}};
   const Range in[] = {{rotation->angles, (size_t)rotation->places * rotation->rotated * 4}, {rotation->positions, (size_t)tokens * 4}};
   const bool same = x == y && ldx == ldy && x_head == y_head;
-  if (any_overlap(out, in) || (!same && nx && overlap(x, nx, y, ny))) return fail(SKSSM_EINVAL, "%s: y overlaps an input", what);
+  const int64_t xr = ((heads - 1) * x_head + dim) * e, yr = ((heads - 1) * y_head + dim) * e;
+  if (any_overlap(out, in) || (!same && rows_overlap(x, xr, ldx * e, y, yr, ldy * e, tokens))) return fail(SKSSM_EINVAL, "%s: y overlaps an input", what);
   if (tokens == 0) return fail(SKSSM_OK, "%s", "");  // nothing to do: no launch, no error
   CacheAppendArgs a{};
   a.tok.seq = sequences(1, tokens, nullptr);
@@ -160,11 +171,16 @@ int sketchssm_cache_append(const skssm_cache* cache, const skssm_new_tokens* seq
               (rc = check_heads(what, "q_out", p.q_out, T, p.heads, D, p.ld_qout, p.qout_head, e, &ny))))
     return rc;
   const Range out[] = {{cache->data, cache_bytes(cache)}, {p.q_out, ny}};
-  const Range in[] = {{p.k, nk}, {p.v, nv}, {seq->offsets, ((size_t)seq->batch + 1) * 4}, {seq->lengths, (size_t)seq->batch * 4},
+  const Range in[] = {{seq->offsets, ((size_t)seq->batch + 1) * 4}, {seq->lengths, (size_t)seq->batch * 4},
                       {seq->table, table_bytes(seq)}, {turns ? rotation->angles : nullptr, turns ? (size_t)rotation->places * rotation->rotated * 4 : 0},
                       {turns ? rotation->positions : nullptr, (size_t)T * 4}};
   const bool same = p.q == p.q_out && p.ldq == p.ld_qout && p.q_head == p.qout_head;
-  if (any_overlap(out, in) || (nq && overlap(p.q, nq, cache->data, out[0].n)) || (!same && nq && overlap(p.q, nq, p.q_out, ny)))
+  const Range held[] = {out[0]};
+  const Range rows[] = {{p.k, nk}, {p.v, nv}, {p.q, nq}};
+  const int64_t kv = (int64_t)cache->kv_heads - 1, yr = ny ? ((p.heads - 1) * p.qout_head + D) * e : 0, yl = p.ld_qout * e;
+  if (any_overlap(out, in) || any_overlap(held, rows) || (ny && rows_overlap(p.q_out, yr, yl, p.k, (kv * p.k_head + D) * e, p.ldk * e, T)) ||
+      (ny && rows_overlap(p.q_out, yr, yl, p.v, (kv * p.v_head + D) * e, p.ldv * e, T)) ||
+      (ny && !same && rows_overlap(p.q_out, yr, yl, p.q, ((p.heads - 1) * p.q_head + D) * e, p.ldq * e, T)))
     return fail(SKSSM_EINVAL, "%s: an output overlaps an input", what);
   if (ny && overlap(p.q_out, ny, cache->data, out[0].n)) return fail(SKSSM_EINVAL, "%s: the outputs overlap", what);
   if (T == 0) return fail(SKSSM_OK, "%s", "");  // nothing to do: no launch, no error
