@@ -281,6 +281,197 @@ template <typename IO, bool FP8> __device__ __forceinline__ void put(const Atten
 
 // ---- the kernel
 
+// A wave's query rows: QT tiles of 16, with the sums over the keys so far.
+template <typename IO, int D, int QT, bool FP8> struct Rows {
+  // bf16 parts of a query and of a weight: what an fp32 result (the scales of an 8-bit output among them) has to keep
+  static constexpr int N = D / 32, QP = sizeof(IO) == 2 ? 1 : 3, WP = FP8 ? 3 : QP;
+  Weight<WP != 1> weight;
+  bf16x8 q[QT][N][QP];
+  floatx4 o[QT][2 * N], l[QT];  // of channels 16 j + 4 (lane / 16) .., and of the weights
+  float m[QT];
+  int lim[QT];                  // the last key that a lane's row sees
+  __device__ __forceinline__ explicit Rows(float scale) : weight(scale) {}
+
+  template <typename F> __device__ __forceinline__ void start(const AttentionArgs& a, const Extent& e, int h, int row0, int rows, int lane, F limit) {
+    const int r = lane & 15, kg = lane >> 4;
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+      const bool in = 16 * t + r < rows;
+      const int row = in ? row0 + 16 * t + r : 0, i = a.by_group(row);
+      lim[t] = in ? limit(row) : -1;
+      const IO* src = static_cast<const IO*>(a.q) + (in ? (size_t)(e.first + i) * a.ldq + (size_t)(h * a.group + row - i * a.group) * a.q_head : 0) + kg * (D / 4);
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        Raw<IO, 8> x;
+        x.zero();
+        if (in) x.load(src + 8 * j);
+        if constexpr (QP == 1) {
+          q[t][j][0] = __builtin_bit_cast(bf16x8, make_uint4(x.w[0], x.w[1], x.w[2], x.w[3]));
+        } else {
+          float f[8];
+#pragma unroll
+          for (int k = 0; k < 8; ++k) f[k] = x.get(k);
+          parts<QP>(f, q[t][j]);
+        }
+      }
+      m[t] = -INFINITY;
+      l[t] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int j = 0; j < 2 * N; ++j) o[t][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+    }
+  }
+
+  // Keys first .. first + 31, of two records: keys(i, j) are channels 8 j .. (of a lane's quarter) of record i's, values(g, lo, hi) block g of
+  // both records' values.  EDGE: some row does not see all of them; spoilt() then has bit i of a lane's eight keys for values that are not
+  // numbers.  fresh: these are the first keys.  used: called when keys have been read.
+  template <bool EDGE, typename K, typename U, typename S, typename V>
+  __device__ __forceinline__ void step(int first, int lane, bool fresh, K keys, U used, S spoil, V values) {
+    const int kg = lane >> 4;
+    floatx4 z[QT][2];
+#pragma unroll
+    for (int t = 0; t < QT; ++t) z[t][0] = z[t][1] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const bf16x8 k = keys(i, j);
+#pragma unroll
+        for (int p = 0; p < QP; ++p)
+#pragma unroll
+          for (int t = 0; t < QT; ++t) z[t][i] = mfma(k, q[t][j][p], z[t][i]);
+      }
+    used();
+    float w[QT][8];
+#pragma unroll
+    for (int t = 0; t < QT; ++t)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) w[t][i] = z[t][i >> 2][i & 3];
+    uint32_t spoilt = 0;
+    if constexpr (EDGE) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int key = first + (i >> 2) * 16 + kg * 4 + (i & 3);
+#pragma unroll
+        for (int t = 0; t < QT; ++t) w[t][i] = key <= lim[t] ? w[t][i] : -INFINITY;
+      }
+      spoilt = spoil();
+    }
+    const bf16x8 ones = __builtin_bit_cast(bf16x8, make_uint4(0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u));
+    bf16x8 p[QT][WP];
+    auto weigh = [&](int t) INLINE {
+      const float under = weight.under(m[t]);
+      float f[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) f[i] = weight(w[t][i], under);
+      if (EDGE && __builtin_amdgcn_ballot_w64(spoilt != 0)) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = (spoilt >> i & 1) && w[t][i] != -INFINITY ? __builtin_nanf("") : f[i];
+      }
+      parts<WP>(f, p[t]);
+      floatx4 sum = l[t];
+#pragma unroll
+      for (int k = 0; k < WP; ++k) sum = mfma(ones, p[t][k], sum);
+      return sum;
+    };
+    floatx4 sum[QT];
+    bool fine = !fresh;
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+      sum[t] = weigh(t);
+      fine = fine && sum[t][0] <= kMost;
+    }
+    if (__builtin_amdgcn_ballot_w64(!fine)) {
+#pragma unroll
+      for (int t = 0; t < QT; ++t) {
+        float top = m[t];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) top = fmaxf(top, w[t][i]);
+        top = across_rows_max(top);
+        const float f = weight.from(m[t], top);
+        m[t] = top;
+        l[t] *= f;
+#pragma unroll
+        for (int j = 0; j < 2 * N; ++j) o[t][j] *= f;
+        sum[t] = weigh(t);
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < QT; ++t) l[t] = sum[t];
+#pragma unroll
+    for (int g = 0; g < N; ++g) {
+      bf16x8 lo, hi;
+      values(g, lo, hi);
+#pragma unroll
+      for (int k = 0; k < WP; ++k)
+#pragma unroll
+        for (int t = 0; t < QT; ++t) {
+          o[t][2 * g] = mfma(lo, p[t][k], o[t][2 * g]);
+          o[t][2 * g + 1] = mfma(hi, p[t][k], o[t][2 * g + 1]);
+        }
+    }
+  }
+
+  // The rows' results, a tile at a time through 16 x (D + 4) floats of LDS that are this wave's.
+  __device__ __forceinline__ void finish(const AttentionArgs& a, const Extent& e, int h, int row0, int rows, int lane, float* so) {
+    constexpr int PITCH = D + 4;
+    const int r = lane & 15, kg = lane >> 4;
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+      const float inv = l[t][0] == 0.f ? 0.f : 1.f / l[t][0];
+#pragma unroll
+      for (int j = 0; j < 2 * N; ++j) *reinterpret_cast<floatx4*>(so + r * PITCH + 16 * j + 4 * kg) = o[t][j] * inv;
+      wave_lds_sync();
+      const int left = rows - 16 * t < 16 ? rows - 16 * t : 16;
+      for (int i = lane; i < left * (D / 8); i += 64) {
+        const int row = i / (D / 8), c = (i - row * (D / 8)) * 8;
+        Vec<8> v;
+        v.load(so + row * PITCH + c);
+        const int at_row = row0 + 16 * t + row, tok = a.by_group(at_row);
+        put<IO, FP8>(a, e.first + tok, (h * a.group + at_row - tok * a.group) * D + c, v.e);
+      }
+      wave_lds_sync();
+    }
+  }
+};
+
+// Zero weights may meet nothing but numbers: what lies behind the sequence (key >= n) may be anything, and values that are not numbers (an
+// exponent of 255) are to reach the rows that see them by their weights.  Takes both out of the values of a lane's four tokens from
+// `key`; bit i of the result: token i's were not numbers.
+template <int D, bool NT> __device__ __forceinline__ uint32_t cleaned(Tile<D, NT>& x, int key, int n) {
+  constexpr int N = D / 32;
+  uint32_t spoilt = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    uint32_t nan = 0;
+#pragma unroll
+    for (int g = 0; g < N; ++g) {
+      const int at = i * N + g, sh = 8 * (at & 3);
+      nan |= (x.vs.w[at >> 2] >> sh & 255u) == 255u;
+    }
+    const bool gone = key + i >= n;
+    spoilt |= gone ? 0u : nan << i;
+    if (gone || nan) {
+#pragma unroll
+      for (int g = 0; g < N; ++g) {
+        const int at = i * N + g, sh = 8 * (at & 3);
+        uint32_t& word = x.vs.w[at >> 2];
+        word = (word & ~(255u << sh)) | 127u << sh;
+      }
+    }
+  }
+  return spoilt;
+}
+// Whether a byte of a lane's exponents is 255.
+template <int D, bool NT> __device__ __forceinline__ bool any_nan(const Tile<D, NT>& x) {
+  uint32_t any = 0;
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) {
+    const uint32_t y = ~x.vs.w[i];
+    any |= (y - 0x01010101u) & ~y & 0x80808080u;  // a byte of y is 0
+  }
+  return any != 0;
+}
+
 // Tiles of rows that a wave takes at most, and waves a SIMD that its registers are held to.
 constexpr int most_tiles_held(size_t io, int D, bool split) {
   return io == 4 ? (D > 96 ? 1 : 2) : D == 256 || (split && D == 192) ? 1 : !split && D == 96 ? 3 : 2;
@@ -292,8 +483,7 @@ constexpr int waves_held(size_t io, int D) { return io == 4 && D == 256 ? 1 : 2;
 // a tile of rows of its own and all their keys.
 template <typename IO, int D, int QT, bool SPLIT, bool FP8, bool NT>
 __global__ __launch_bounds__(kThreads, waves_held(sizeof(IO), D)) void attention_kernel(AttentionArgs a) {
-  // bf16 parts of a query and of a weight: what an fp32 result (the scales of an 8-bit output among them) has to keep
-  constexpr int N = D / 32, ROWS = 16 * QT, QP = sizeof(IO) == 2 ? 1 : 3, WP = FP8 ? 3 : QP, PITCH = D + 4;
+  constexpr int N = D / 32, ROWS = 16 * QT, PITCH = D + 4;
   __shared__ float shared[SPLIT ? kWaves * ROWS * PITCH + 2 * kWaves * ROWS : kWaves * 16 * PITCH];
   const int lane = threadIdx.x & 63, r = lane & 15, kg = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -347,43 +537,8 @@ __global__ __launch_bounds__(kThreads, waves_held(sizeof(IO), D)) void attention
     return place < most ? place : most;
   };
   const int low = limit(row0), high = limit(row0 + rows - 1);
-  int lim[QT];
-#pragma unroll
-  for (int t = 0; t < QT; ++t) lim[t] = 16 * t + r < rows ? limit(row0 + 16 * t + r) : -1;
-
-  bf16x8 q[QT][N][QP];
-#pragma unroll
-  for (int t = 0; t < QT; ++t) {
-    const int row = row0 + 16 * t + r, i = a.by_group(row);
-    const bool in = 16 * t + r < rows;
-    const IO* src = static_cast<const IO*>(a.q) + (in ? (size_t)(e.first + i) * a.ldq + (size_t)(h * a.group + row - i * a.group) * a.q_head : 0) + kg * (D / 4);
-#pragma unroll
-    for (int j = 0; j < N; ++j) {
-      Raw<IO, 8> x;
-      x.zero();
-      if (in) x.load(src + 8 * j);
-      if constexpr (QP == 1) {
-        q[t][j][0] = __builtin_bit_cast(bf16x8, make_uint4(x.w[0], x.w[1], x.w[2], x.w[3]));
-      } else {
-        float f[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) f[k] = x.get(k);
-        parts<QP>(f, q[t][j]);
-      }
-    }
-  }
-
-  const Weight<WP != 1> weight(a.scale);
-  floatx4 o[QT][2 * N], l[QT];
-  float m[QT];
-#pragma unroll
-  for (int t = 0; t < QT; ++t) {
-    m[t] = -INFINITY;
-    l[t] = floatx4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int j = 0; j < 2 * N; ++j) o[t][j] = floatx4{0.f, 0.f, 0.f, 0.f};
-  }
-  const bf16x8 ones = __builtin_bit_cast(bf16x8, make_uint4(0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u));
+  Rows<IO, D, QT, FP8> mine(a.scale);
+  mine.start(a, e, h, row0, rows, lane, limit);
 
   const int stride = SPLIT ? kWaves : 1;
   const int last = high < 0 ? 0 : high / kStep + 1;
@@ -425,121 +580,15 @@ __global__ __launch_bounds__(kThreads, waves_held(sizeof(IO), D)) void attention
     x[0].load_values(r.r0, lane);
     x[1].load_values(r.r1, lane);
   };
-  // EDGE: some row does not see all of the step's keys
-  // keys_used, values_used: called once the step's registers are free
+  const int n = e.length < most ? e.length : most + 1;  // keys there are
   auto compute = [&](Two (&x)[2], int s, auto at_edge, auto keys_used, auto values_used) INLINE {
-    constexpr bool EDGE = decltype(at_edge)::value;
-    floatx4 z[QT][2];
-#pragma unroll
-    for (int t = 0; t < QT; ++t) z[t][0] = z[t][1] = floatx4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int j = 0; j < N; ++j)
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const bf16x8 k = x[i].key(j, lane);
-#pragma unroll
-        for (int p = 0; p < QP; ++p)
-#pragma unroll
-          for (int t = 0; t < QT; ++t) z[t][i] = mfma(k, q[t][j][p], z[t][i]);
-      }
-    keys_used();
-    float w[QT][8];
-#pragma unroll
-    for (int t = 0; t < QT; ++t)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) w[t][i] = z[t][i >> 2][i & 3];
-    uint32_t spoilt = 0;  // bit i: a value of token i is not a number
-    if constexpr (EDGE) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int key = kStep * s + (i >> 2) * 16 + kg * 4 + (i & 3);
-#pragma unroll
-        for (int t = 0; t < QT; ++t) w[t][i] = key <= lim[t] ? w[t][i] : -INFINITY;
-      }
-      // Zero weights may meet nothing but numbers: what lies behind the sequence may be anything, and values that are not
-      // numbers (an exponent of 255) reach the rows that see them by their weights.
-      const int n = e.length < most ? e.length : most + 1;  // keys there are
-      uint32_t any = 0;
-#pragma unroll
-      for (int i = 0; i < 2 * N; ++i) {
-        const uint32_t y = ~x[i / N].vs.w[i % N];
-        any |= (y - 0x01010101u) & ~y & 0x80808080u;  // a byte of y is 0
-      }
-      if (kStep * s + kStep > n || __builtin_amdgcn_ballot_w64(any != 0)) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int key = kStep * s + (i >> 2) * 16 + kg * 4 + (i & 3);
-          uint32_t nan = 0;
-#pragma unroll
-          for (int g = 0; g < N; ++g) {
-            const int at = (i & 3) * N + g, sh = 8 * (at & 3);
-            nan |= (x[i >> 2].vs.w[at >> 2] >> sh & 255u) == 255u;
-          }
-          const bool gone = key >= n;
-          spoilt |= gone ? 0u : nan << i;
-          if (gone || nan) {
-#pragma unroll
-            for (int g = 0; g < N; ++g) {
-              const int at = (i & 3) * N + g, sh = 8 * (at & 3);
-              uint32_t& word = x[i >> 2].vs.w[at >> 2];
-              word = (word & ~(255u << sh)) | 127u << sh;
-            }
-          }
-        }
-      }
-    }
-    bf16x8 p[QT][WP];
-    auto weigh = [&](int t) INLINE {
-      const float under = weight.under(m[t]);
-      float f[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) f[i] = weight(w[t][i], under);
-      if (EDGE && __builtin_amdgcn_ballot_w64(spoilt != 0)) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] = (spoilt >> i & 1) && w[t][i] != -INFINITY ? __builtin_nanf("") : f[i];
-      }
-      parts<WP>(f, p[t]);
-      floatx4 sum = l[t];
-#pragma unroll
-      for (int k = 0; k < WP; ++k) sum = mfma(ones, p[t][k], sum);
-      return sum;
+    auto spoil = [&]() INLINE {
+      if (kStep * s + kStep <= n && !__builtin_amdgcn_ballot_w64(any_nan(x[0]) || any_nan(x[1]))) return 0u;
+      const uint32_t lo = cleaned(x[0], kStep * s + 4 * kg, n);
+      return lo | cleaned(x[1], kStep * s + 16 + 4 * kg, n) << 4;
     };
-    floatx4 sum[QT];
-    bool fine = s != s0;
-#pragma unroll
-    for (int t = 0; t < QT; ++t) {
-      sum[t] = weigh(t);
-      fine = fine && sum[t][0] <= kMost;
-    }
-    if (__builtin_amdgcn_ballot_w64(!fine)) {
-#pragma unroll
-      for (int t = 0; t < QT; ++t) {
-        float top = m[t];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) top = fmaxf(top, w[t][i]);
-        top = across_rows_max(top);
-        const float f = weight.from(m[t], top);
-        m[t] = top;
-        l[t] *= f;
-#pragma unroll
-        for (int j = 0; j < 2 * N; ++j) o[t][j] *= f;
-        sum[t] = weigh(t);
-      }
-    }
-#pragma unroll
-    for (int t = 0; t < QT; ++t) l[t] = sum[t];
-#pragma unroll
-    for (int g = 0; g < N; ++g) {
-      bf16x8 lo, hi;
-      values(x[0], x[1], g, lo, hi);
-#pragma unroll
-      for (int k = 0; k < WP; ++k)
-#pragma unroll
-        for (int t = 0; t < QT; ++t) {
-          o[t][2 * g] = mfma(lo, p[t][k], o[t][2 * g]);
-          o[t][2 * g + 1] = mfma(hi, p[t][k], o[t][2 * g + 1]);
-        }
-    }
+    mine.template step<decltype(at_edge)::value>(kStep * s, lane, s == s0, [&](int i, int j) INLINE { return x[i].key(j, lane); }, keys_used, spoil,
+                                                 [&](int g, bf16x8& lo, bf16x8& hi) INLINE { values(x[0], x[1], g, lo, hi); });
     values_used();
   };
 
@@ -599,8 +648,8 @@ __global__ __launch_bounds__(kThreads, waves_held(sizeof(IO), D)) void attention
     for (int t = 0; t < QT; ++t) {
       const int row = wave * ROWS + 16 * t + r;
 #pragma unroll
-      for (int j = 0; j < 2 * N; ++j) *reinterpret_cast<floatx4*>(so + row * PITCH + 16 * j + 4 * kg) = o[t][j];
-      if (kg == 0) { sm[row] = m[t]; sl[row] = l[t][0]; }
+      for (int j = 0; j < 2 * N; ++j) *reinterpret_cast<floatx4*>(so + row * PITCH + 16 * j + 4 * kg) = mine.o[t][j];
+      if (kg == 0) { sm[row] = mine.m[t]; sl[row] = mine.l[t][0]; }
     }
     __syncthreads();
     for (int i = threadIdx.x; i < rows * (D / 8); i += kThreads) {
@@ -610,7 +659,7 @@ __global__ __launch_bounds__(kThreads, waves_held(sizeof(IO), D)) void attention
       for (int k = 0; k < kWaves; ++k) to = fmaxf(to, sm[k * ROWS + row]);
 #pragma unroll
       for (int k = 0; k < kWaves; ++k) {
-        const float mk = sm[k * ROWS + row], f = weight.from(mk, to);
+        const float mk = sm[k * ROWS + row], f = mine.weight.from(mk, to);
         sum = fmaf(f, sl[k * ROWS + row], sum);
         Vec<8> v;
         v.load(so + (k * ROWS + row) * PITCH + c);
@@ -645,26 +694,122 @@ __global__ __launch_bounds__(kThreads, waves_held(sizeof(IO), D)) void attention
       }
     }
   } else {
-    float* so = shared + wave * 16 * PITCH;  // a tile of this wave's
-#pragma unroll
-    for (int t = 0; t < QT; ++t) {
-      const float inv = l[t][0] == 0.f ? 0.f : 1.f / l[t][0];
-#pragma unroll
-      for (int j = 0; j < 2 * N; ++j) *reinterpret_cast<floatx4*>(so + r * PITCH + 16 * j + 4 * kg) = o[t][j] * inv;
-      wave_lds_sync();
-      const int left = rows - 16 * t < 16 ? rows - 16 * t : 16;
-      for (int i = lane; i < left * (D / 8); i += 64) {
-        const int row = i / (D / 8), c = (i - row * (D / 8)) * 8;
-        Vec<8> v;
-        v.load(so + row * PITCH + c);
-        const int at_row = row0 + 16 * t + row, tok = a.by_group(at_row);
-        put<IO, FP8>(a, e.first + tok, (h * a.group + at_row - tok * a.group) * D + c, v.e);
-      }
-      wave_lds_sync();
-    }
+    mine.finish(a, e, h, row0, rows, lane, shared + wave * 16 * PITCH);
     x = x1;
   }
   }
+}
+
+// Prompts: each of a workgroup's waves has a tile of rows, and all of them go over the keys together, 64 a step.  Each wave turns one
+// of the step's four records into the products' operands, which all read from LDS: alone, every wave would turn all four.
+// Two buffers: a step's operands are made while the one before is summed, a barrier a step.
+template <typename IO, int D, int QT, bool FP8> __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(AttentionArgs a) {
+  constexpr int N = D / 32, ROWS = 16 * QT, PITCH = D + 4, KEYS = 16 * kWaves;
+  struct Operands { uint4 k[kWaves][N][64], v[kWaves / 2][2 * N][64]; };
+  __shared__ union { Operands x[2]; float so[kWaves * 16 * PITCH]; } shared;
+  __shared__ uint32_t spoil[2][kWaves][4];
+  __shared__ int upto[kThreads];
+  const int lane = threadIdx.x & 63, r = lane & 15, kg = lane >> 4;
+  const int wave = uniform(threadIdx.x >> 6);
+  const int G = a.cache.heads, h = blockIdx.x % G, u = blockIdx.x / G;
+  auto blocks_of = [&](int b) INLINE { return extent<ROWS * kWaves>(a, b).tiles; };
+  if (u >= lay_out(a.tok.seq.batch, blocks_of, upto)) return;
+  int place;
+  const int b = seek(a.tok.seq.batch, blocks_of, upto, u, place);
+  Extent e = extent<ROWS * kWaves>(a, b);
+  e.first = uniform(e.first);
+  e.n = uniform(e.n);
+  e.length = uniform(e.length);
+  e.tiles = uniform(e.tiles);
+  // the last rows see the most keys: they go first
+  const int block0 = (e.tiles - 1 - place) * (ROWS * kWaves), left = e.n * a.group - block0, row0 = block0 + wave * ROWS;
+  const int rows = left - wave * ROWS < ROWS ? left - wave * ROWS : ROWS;
+  const int most = a.tok.columns << (a.cache.shift + 4);
+  auto limit = [&](int row) INLINE {  // the last key that a row sees; of keys past the table one, which reads as NaN
+    const int place = e.length - e.n + a.by_group(row);
+    return place < most ? place : most;
+  };
+  const int low = limit(block0), high = limit(block0 + (left < ROWS * kWaves ? left : ROWS * kWaves) - 1);  // of the workgroup
+  const int mine_high = rows > 0 ? limit(row0 + rows - 1) : -1;
+  Rows<IO, D, QT, FP8> mine(a.scale);
+  mine.start(a, e, h, row0, rows, lane, limit);
+  const int n = e.length < most ? e.length : most + 1;  // keys there are
+  const int steps = high < 0 ? 0 : high / KEYS + 1, whole = low < 0 ? 0 : (low + 1) / KEYS;
+
+  const int32_t* row_of_table = a.tok.table + (size_t)b * a.tok.ld_table;
+  int window = 0, entries = 0;
+  auto look = [&](int j) INLINE {  // 64 entries of the table's row, one a lane
+    window = j;
+    const int at = j + lane;
+    entries = row_of_table[at < a.tok.columns ? at : a.tok.columns - 1];
+    __builtin_amdgcn_s_waitcnt(0x0F70);  // here, where it is rare, and not at every use
+  };
+  Tile<D, false> x;
+  auto load = [&](int s) INLINE {
+    const int t = s * kWaves + wave, tile = t * 16 <= high ? t : high >> 4;  // behind the last key any row sees: that one's record
+    const int j = tile >> a.cache.shift;
+    if (j - window >= 64) look(j);
+    const int page = __builtin_amdgcn_readlane(entries, j - window);
+    const bool good = j < a.tok.columns && (unsigned)page < (unsigned)a.cache.pages;
+    const uint8_t* rec = record<D>(a.cache, good ? page : 0, h, tile);
+    x.load_keys(rec, lane, good ? 0u : 255u);
+    x.load_values(rec, lane);
+  };
+  auto turn = [&](int s) INLINE {
+    Operands& to = shared.x[s & 1];
+    if (s >= whole) {
+      const uint32_t bad = cleaned(x, s * KEYS + wave * 16 + 4 * kg, n);
+      if (r == 0) spoil[s & 1][wave][kg] = bad;
+    }
+#pragma unroll
+    for (int j = 0; j < N; ++j) to.k[wave][j][lane] = __builtin_bit_cast(uint4, x.key(j, lane));
+#pragma unroll
+    for (int g = 0; g < N; ++g) {
+      uint32_t c[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) c[i] = two(x.v.w[g], exponent(x.vs, i * N + g), i);
+      uint2 lo, hi;
+      lo.x = __builtin_amdgcn_perm(c[1], c[0], 0x05040100u);
+      lo.y = __builtin_amdgcn_perm(c[3], c[2], 0x05040100u);
+      hi.x = __builtin_amdgcn_perm(c[1], c[0], 0x07060302u);
+      hi.y = __builtin_amdgcn_perm(c[3], c[2], 0x07060302u);
+      reinterpret_cast<uint2*>(&to.v[wave >> 1][2 * g][lane])[wave & 1] = lo;
+      reinterpret_cast<uint2*>(&to.v[wave >> 1][2 * g + 1][lane])[wave & 1] = hi;
+    }
+  };
+  auto sum = [&](int s, auto at_edge) INLINE {
+    const Operands& from = shared.x[s & 1];
+#pragma unroll
+    for (int p = 0; p < kWaves / 2; ++p) {
+      if (s * KEYS + 32 * p > mine_high) break;
+      mine.template step<decltype(at_edge)::value>(
+          s * KEYS + 32 * p, lane, s == 0 && p == 0, [&](int i, int j) INLINE { return __builtin_bit_cast(bf16x8, from.k[2 * p + i][j][lane]); }, [] {},
+          [&]() INLINE { return spoil[s & 1][2 * p][kg] | spoil[s & 1][2 * p + 1][kg] << 4; },
+          [&](int g, bf16x8& lo, bf16x8& hi) INLINE {
+            lo = __builtin_bit_cast(bf16x8, from.v[p][2 * g][lane]);
+            hi = __builtin_bit_cast(bf16x8, from.v[p][2 * g + 1][lane]);
+          });
+    }
+  };
+  if (steps > 0) {
+    look(0);
+    load(0);
+    turn(0);
+    load(steps > 1 ? 1 : 0);
+    lds_barrier();
+    int s = 0;
+    auto one = [&](auto at_edge) INLINE {
+      if (s + 1 < steps) {
+        turn(s + 1);
+        load(s + 2 < steps ? s + 2 : s + 1);
+      }
+      sum(s, at_edge);
+      lds_barrier();
+    };
+    for (; s < whole && s < steps; ++s) one(std::false_type{});
+    for (; s < steps; ++s) one(std::true_type{});
+  }
+  if (rows > 0) mine.finish(a, e, h, row0, rows, lane, shared.so + wave * 16 * PITCH);
 }
 
 // Joins what workgroups left of a tile.  A token's rows of a key head are pieces of 8 channels; a workgroup has `span`
@@ -801,7 +946,8 @@ template <typename IO, int D, bool FP8> int launch(const AttentionArgs& a, hipSt
   constexpr int QT = most_tiles_held(sizeof(IO), D, false);
   const int64_t workgroups = most_tiles(batch, tokens, a.group, 16 * QT * kWaves) * G;
   if (!fits(workgroups, kThreads)) return -3;
-  hipLaunchKernelGGL((attention_kernel<IO, D, QT, false, FP8, false>), dim3((unsigned)workgroups), dim3(kThreads), 0, s, a);
+  if constexpr (sizeof(IO) == 2 && D <= 128) hipLaunchKernelGGL((prompt_kernel<IO, D, QT, FP8>), dim3((unsigned)workgroups), dim3(kThreads), 0, s, a);
+  else hipLaunchKernelGGL((attention_kernel<IO, D, QT, false, FP8, false>), dim3((unsigned)workgroups), dim3(kThreads), 0, s, a);
   return 0;
 }
 
