@@ -51,8 +51,8 @@ size_t sketchssm_cache_bytes(const skssm_cache* cache); /* 0: not a cache (sketc
  * lengths [batch]: tokens of the sequence with the new ones, so that its i-th of n new
  * tokens has the place lengths[b] - n + i; a token at a place below 0 is a
  * padding row: it is not appended and its attention is 0.  table [batch][columns] (rows ld_table
- * apart): the page that holds places page j .. page (j + 1) - 1 of sequence b at [b][j]; only entries
- * that lengths reach are read.  All int32, on the device.  A place whose page
+ * apart): the page that holds places page j .. page (j + 1) - 1 of sequence b at [b][j]; entries that lengths do not reach may
+ * hold anything.  All int32, on the device.  A place whose page
  * is not in 0..pages-1 or past `columns` is not written by the append and reads as NaN.
  */
 typedef struct {
@@ -120,10 +120,10 @@ int sketchssm_cache_read(const skssm_cache* cache, const skssm_new_tokens* seq, 
  * Scores, softmax statistics and sums are fp32.  Keys and values enter the products as they
  * are; with bf16 io the weights e^(s - max) are rounded to bf16 (their sum is that of the
  * rounded ones), with F32 io queries and weights keep 24 bits.
- * scale > 0.  A NaN reaches only outputs of its head whose token sees it.
+ * scale is from 2^-96 to 2^96.  A NaN reaches only outputs of its head whose token sees it.
  *
  * workspace: sketchssm_attention_workspace bytes (may be 0), where a sequence
- * is split over workgroups; its contents need not be kept.
+ * is split over workgroups; its contents need not be kept, and calls that may run at the same time need one each.
  */
 typedef struct {
   int32_t io_dtype, out_dtype, heads;

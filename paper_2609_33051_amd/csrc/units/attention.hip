@@ -474,7 +474,7 @@ template <int D, bool NT> __device__ __forceinline__ bool any_nan(const Tile<D, 
 
 // Tiles of rows that a wave takes at most, and waves a SIMD that its registers are held to.
 constexpr int most_tiles_held(size_t io, int D, bool split) {
-  return io == 4 ? (D > 96 ? 1 : 2) : D == 256 || (split && D == 192) ? 1 : !split && D == 96 ? 3 : 2;
+  return io == 4 ? (D > (split ? 64 : 96) ? 1 : 2) : D == 256 || (split && D == 192) ? 1 : !split && D == 96 ? 3 : 2;
 }
 constexpr int waves_held(size_t io, int D) { return io == 4 && D == 256 ? 1 : 2; }
 

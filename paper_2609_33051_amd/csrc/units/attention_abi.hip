@@ -2,8 +2,6 @@
 // and the kernels' argument blocks.
 #include "../../../include/sketchssm_attention.h"
 
-#include <cmath>
-
 #include "../attention.h"
 #include "../checks.h"
 
@@ -245,7 +243,7 @@ int sketchssm_attention(const skssm_cache* cache, const skssm_new_tokens* seq, c
   const bool fp8 = p.out_dtype == SKSSM_E4M3;
   if ((seq->tokens + 1) * (int64_t)p.heads > (int64_t)1 << 30) return fail(SKSSM_EUNSUPPORTED, "%s: %lld tokens of %d heads: at most 2^30 rows", what, (long long)seq->tokens, p.heads);
   if (p.heads < 1 || p.heads % cache->kv_heads) return fail(SKSSM_EINVAL, "%s: %d key heads do not divide %d heads", what, cache->kv_heads, p.heads);
-  if (!(p.scale > 0.f) || !std::isfinite(p.scale)) return fail(SKSSM_EINVAL, "%s: scale must be > 0 and finite", what);
+  if (!(p.scale >= 0x1p-96f && p.scale <= 0x1p96f)) return fail(SKSSM_EINVAL, "%s: scale %g outside 2^-96..2^96", what, (double)p.scale);
   const int64_t T = seq->tokens, D = cache->dim, H = p.heads;
   if (fp8 && D % 128 && (D != 64 || (H / cache->kv_heads) % 2))
     return fail(SKSSM_EUNSUPPORTED, "%s: E4M3 with %lld channels and %lld heads a key head: blocks of 128 columns lie in one key head's", what, (long long)D,
@@ -262,9 +260,11 @@ int sketchssm_attention(const skssm_cache* cache, const skssm_new_tokens* seq, c
     return fail(SKSSM_EINVAL, "%s: workspace of %zu bytes, %zu needed", what, p.workspace ? p.workspace_bytes : (size_t)0, need);
   const size_t no = span(T, p.ld_out, H * D, eo), ns = fp8 ? span(H * D / 128, p.ld_scales, T, 4) : 0;
   const Range out[] = {{p.out, no}, {p.scales, ns}, {p.workspace, need}};
-  const Range in[] = {{p.q, nq}, {cache->data, cache_bytes(cache)}, {seq->offsets, ((size_t)seq->batch + 1) * 4}, {seq->lengths, (size_t)seq->batch * 4},
+  const Range beside[] = {out[1], out[2]};  // out itself may lie between q's rows
+  const Range queries[] = {{p.q, nq}};
+  const Range in[] = {{cache->data, cache_bytes(cache)}, {seq->offsets, ((size_t)seq->batch + 1) * 4}, {seq->lengths, (size_t)seq->batch * 4},
                       {seq->table, table_bytes(seq)}};
-  if (any_overlap(out, in)) return fail(SKSSM_EINVAL, "%s: an output overlaps an input", what);
+  if (any_overlap(out, in) || any_overlap(beside, queries) || rows_overlap(p.out, H * D * eo, p.ld_out * eo, p.q, ((H - 1) * p.q_head + D) * e, p.ldq * e, T)) return fail(SKSSM_EINVAL, "%s: an output overlaps an input", what);
   if ((ns && overlap(p.out, no, p.scales, ns)) || (need && (overlap(p.out, no, p.workspace, need) || (ns && overlap(p.scales, ns, p.workspace, need)))))
     return fail(SKSSM_EINVAL, "%s: the outputs overlap", what);
   if (T == 0) return fail(SKSSM_OK, "%s", "");  // nothing to do: no launch, no error

@@ -369,3 +369,92 @@ def test_many_sequences(io, B, longest, H, G, D):
     lengths = [int(x) for x in torch.randint(0, longest + 1, (B,), generator=g)]
     new = [min(1, n) for n in lengths] if B != 130 else [min(n, int(x)) for n, x in zip(lengths, torch.randint(0, 4, (B,), generator=g))]
     check(io, H, G, D, 16, new, lengths, seed=B)
+
+
+@pytest.mark.parametrize("io,D,H,G", [("bf16", 128, 32, 8), ("bf16", 96, 64, 16), ("f32", 128, 32, 16), ("bf16", 256, 16, 8)])
+def test_padding_rows_of_prompts(io, D, H, G):
+    """Places below 0 among rows enough for a workgroup of them a CU: zeros, and the rows behind them as without."""
+    case("padding of prompts", io, D, H, G)
+    dt, r = DT[io], rnd(D)
+    lengths, pad = [1300, 700], [37, 1000]
+    cache, tab, ln, ks, vs = built(r, lengths, G, D, 64, dt)
+    q = r((sum(lengths) + sum(pad), H, D), dt)
+    n = [a + b for a, b in zip(lengths, pad)]
+    got, _ = ops.attention(cache, tab, ln, q, offsets=R.offsets(n))
+    at = 0
+    for b in range(2):
+        assert not bool(got[at:at + pad[b]].any())
+        o, mag, most = R.attention(q[at + pad[b]:at + n[b]], ks[b], vs[b], lengths[b], D ** -0.5)
+        R.close(got[at + pad[b]:at + n[b]], o, R.bound(o, mag, most, lengths[b], D, dt), f"sequence {b}")
+        at += n[b]
+
+
+def test_a_cache_past_4_gib():
+    """Pages whose bytes lie past 2^32 of the cache's start, written, read and attended to."""
+    case("4 GiB")
+    r, G, D, page, pages = rnd(6), 8, 256, 1024, 2100
+    cache = torch.empty((pages, G, page // 16, 17 * D), dtype=torch.uint8, device="cuda")
+    assert cache.numel() > 1 << 32
+    lengths, new = [1500, 40], [1500, 40]
+    tab = i32([[2099, 2050], [2098, -1]])
+    k, v, q = r((1540, G, D), torch.bfloat16), r((1540, G, D), torch.bfloat16), r((1540, G, D), torch.bfloat16)
+    ops.cache_append(cache, tab, i32(lengths), k, v, offsets=R.offsets(new))
+    a, b = ops.cache_read(cache, tab, i32(lengths), 1540, offsets=R.offsets(new))
+    hk, hv = R.held(k), R.held(v)
+    assert same(a, hk) and same(b, hv)
+    one, _ = ops.attention(cache, tab, i32(lengths), q[[1499, 1539]])
+    for got, rows in ((ops.attention(cache, tab, i32(lengths), q, offsets=R.offsets(new))[0], None), (one, True)):
+        for s, at, L in ((0, 0, 1500), (1, 1500, 40)):
+            qs = q[at:at + L] if rows is None else q[at + L - 1:at + L]
+            g = got[at:at + L] if rows is None else got[s:s + 1]
+            o, mag, most = R.attention(qs, hk[at:at + L], hv[at:at + L], qs.shape[0], D ** -0.5)
+            R.close(g, o, R.bound(o, mag, most, L, D, torch.bfloat16), f"sequence {s}")
+
+
+def test_outputs_between_the_queries_rows():
+    """Queries turned, and outputs written, where others' rows lie between; the same on a table with unused columns of anything."""
+    case("between")
+    r, H, G, D = rnd(12), 4, 2, 64
+    lengths = [30, 5]
+    cache, tab, ln, ks, vs = built(r, lengths, G, D, 16, torch.bfloat16)
+    wide = r((35, 2 * H * D), torch.bfloat16)
+    q, out = wide[:, :H * D].unflatten(1, (H, D)), wide[:, H * D:].unflatten(1, (H, D))
+    want, _ = ops.attention(cache, tab, ln, q.clone(), offsets=R.offsets(lengths))
+    ops.attention(cache, tab, ln, q, offsets=R.offsets(lengths), out=out)
+    assert torch.equal(out, want)
+    more = torch.full((2, 200), -(1 << 31), dtype=torch.int32, device="cuda")
+    more[:, :tab.shape[1]] = tab
+    assert torch.equal(ops.attention(cache, more, ln, wide[:, :H * D].unflatten(1, (H, D)), offsets=R.offsets(lengths))[0], want)
+
+
+def test_refused_before_any_launch():
+    """What the calls on tensors refuse: wrong types, shapes, devices and layouts."""
+    case("refusals")
+    r = rnd(1)
+    tab, pool = R.table([20], 16)
+    cache = ops.new_cache(pool, 2, 16, 64)
+    k, q, ln = r((20, 2, 64), torch.bfloat16), r((20, 4, 64), torch.bfloat16), i32([20])
+    ang = R.angles(20, 64)
+    good = dict(cache=cache, table=tab, lengths=ln)
+    for kw in (dict(cache=cache.float()), dict(cache=cache[..., :-1]), dict(cache=cache.cpu()), dict(cache=cache[:, :, :, ::2]), dict(table=tab.long()), dict(table=tab.cpu()),
+               dict(table=tab[0]), dict(lengths=ln.long()), dict(lengths=i32([20, 1])), dict(offsets=R.offsets([20]).long()), dict(offsets=R.offsets([10, 10]))):
+        with pytest.raises(ValueError):
+            ops.attention(*{**good, **{x: y for x, y in kw.items() if x != "offsets"}}.values(), q, offsets=kw.get("offsets"))
+        with pytest.raises(ValueError):
+            ops.cache_append(*{**good, **{x: y for x, y in kw.items() if x != "offsets"}}.values(), k, k, offsets=kw.get("offsets"))
+        with pytest.raises(ValueError):
+            ops.cache_read(*{**good, **{x: y for x, y in kw.items() if x != "offsets"}}.values(), 20, offsets=kw.get("offsets"))
+    for f in (lambda: ops.attention(cache, tab, ln, q.half()), lambda: ops.attention(cache, tab, ln, q[..., :32]), lambda: ops.attention(cache, tab, ln, q.cpu()),
+              lambda: ops.attention(cache, tab, ln, q.transpose(1, 2)), lambda: ops.attention(cache, tab, ln, q, out=q[:, :2]), lambda: ops.attention(cache, tab, ln, q[0]),
+              lambda: ops.attention(cache, tab, ln, q, scales=torch.zeros(2, 20, device="cuda")), lambda: ops.attention(cache, tab, ln, q, out=torch.zeros_like(q).float()),
+              lambda: ops.cache_append(cache, tab, ln, k, k[:, :1]), lambda: ops.cache_append(cache, tab, ln, k, k.float()), lambda: ops.cache_append(cache, tab, ln, k, k, q=q),
+              lambda: ops.cache_append(cache, tab, ln, k, k, positions=i32(list(range(20)))), lambda: ops.cache_append(cache, tab, ln, k, k, q_out=q),
+              lambda: ops.cache_append(cache, tab, ln, k, k, rotation=ang, positions=i32([0, 1])), lambda: ops.cache_append(cache, tab, ln, k, k, rotation=ang.double()),
+              lambda: ops.cache_read(cache, tab, ln, 20, dtype=torch.float16), lambda: ops.cache_read(cache, tab, ln, 20, k=q), lambda: ops.rotary(q, ang[0]),
+              lambda: ops.rotary(q, ang, positions=i32([1])), lambda: ops.rotary(q[0], ang), lambda: ops.rotary(q, ang, out=q[:, :, :32])):
+        with pytest.raises(ValueError):
+            f()
+    for f in (lambda: ops.attention(cache, tab, ln, q, scale=-1.0), lambda: ops.attention(cache, tab, ln, q[:, :3]), lambda: ops.rotary(q, R.angles(20, 66)),
+              lambda: ops.rotary(q[:, :2], ang, out=q[:, 1:3]), lambda: ops.attention(cache, tab, ln, q, scale=float("inf")), lambda: ops.new_cache(4, 2, 24, 64), lambda: ops.new_cache(4, 2, 16, 80)):
+        with pytest.raises(B.SketchSSMError):
+            f()
