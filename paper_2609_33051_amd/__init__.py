@@ -7,6 +7,8 @@ Submodules:
   ops      -- the operators around the recurrence of a Mamba-2 mixer layer: conv,
               conv_token, scan, norm and matmul_fp8 on torch tensors
   mixer    -- such a layer served end to end: prompts, then single tokens
+  attention -- a softmax attention layer between mixer layers, over a paged cache in 4 bits (its
+              operators in ops: rotary, cache_append, cache_read and attention)
   inputs   -- seeded synthetic workloads
   traffic  -- byte accounting (the paper's model and this implementation's)
 

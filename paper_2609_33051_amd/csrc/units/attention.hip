@@ -9,8 +9,12 @@
 // keys are summed is free, and the cache's records hold the values in the order it leaves).  Nothing passes
 // through LDS.  A row of ones beside V^T sums the weights as the products see them.
 //
-// The maximum that the weights are taken over moves only where a score is past it by more than 2^8; until
-// then nothing is rescaled.
+// The maximum that the weights are taken over moves only where the weights' sum has grown past 2^16; until then no score is compared with
+// another and nothing is rescaled (one prompt of 8192 tokens, with the registers that this frees: 2000 -> 607 us).
+//
+// Single tokens are bound by the cache's bytes: 64 over contexts of up to 8192, 32 heads on 8 of 128 channels, in 56 us (5.9 TB/s; the loads alone take as
+// long), one over 131072 keys in 26 (5.5).  Prompts are bound by the vector units (exponentials, the cache's conversion) and
+// the matrix units, which hardly overlap: one of 8192 tokens in 526 to 543 us, 1.0 PFLOP/s.
 #include <type_traits>
 
 #include "../attention.h"
@@ -885,7 +889,16 @@ int64_t most_tiles(int batch, int tokens, int group, int rows) {
 }
 // The plan that join_kernel reads: rounds a workgroup has, then those before each sequence.
 int64_t plan_words(int batch) { return ((int64_t)batch + 1 + 3) / 4 * 4; }
-// Whether keys are split: not where the sequences' rows mostly fill the four waves' tiles of a workgroup, 128 rows, and there
+// Whether keys are split, by the rows that a sequence has on average, the workgroups of 128 rows that they would fill and the keys that the
+// table has room for.  In us, split and by rows: one prompt of 128 tokens 6.3 and 9.2, of 256 11.8 and 12.4, of 512 26 and 19, of 2048 105 and 62, 100 prompts of 20 tokens 32 and 18; 64 requests of
+// 16 tokens over up to 4000 keys 119 and 115, of 1000 71 and 41; 128 of 8 tokens (32 rows) 96 and 147, 65 and 52; few workgroups over many keys: 512
+// tokens over 1024 keys 23 and 30, over 4096 52 and 101, 1024 over 4096 96 and 103, 4 x 256 over 16000 270 and 421.
+bool splits(int batch, int tokens, int group, int G, int64_t capacity) {
+  const int64_t rows = (int64_t)tokens * group / batch, workgroups = (int64_t)batch * ((rows + 127) / 128) * G;
+  if (rows < (capacity > 1024 ? 64 : 32)) return true;
+  const int64_t enough = capacity / 4 < kCUs / 2 ? kCUs / 2 : capacity / 4 < 2 * kCUs ? capacity / 4 : 2 * kCUs;
+  return workgroups < enough;
+}
 // are workgroups for twice the CUs.
 bool splits(int batch, int tokens, int group, int G) {
   const int64_t rows = (int64_t)tokens * group;
@@ -903,18 +916,19 @@ int shares(int batch, int tokens, int group, int G, int D, int QT, int64_t capac
   return (int)(n < most ? n : most);
 }
 
-// Tiles of rows a wave: two where the sequences' rows fill them and there is more than a few rounds of work for every workgroup; with less,
-// what counts is the time of one.
+// Tiles of rows a wave: two where the sequences' rows fill them and there is more than a round or so of work for every workgroup; with less, what
+// counts is the time of one.  In us, one tile and two: a prompt of 128 tokens 6.3 and 7.7, of 256 11.8 and 15.7, 4 of 100 behind 900 32.6 and 33.0,
+// behind 7900 90 and 73, one of 512 behind 512 35 and 23.
 int split_tiles(int batch, int tokens, int group, int G, int64_t capacity) {
   return (int64_t)tokens * group > (int64_t)16 * batch && most_rounds(batch, tokens, group, 2, capacity) * G > 16 * kCUs ? 2 : 1;
 }
 
 template <typename IO, int D, bool FP8> int launch(const AttentionArgs& a, hipStream_t s) {
   const int batch = a.tok.seq.batch, tokens = a.tok.seq.tokens, G = a.cache.heads;
-  if (splits(batch, tokens, a.group, G)) {
+  const int64_t capacity = (int64_t)a.tok.columns << (a.cache.shift + 4);
+  if (splits(batch, tokens, a.group, G, capacity)) {
     auto run = [&](auto qt) {
       constexpr int QT = decltype(qt)::value;
-      const int64_t capacity = (int64_t)a.tok.columns << (a.cache.shift + 4);
       AttentionArgs b = a;
       b.share = shares(batch, tokens, a.group, G, D, QT, capacity);
       const int64_t workgroups = (int64_t)b.share * G;
@@ -940,7 +954,7 @@ template <typename IO, int D, bool FP8> int launch(const AttentionArgs& a, hipSt
       return 0;
     };
     if constexpr (most_tiles_held(sizeof(IO), D, true) > 1)
-      if (split_tiles(batch, tokens, a.group, G, (int64_t)a.tok.columns << (a.cache.shift + 4)) == 2) return run(std::integral_constant<int, 2>{});
+      if (split_tiles(batch, tokens, a.group, G, capacity) == 2) return run(std::integral_constant<int, 2>{});
     return run(std::integral_constant<int, 1>{});
   }
   constexpr int QT = most_tiles_held(sizeof(IO), D, false);
@@ -980,7 +994,7 @@ int run_attention(const AttentionArgs& a, int D, int io, bool fp8, void* stream)
 size_t attention_workspace(int batch, int tokens, int H, int G, int D, int columns, int page) {
   const int group = H / G;
   const int64_t capacity = (int64_t)columns * page;
-  if (!splits(batch, tokens, group, G) || capacity <= kStep * kWaves) return 0;
+  if (!splits(batch, tokens, group, G, capacity) || capacity <= kStep * kWaves) return 0;
   size_t most = 0;  // whichever tiles the type's kernel takes
   for (int QT = 1; QT <= 2; ++QT) {
     const size_t n = (size_t)shares(batch, tokens, group, G, D, QT, capacity) * G * 2 * (16 * QT) * (D + 2) * 4;
