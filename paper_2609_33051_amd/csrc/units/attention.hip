@@ -326,8 +326,8 @@ template <typename IO, int D, int QT, bool FP8> struct Rows {
   }
 
   // Keys first .. first + 31, of two records: keys(i, j) are channels 8 j .. (of a lane's quarter) of record i's, values(g, lo, hi) block g of
-  // both records' values.  EDGE: some row does not see all of them; spoilt() then has bit i of a lane's eight keys for values that are not
-  // numbers.  fresh: these are the first keys.  used: called when keys have been read.
+  // both records' values.  EDGE: some row does not see all of them; spoil() then has bit i of a lane's eight keys for values that are not
+  // finite.  fresh: these are the first keys.  used: called when keys have been read.
   template <bool EDGE, typename K, typename U, typename S, typename V>
   __device__ __forceinline__ void step(int first, int lane, bool fresh, K keys, U used, S spoil, V values) {
     const int kg = lane >> 4;
@@ -438,9 +438,9 @@ template <typename IO, int D, int QT, bool FP8> struct Rows {
   }
 };
 
-// Zero weights may meet nothing but numbers: what lies behind the sequence (key >= n) may be anything, and values that are not numbers (an
-// exponent of 255) are to reach the rows that see them by their weights.  Takes both out of the values of a lane's four tokens from
-// `key`; bit i of the result: token i's were not numbers.
+// Zero weights may meet nothing but numbers: what lies behind the sequence (key >= n) may be anything, and values that are not finite (an
+// exponent of 255; of 252 to 254 only where nothing was appended) are to reach the rows that see them by their weights.  Takes both out of the
+// values of a lane's four tokens from `key`; bit i of the result: token i's were not finite.
 template <int D, bool NT> __device__ __forceinline__ uint32_t cleaned(Tile<D, NT>& x, int key, int n) {
   constexpr int N = D / 32;
   uint32_t spoilt = 0;
@@ -450,7 +450,7 @@ template <int D, bool NT> __device__ __forceinline__ uint32_t cleaned(Tile<D, NT
 #pragma unroll
     for (int g = 0; g < N; ++g) {
       const int at = i * N + g, sh = 8 * (at & 3);
-      nan |= (x.vs.w[at >> 2] >> sh & 255u) == 255u;
+      nan |= (x.vs.w[at >> 2] >> sh & 255u) >= 252u;
     }
     const bool gone = key + i >= n;
     spoilt |= gone ? 0u : nan << i;
@@ -465,12 +465,12 @@ template <int D, bool NT> __device__ __forceinline__ uint32_t cleaned(Tile<D, NT
   }
   return spoilt;
 }
-// Whether a byte of a lane's exponents is 255.
+// Whether a byte of a lane's exponents is 252 or more.
 template <int D, bool NT> __device__ __forceinline__ bool any_nan(const Tile<D, NT>& x) {
   uint32_t any = 0;
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) {
-    const uint32_t y = ~x.vs.w[i];
+    const uint32_t y = ~x.vs.w[i] & 0xFCFCFCFCu;
     any |= (y - 0x01010101u) & ~y & 0x80808080u;  // a byte of y is 0
   }
   return any != 0;

@@ -319,6 +319,35 @@ def test_not_numbers_stay_where_they_are_seen(io):
         assert torch.equal(torch.isnan(ops.attention(cache, tab, i32([L]), q2)[0])[8:40], bad[8:40])
 
 
+@pytest.mark.parametrize("fill", [252, 254, 255])
+@pytest.mark.parametrize("io,D,H,G,new,before", [("bf16", 128, 4, 2, [5, 1], [30, 17]), ("bf16", 128, 32, 8, [1100, 900], [5, 0]), ("bf16", 64, 64, 16, [700, 333], [0, 77]),
+                                                 ("f32", 96, 32, 16, [2100], [3]), ("bf16", 256, 16, 16, [900, 3200], [10, 0])])
+def test_anything_behind_a_sequence(fill, io, D, H, G, new, before):
+    """Bytes that were never appended, with the largest exponents, infinities and NaN, behind the last token and in its page."""
+    case("behind", fill, io, D, H, G, new, before)
+    check(io, H, G, D, 32, new, [a + b for a, b in zip(new, before)], fill=fill, seed=fill)
+
+
+@pytest.mark.parametrize("H,G,n", [(4, 2, 40), (32, 16, 2100)])
+def test_a_page_that_is_not_there(H, G, n):
+    """Rows before its first place are as they are, whatever bytes the cache begins with; the others are NaN."""
+    case("no page", H, G, n)
+    r = rnd(n)
+    for fill in (0, 254):
+        cache, tab, ln, ks, vs = built(r, [n], G, 128, 16, torch.bfloat16, fill=fill)
+        k0 = torch.full_like(cache[0], fill)
+        spare = [p for p in range(cache.shape[0]) if p not in tab.tolist()[0]][0]
+        cache[spare] = cache[0]  # page 0 holds bytes that were never appended
+        tab[tab == 0] = spare
+        cache[0] = k0
+        tab[0, 1] = -1  # places 16 .. 31
+        q = r((n, H, 128), torch.bfloat16)
+        got, _ = ops.attention(cache, tab, ln, q, offsets=R.offsets([n]))
+        o, mag, most = R.attention(q[:16], ks[0][:16], vs[0][:16], 16, 128 ** -0.5)
+        R.close(got[:16], o, R.bound(o, mag, most, 16, 128, torch.bfloat16), "before")
+        assert bool(torch.isnan(got[16:]).all())
+
+
 def test_equal_calls_and_equal_forms():
     """Equal calls give equal bits; offsets of ones are no offsets; a token's output does not hang on who shares its call."""
     case("equal")
