@@ -29,6 +29,7 @@ constexpr int kWaves = 4, kThreads = 64 * kWaves;
 constexpr int kStep = 32;         // keys a step
 constexpr float kMost = 65536.f;  // sum of weights from which on the maximum is taken again
 constexpr int kCUs = 256;
+constexpr int kApart = 8;
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
@@ -247,6 +248,10 @@ template <typename F> __device__ __forceinline__ int seek(int batch, F weight, c
 // whatever tiles they are of.  A tile that one workgroup has whole is written by it; of others it leaves the sums
 // in one of its two slots, the second where the tile begins behind the workgroup's own first round.
 __device__ __forceinline__ int rounds(const Extent& e) { return e.steps <= kWaves ? 1 : (e.steps + kWaves - 1) / kWaves; }
+//
+// Where there are no more tiles than workgroups and the longest is not much longer than an even share, every tile is one workgroup's: a share
+// that ends inside a tile costs a second start and the join of its parts, some kApart rounds (us, even shares and whole
+// tiles: 256 requests of up to 1500 keys, 2 key heads of 256 channels 42.7 and 34.4, of up to 1000, 128 channels 23.3 and 19.6; 64 of 1500, 8 key heads 24.0 and 22.1).
 template <int ROWS> struct Rounds {
   const AttentionArgs& a;
   __device__ __forceinline__ int operator()(int b) const {
@@ -254,6 +259,28 @@ template <int ROWS> struct Rounds {
     return e.tiles * rounds(e);
   }
 };
+template <int ROWS> struct Tiles {
+  const AttentionArgs& a;
+  __device__ __forceinline__ int operator()(int b) const { return extent<ROWS>(a, b).tiles; }
+};
+// The most rounds of a tile, over all sequences.
+template <int ROWS> __device__ __forceinline__ int longest(const AttentionArgs& a) {
+  __shared__ int most[kWaves];
+  int x = 0;
+  for (int b = threadIdx.x; b < a.tok.seq.batch; b += kThreads) {
+    const Extent e = extent<ROWS>(a, b);
+    x = e.tiles > 0 && rounds(e) > x ? rounds(e) : x;
+  }
+  for (int d = 1; d < 64; d *= 2) {
+    const int y = __shfl_xor(x, d);
+    x = y > x ? y : x;
+  }
+  if ((threadIdx.x & 63) == 0) most[threadIdx.x >> 6] = x;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) x = most[w] > x ? most[w] : x;
+  return uniform(x);
+}
 
 // ---- outputs
 
@@ -499,13 +526,26 @@ __global__ __launch_bounds__(kThreads, waves_held(sizeof(IO), D)) void attention
   auto blocks_of = [&](int b) INLINE { return extent<ROWS * kWaves>(a, b).tiles; };
   int x = u, x1 = u + 1, each = 1, place = 0, total;
   int b;
+  bool entire = false;
   if constexpr (SPLIT) {
     total = lay_out(batch, weight_of, upto);
     each = (int)(((uint32_t)total + a.share - 1) / a.share);
+    if (batch > 1 && batch <= a.share && longest<ROWS>(a) <= each + kApart) {  // as many tiles as there are rows for
+      __syncthreads();
+      const int tiles = lay_out(batch, Tiles<ROWS>{a}, upto);
+      entire = tiles <= a.share;
+      if (entire) {
+        total = tiles;
+        each = 1;
+      } else {
+        __syncthreads();
+        lay_out(batch, weight_of, upto);
+      }
+    }
     x = u * each;
     x1 = total - x < each ? total : x + each;
     if (a.plan && blockIdx.x == 0) {  // for join_kernel
-      if (threadIdx.x == 0) a.plan[0] = each;
+      if (threadIdx.x == 0) a.plan[0] = entire ? 1 << 30 : each;  // nothing ends inside a tile
       const int run = (batch + kThreads - 1) / kThreads;
       int before = batch == 1 || threadIdx.x == 0 ? 0 : upto[threadIdx.x - 1];
       for (int i = threadIdx.x * run; i < (int)(threadIdx.x + 1) * run && i < batch; ++i) {
@@ -514,7 +554,7 @@ __global__ __launch_bounds__(kThreads, waves_held(sizeof(IO), D)) void attention
       }
     }
     if (x >= total) return;
-    b = seek(batch, weight_of, upto, x, place);
+    b = entire ? seek(batch, Tiles<ROWS>{a}, upto, x, place) : seek(batch, weight_of, upto, x, place);
   } else {
     total = lay_out(batch, blocks_of, upto);
     if (x >= total) return;
@@ -530,8 +570,8 @@ __global__ __launch_bounds__(kThreads, waves_held(sizeof(IO), D)) void attention
   e.steps = uniform(e.steps);
   const int all = rounds(e);
   // the last rows see the most keys: they go first
-  const int tile = SPLIT ? place / all : ((e.tiles + kWaves - 1) / kWaves - 1 - place) * kWaves + wave;
-  const int r0 = SPLIT ? place - tile * all : 0, r1 = SPLIT && x1 - x < all - r0 ? r0 + x1 - x : all;
+  const int tile = entire ? place : SPLIT ? place / all : ((e.tiles + kWaves - 1) / kWaves - 1 - place) * kWaves + wave;
+  const int r0 = SPLIT && !entire ? place - tile * all : 0, r1 = SPLIT && !entire && x1 - x < all - r0 ? r0 + x1 - x : all;
   const bool whole_tile = !SPLIT || (r0 == 0 && r1 == all);
   const int row0 = tile * ROWS, rows = e.n * a.group - row0 < ROWS ? e.n * a.group - row0 : ROWS;
   if (!SPLIT && rows <= 0) return;
@@ -686,7 +726,7 @@ __global__ __launch_bounds__(kThreads, waves_held(sizeof(IO), D)) void attention
         }
       }
     }
-    x += r1 - r0;
+    x += entire ? 1 : r1 - r0;
     place += r1 - r0;
     if (x < x1) {
       __syncthreads();  // `shared` is written again
