@@ -12,9 +12,10 @@
 // The maximum that the weights are taken over moves only where the weights' sum has grown past 2^16; until then no score is compared with
 // another and nothing is rescaled (one prompt of 8192 tokens, with the registers that this frees: 2000 -> 607 us).
 //
-// Single tokens are bound by the cache's bytes: 64 over contexts of up to 8192, 32 heads on 8 of 128 channels, in 56 us (5.9 TB/s; the loads alone take as
-// long), one over 131072 keys in 26 (5.5).  Prompts are bound by the vector units (exponentials, the cache's conversion) and
-// the matrix units, which hardly overlap: one of 8192 tokens in 526 to 543 us, 1.0 PFLOP/s.
+// Single tokens are bound by the cache's bytes: 64 over contexts of up to 8192, 32 heads on 8 of 128 channels, in 56
+// us (5.9 TB/s; the loads alone take as long), one over 131072 keys in 26 (5.5).  Prompts are bound by the vector
+// units (exponentials, the cache's conversion) and the matrix units, which hardly overlap: one of 8192 tokens in 526
+// to 543 us, 1.0 PFLOP/s.
 #include <type_traits>
 
 #include "../attention.h"
@@ -249,9 +250,10 @@ template <typename F> __device__ __forceinline__ int seek(int batch, F weight, c
 // in one of its two slots, the second where the tile begins behind the workgroup's own first round.
 __device__ __forceinline__ int rounds(const Extent& e) { return e.steps <= kWaves ? 1 : (e.steps + kWaves - 1) / kWaves; }
 //
-// Where there are no more tiles than workgroups and the longest is not much longer than an even share, every tile is one workgroup's: a share
-// that ends inside a tile costs a second start and the join of its parts, some kApart rounds (us, even shares and whole
-// tiles: 256 requests of up to 1500 keys, 2 key heads of 256 channels 42.7 and 34.4, of up to 1000, 128 channels 23.3 and 19.6; 64 of 1500, 8 key heads 24.0 and 22.1).
+// Where there are no more tiles than workgroups and the longest is not much longer than an even share, every tile is
+// one workgroup's: a share that ends inside a tile costs a second start and the join of its parts, some kApart rounds
+// (us, even shares and whole tiles: 256 requests of up to 1500 keys, 2 key heads of 256 channels 42.7 and 34.4, of up
+// to 1000, 128 channels 23.3 and 19.6; 64 of 1500, 8 key heads 24.0 and 22.1).
 template <int ROWS> struct Rounds {
   const AttentionArgs& a;
   __device__ __forceinline__ int operator()(int b) const {
@@ -352,9 +354,10 @@ template <typename IO, int D, int QT, bool FP8> struct Rows {
     }
   }
 
-  // Keys first .. first + 31, of two records: keys(i, j) are channels 8 j .. (of a lane's quarter) of record i's, values(g, lo, hi) block g of
-  // both records' values.  EDGE: some row does not see all of them; spoil() then has bit i of a lane's eight keys for values that are not
-  // finite.  fresh: these are the first keys.  used: called when keys have been read.
+  // Keys first .. first + 31, of two records: keys(i, j) are channels 8 j .. (of a lane's quarter) of record i's,
+  // values(g, lo, hi) block g of both records' values.  EDGE: some row does not see all of them; spoil() then has
+  // bit i of a lane's eight keys for values that are not finite.  fresh: these are the first keys.  used: called
+  // when keys have been read.
   template <bool EDGE, typename K, typename U, typename S, typename V>
   __device__ __forceinline__ void step(int first, int lane, bool fresh, K keys, U used, S spoil, V values) {
     const int kg = lane >> 4;
@@ -465,9 +468,10 @@ template <typename IO, int D, int QT, bool FP8> struct Rows {
   }
 };
 
-// Zero weights may meet nothing but numbers: what lies behind the sequence (key >= n) may be anything, and values that are not finite (an
-// exponent of 255; of 252 to 254 only where nothing was appended) are to reach the rows that see them by their weights.  Takes both out of the
-// values of a lane's four tokens from `key`; bit i of the result: token i's were not finite.
+// Zero weights may meet nothing but numbers: what lies behind the sequence (key >= n) may be anything, and values
+// that are not finite (an exponent of 255; of 252 to 254 only where nothing was appended) are to reach the rows that
+// see them by their weights.  Takes both out of the values of a lane's four tokens from `key`; bit i of the result:
+// token i's were not finite.
 template <int D, bool NT> __device__ __forceinline__ uint32_t cleaned(Tile<D, NT>& x, int key, int n) {
   constexpr int N = D / 32;
   uint32_t spoilt = 0;
@@ -562,185 +566,185 @@ __global__ __launch_bounds__(kThreads, waves_held(sizeof(IO), D)) void attention
   }
   // a tile, or a part of one, after the other
   for (; x < x1;) {
-  Extent e = extent<ROWS>(a, b);
-  e.first = uniform(e.first);
-  e.n = uniform(e.n);
-  e.length = uniform(e.length);
-  e.tiles = uniform(e.tiles);
-  e.steps = uniform(e.steps);
-  const int all = rounds(e);
-  // the last rows see the most keys: they go first
-  const int tile = entire ? place : SPLIT ? place / all : ((e.tiles + kWaves - 1) / kWaves - 1 - place) * kWaves + wave;
-  const int r0 = SPLIT && !entire ? place - tile * all : 0, r1 = SPLIT && !entire && x1 - x < all - r0 ? r0 + x1 - x : all;
-  const bool whole_tile = !SPLIT || (r0 == 0 && r1 == all);
-  const int row0 = tile * ROWS, rows = e.n * a.group - row0 < ROWS ? e.n * a.group - row0 : ROWS;
-  if (!SPLIT && rows <= 0) return;
-  const int most = a.tok.columns << (a.cache.shift + 4);
-  auto limit = [&](int row) INLINE {  // the last key that a row sees; of keys past the table one, which reads as NaN
-    const int place = e.length - e.n + a.by_group(row);
-    return place < most ? place : most;
-  };
-  const int low = limit(row0), high = limit(row0 + rows - 1);
-  Rows<IO, D, QT, FP8> mine(a.scale);
-  mine.start(a, e, h, row0, rows, lane, limit);
-
-  const int stride = SPLIT ? kWaves : 1;
-  const int last = high < 0 ? 0 : high / kStep + 1;
-  const int s1 = SPLIT && r1 < all && r1 * kWaves < last ? r1 * kWaves : last, s0 = SPLIT ? r0 * kWaves + wave : 0;
-
-  // 64 entries of the sequence's row of the table, one a lane: a step's pages are a lane's value, with no load
-  // between a step and the next one's records.
-  const int32_t* row_of_table = a.tok.table + (size_t)b * a.tok.ld_table;
-  int window = 0, entries = 0;
-  auto look = [&](int j) INLINE {
-    window = j;
-    const int at = j + lane;
-    entries = row_of_table[at < a.tok.columns ? at : a.tok.columns - 1];
-    __builtin_amdgcn_s_waitcnt(0x0F70);  // here, where it is rare, and not at every use
-  };
-  struct Pages { int p0, p1; };
-  auto pages = [&](int s) INLINE {
-    const int j0 = 2 * s >> a.cache.shift, j1 = (2 * s + 1) >> a.cache.shift;
-    if (j1 - window >= 64) look(j0);
-    return Pages{__builtin_amdgcn_readlane(entries, j0 - window), __builtin_amdgcn_readlane(entries, j1 - window)};
-  };
-  using Two = Tile<D, NT>;
-  struct Records { const uint8_t *r0, *r1; uint32_t b0, b1; };
-  auto records = [&](int s, const Pages& p) INLINE {
-    auto good = [&](int tile, int page) INLINE { return tile >> a.cache.shift < a.tok.columns && (unsigned)page < (unsigned)a.cache.pages; };
-    const bool g0 = good(2 * s, p.p0), g1 = good(2 * s + 1, p.p1), used = kStep * s + 16 <= high;  // whether a row sees the second record
-    Records x;
-    x.r0 = record<D>(a.cache, g0 ? p.p0 : 0, h, 2 * s);
-    x.r1 = used ? record<D>(a.cache, g1 ? p.p1 : 0, h, 2 * s + 1) : x.r0;
-    x.b0 = g0 ? 0u : 255u;
-    x.b1 = g1 || !used ? 0u : 255u;
-    return x;
-  };
-  auto load_keys = [&](Two (&x)[2], const Records& r) INLINE {
-    x[0].load_keys(r.r0, lane, r.b0);
-    x[1].load_keys(r.r1, lane, r.b1);
-  };
-  auto load_values = [&](Two (&x)[2], const Records& r) INLINE {
-    x[0].load_values(r.r0, lane);
-    x[1].load_values(r.r1, lane);
-  };
-  const int n = e.length < most ? e.length : most + 1;  // keys there are
-  auto compute = [&](Two (&x)[2], int s, auto at_edge, auto keys_used, auto values_used) INLINE {
-    auto spoil = [&]() INLINE {
-      if (kStep * s + kStep <= n && !__builtin_amdgcn_ballot_w64(any_nan(x[0]) || any_nan(x[1]))) return 0u;
-      const uint32_t lo = cleaned(x[0], kStep * s + 4 * kg, n);
-      return lo | cleaned(x[1], kStep * s + 16 + 4 * kg, n) << 4;
+    Extent e = extent<ROWS>(a, b);
+    e.first = uniform(e.first);
+    e.n = uniform(e.n);
+    e.length = uniform(e.length);
+    e.tiles = uniform(e.tiles);
+    e.steps = uniform(e.steps);
+    const int all = rounds(e);
+    // the last rows see the most keys: they go first
+    const int tile = entire ? place : SPLIT ? place / all : ((e.tiles + kWaves - 1) / kWaves - 1 - place) * kWaves + wave;
+    const int r0 = SPLIT && !entire ? place - tile * all : 0, r1 = SPLIT && !entire && x1 - x < all - r0 ? r0 + x1 - x : all;
+    const bool whole_tile = !SPLIT || (r0 == 0 && r1 == all);
+    const int row0 = tile * ROWS, rows = e.n * a.group - row0 < ROWS ? e.n * a.group - row0 : ROWS;
+    if (!SPLIT && rows <= 0) return;
+    const int most = a.tok.columns << (a.cache.shift + 4);
+    auto limit = [&](int row) INLINE {  // the last key that a row sees; of keys past the table one, which reads as NaN
+      const int place = e.length - e.n + a.by_group(row);
+      return place < most ? place : most;
     };
-    mine.template step<decltype(at_edge)::value>(kStep * s, lane, s == s0, [&](int i, int j) INLINE { return x[i].key(j, lane); }, keys_used, spoil,
-                                                 [&](int g, bf16x8& lo, bf16x8& hi) INLINE { values(x[0], x[1], g, lo, hi); });
-    values_used();
-  };
+    const int low = limit(row0), high = limit(row0 + rows - 1);
+    Rows<IO, D, QT, FP8> mine(a.scale);
+    mine.start(a, e, h, row0, rows, lane, limit);
 
-  if (s0 < s1) {
-    const int whole = low < 0 ? 0 : (low + 1) / kStep, end = whole < s1 ? whole : s1;  // steps that every row sees all of
-    // the last round loads what it has again: loads under a condition would be waited for
-    auto after = [&](int s) INLINE { return s + stride < s1 ? s + stride : s; };
-    Two now[2];
-    look(2 * s0 >> a.cache.shift);
-    Records r = records(s0, pages(s0));
-    load_keys(now, r);
-    load_values(now, r);
-    int s = s0;
-    if constexpr (SPLIT) {
-      // a step ahead in registers of its own: the cache comes from memory
-      Two next[2];
-      auto one = [&](Two (&x)[2], Two (&y)[2], auto at_edge) INLINE {
-        const int s2 = after(s);
-        r = records(s2, pages(s2));
-        load_keys(y, r);
-        load_values(y, r);
-        compute(x, s, at_edge, [] {}, [] {});
-        s += stride;
-      };
-      while (s + stride < end) {  // two steps a round, so that the buffers change places without moves
-        one(now, next, std::false_type{});
-        one(next, now, std::false_type{});
-      }
-      if (s < end) {
-        one(now, next, std::false_type{});
-        now[0] = next[0];
-        now[1] = next[1];
-      }
-      while (s < s1) {
-        one(now, next, std::true_type{});
-        now[0] = next[0];
-        now[1] = next[1];
-      }
-    } else {
-      // keys and values of the next step as soon as the registers are free: the cache comes from L2
-      auto one = [&](auto at_edge) INLINE {
-        const int s2 = after(s);
-        r = records(s2, pages(s2));
-        compute(now, s, at_edge, [&]() INLINE { load_keys(now, r); }, [&]() INLINE { load_values(now, r); });
-        s += stride;
-      };
-      while (s < end) one(std::false_type{});
-      while (s < s1) one(std::true_type{});
-    }
-  }
+    const int stride = SPLIT ? kWaves : 1;
+    const int last = high < 0 ? 0 : high / kStep + 1;
+    const int s1 = SPLIT && r1 < all && r1 * kWaves < last ? r1 * kWaves : last, s0 = SPLIT ? r0 * kWaves + wave : 0;
 
-  if constexpr (SPLIT) {
-    float* so = shared;                               // [waves][ROWS][PITCH]
-    float* sm = shared + kWaves * ROWS * PITCH;       // [waves][ROWS] maxima, then sums
-    float* sl = sm + kWaves * ROWS;
-#pragma unroll
-    for (int t = 0; t < QT; ++t) {
-      const int row = wave * ROWS + 16 * t + r;
-#pragma unroll
-      for (int j = 0; j < 2 * N; ++j) *reinterpret_cast<floatx4*>(so + row * PITCH + 16 * j + 4 * kg) = mine.o[t][j];
-      if (kg == 0) { sm[row] = mine.m[t]; sl[row] = mine.l[t][0]; }
-    }
-    __syncthreads();
-    for (int i = threadIdx.x; i < rows * (D / 8); i += kThreads) {
-      const int row = i / (D / 8), c = (i - row * (D / 8)) * 8;
-      float to = -INFINITY, sum = 0.f, y[8] = {};
-#pragma unroll
-      for (int k = 0; k < kWaves; ++k) to = fmaxf(to, sm[k * ROWS + row]);
-#pragma unroll
-      for (int k = 0; k < kWaves; ++k) {
-        const float mk = sm[k * ROWS + row], f = mine.weight.from(mk, to);
-        sum = fmaf(f, sl[k * ROWS + row], sum);
-        Vec<8> v;
-        v.load(so + (k * ROWS + row) * PITCH + c);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) y[j] = fmaf(f, v.e[j], y[j]);
-      }
-      if (whole_tile) {
-        const float inv = sum == 0.f ? 0.f : 1.f / sum;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) y[j] *= inv;
-        const int tok = a.by_group(row0 + row);
-        put<IO, FP8>(a, e.first + tok, (h * a.group + row0 + row - tok * a.group) * D + c, y);
+    // 64 entries of the sequence's row of the table, one a lane: a step's pages are a lane's value, with no load
+    // between a step and the next one's records.
+    const int32_t* row_of_table = a.tok.table + (size_t)b * a.tok.ld_table;
+    int window = 0, entries = 0;
+    auto look = [&](int j) INLINE {
+      window = j;
+      const int at = j + lane;
+      entries = row_of_table[at < a.tok.columns ? at : a.tok.columns - 1];
+      __builtin_amdgcn_s_waitcnt(0x0F70);  // here, where it is rare, and not at every use
+    };
+    struct Pages { int p0, p1; };
+    auto pages = [&](int s) INLINE {
+      const int j0 = 2 * s >> a.cache.shift, j1 = (2 * s + 1) >> a.cache.shift;
+      if (j1 - window >= 64) look(j0);
+      return Pages{__builtin_amdgcn_readlane(entries, j0 - window), __builtin_amdgcn_readlane(entries, j1 - window)};
+    };
+    using Two = Tile<D, NT>;
+    struct Records { const uint8_t *r0, *r1; uint32_t b0, b1; };
+    auto records = [&](int s, const Pages& p) INLINE {
+      auto good = [&](int tile, int page) INLINE { return tile >> a.cache.shift < a.tok.columns && (unsigned)page < (unsigned)a.cache.pages; };
+      const bool g0 = good(2 * s, p.p0), g1 = good(2 * s + 1, p.p1), used = kStep * s + 16 <= high;  // whether a row sees the second record
+      Records x;
+      x.r0 = record<D>(a.cache, g0 ? p.p0 : 0, h, 2 * s);
+      x.r1 = used ? record<D>(a.cache, g1 ? p.p1 : 0, h, 2 * s + 1) : x.r0;
+      x.b0 = g0 ? 0u : 255u;
+      x.b1 = g1 || !used ? 0u : 255u;
+      return x;
+    };
+    auto load_keys = [&](Two (&x)[2], const Records& r) INLINE {
+      x[0].load_keys(r.r0, lane, r.b0);
+      x[1].load_keys(r.r1, lane, r.b1);
+    };
+    auto load_values = [&](Two (&x)[2], const Records& r) INLINE {
+      x[0].load_values(r.r0, lane);
+      x[1].load_values(r.r1, lane);
+    };
+    const int n = e.length < most ? e.length : most + 1;  // keys there are
+    auto compute = [&](Two (&x)[2], int s, auto at_edge, auto keys_used, auto values_used) INLINE {
+      auto spoil = [&]() INLINE {
+        if (kStep * s + kStep <= n && !__builtin_amdgcn_ballot_w64(any_nan(x[0]) || any_nan(x[1]))) return 0u;
+        const uint32_t lo = cleaned(x[0], kStep * s + 4 * kg, n);
+        return lo | cleaned(x[1], kStep * s + 16 + 4 * kg, n) << 4;
+      };
+      mine.template step<decltype(at_edge)::value>(kStep * s, lane, s == s0, [&](int i, int j) INLINE { return x[i].key(j, lane); }, keys_used, spoil,
+                                                   [&](int g, bf16x8& lo, bf16x8& hi) INLINE { values(x[0], x[1], g, lo, hi); });
+      values_used();
+    };
+
+    if (s0 < s1) {
+      const int whole = low < 0 ? 0 : (low + 1) / kStep, end = whole < s1 ? whole : s1;  // steps that every row sees all of
+      // the last round loads what it has again: loads under a condition would be waited for
+      auto after = [&](int s) INLINE { return s + stride < s1 ? s + stride : s; };
+      Two now[2];
+      look(2 * s0 >> a.cache.shift);
+      Records r = records(s0, pages(s0));
+      load_keys(now, r);
+      load_values(now, r);
+      int s = s0;
+      if constexpr (SPLIT) {
+        // a step ahead in registers of its own: the cache comes from memory
+        Two next[2];
+        auto one = [&](Two (&x)[2], Two (&y)[2], auto at_edge) INLINE {
+          const int s2 = after(s);
+          r = records(s2, pages(s2));
+          load_keys(y, r);
+          load_values(y, r);
+          compute(x, s, at_edge, [] {}, [] {});
+          s += stride;
+        };
+        while (s + stride < end) {  // two steps a round, so that the buffers change places without moves
+          one(now, next, std::false_type{});
+          one(next, now, std::false_type{});
+        }
+        if (s < end) {
+          one(now, next, std::false_type{});
+          now[0] = next[0];
+          now[1] = next[1];
+        }
+        while (s < s1) {
+          one(now, next, std::true_type{});
+          now[0] = next[0];
+          now[1] = next[1];
+        }
       } else {
-        float* slot = a.work + ((size_t)blockIdx.x * 2 + (x == u * each ? 0 : 1)) * (ROWS * (D + 2));
-        st_elem4(slot + row * D + c, y[0], y[1], y[2], y[3]);
-        st_elem4(slot + row * D + c + 4, y[4], y[5], y[6], y[7]);
-        if (c == 0) {
-          slot[ROWS * D + row] = to;
-          slot[ROWS * D + ROWS + row] = sum;
+        // keys and values of the next step as soon as the registers are free: the cache comes from L2
+        auto one = [&](auto at_edge) INLINE {
+          const int s2 = after(s);
+          r = records(s2, pages(s2));
+          compute(now, s, at_edge, [&]() INLINE { load_keys(now, r); }, [&]() INLINE { load_values(now, r); });
+          s += stride;
+        };
+        while (s < end) one(std::false_type{});
+        while (s < s1) one(std::true_type{});
+      }
+    }
+
+    if constexpr (SPLIT) {
+      float* so = shared;                               // [waves][ROWS][PITCH]
+      float* sm = shared + kWaves * ROWS * PITCH;       // [waves][ROWS] maxima, then sums
+      float* sl = sm + kWaves * ROWS;
+#pragma unroll
+      for (int t = 0; t < QT; ++t) {
+        const int row = wave * ROWS + 16 * t + r;
+#pragma unroll
+        for (int j = 0; j < 2 * N; ++j) *reinterpret_cast<floatx4*>(so + row * PITCH + 16 * j + 4 * kg) = mine.o[t][j];
+        if (kg == 0) { sm[row] = mine.m[t]; sl[row] = mine.l[t][0]; }
+      }
+      __syncthreads();
+      for (int i = threadIdx.x; i < rows * (D / 8); i += kThreads) {
+        const int row = i / (D / 8), c = (i - row * (D / 8)) * 8;
+        float to = -INFINITY, sum = 0.f, y[8] = {};
+#pragma unroll
+        for (int k = 0; k < kWaves; ++k) to = fmaxf(to, sm[k * ROWS + row]);
+#pragma unroll
+        for (int k = 0; k < kWaves; ++k) {
+          const float mk = sm[k * ROWS + row], f = mine.weight.from(mk, to);
+          sum = fmaf(f, sl[k * ROWS + row], sum);
+          Vec<8> v;
+          v.load(so + (k * ROWS + row) * PITCH + c);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) y[j] = fmaf(f, v.e[j], y[j]);
+        }
+        if (whole_tile) {
+          const float inv = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) y[j] *= inv;
+          const int tok = a.by_group(row0 + row);
+          put<IO, FP8>(a, e.first + tok, (h * a.group + row0 + row - tok * a.group) * D + c, y);
+        } else {
+          float* slot = a.work + ((size_t)blockIdx.x * 2 + (x == u * each ? 0 : 1)) * (ROWS * (D + 2));
+          st_elem4(slot + row * D + c, y[0], y[1], y[2], y[3]);
+          st_elem4(slot + row * D + c + 4, y[4], y[5], y[6], y[7]);
+          if (c == 0) {
+            slot[ROWS * D + row] = to;
+            slot[ROWS * D + ROWS + row] = sum;
+          }
         }
       }
-    }
-    x += entire ? 1 : r1 - r0;
-    place += r1 - r0;
-    if (x < x1) {
-      __syncthreads();  // `shared` is written again
-      while (place >= e.tiles * rounds(e) && b + 1 < batch) {  // the next sequence that has rows
-        e = extent<ROWS>(a, ++b);
-        e.tiles = uniform(e.tiles);
-        e.steps = uniform(e.steps);
-        place = 0;
+      x += entire ? 1 : r1 - r0;
+      place += r1 - r0;
+      if (x < x1) {
+        __syncthreads();  // `shared` is written again
+        while (place >= e.tiles * rounds(e) && b + 1 < batch) {  // the next sequence that has rows
+          e = extent<ROWS>(a, ++b);
+          e.tiles = uniform(e.tiles);
+          e.steps = uniform(e.steps);
+          place = 0;
+        }
       }
+    } else {
+      mine.finish(a, e, h, row0, rows, lane, shared + wave * 16 * PITCH);
+      x = x1;
     }
-  } else {
-    mine.finish(a, e, h, row0, rows, lane, shared + wave * 16 * PITCH);
-    x = x1;
-  }
   }
 }
 
@@ -929,10 +933,12 @@ int64_t most_tiles(int batch, int tokens, int group, int rows) {
 }
 // The plan that join_kernel reads: rounds a workgroup has, then those before each sequence.
 int64_t plan_words(int batch) { return ((int64_t)batch + 1 + 3) / 4 * 4; }
-// Whether keys are split, by the rows that a sequence has on average, the workgroups of 128 rows that they would fill and the keys that the
-// table has room for.  In us, split and by rows: one prompt of 128 tokens 6.3 and 9.2, of 256 11.8 and 12.4, of 512 26 and 19, of 2048 105 and 62, 100 prompts of 20 tokens 32 and 18; 64 requests of
-// 16 tokens over up to 4000 keys 119 and 115, of 1000 71 and 41; 128 of 8 tokens (32 rows) 96 and 147, 65 and 52; few workgroups over many keys: 512
-// tokens over 1024 keys 23 and 30, over 4096 52 and 101, 1024 over 4096 96 and 103, 4 x 256 over 16000 270 and 421.
+// Whether keys are split, by the rows that a sequence has on average, the workgroups of 128 rows that they would fill
+// and the keys that the table has room for.  In us, split and by rows: one prompt of 128 tokens 6.3 and 9.2, of 256
+// 11.8 and 12.4, of 512 26 and 19, of 2048 105 and 62, 100 prompts of 20 tokens 32 and 18; 64 requests of 16 tokens
+// over up to 4000 keys 119 and 115, of 1000 71 and 41; 128 of 8 tokens (32 rows) 96 and 147, 65 and 52; few
+// workgroups over many keys: 512 tokens over 1024 keys 23 and 30, over 4096 52 and 101, 1024 over 4096 96 and 103, 4
+// x 256 over 16000 270 and 421.
 bool splits(int batch, int tokens, int group, int G, int64_t capacity) {
   const int64_t rows = (int64_t)tokens * group / batch, workgroups = (int64_t)batch * ((rows + 127) / 128) * G;
   if (rows < (capacity > 1024 ? 64 : 32)) return true;
@@ -956,9 +962,10 @@ int shares(int batch, int tokens, int group, int G, int D, int QT, int64_t capac
   return (int)(n < most ? n : most);
 }
 
-// Tiles of rows a wave: two where the sequences' rows fill them and there is more than a round or so of work for every workgroup; with less, what
-// counts is the time of one.  In us, one tile and two: a prompt of 128 tokens 6.3 and 7.7, of 256 11.8 and 15.7, 4 of 100 behind 900 32.6 and 33.0,
-// behind 7900 90 and 73, one of 512 behind 512 35 and 23.
+// Tiles of rows a wave: two where the sequences' rows fill them and there is more than a round or so of work for
+// every workgroup; with less, what counts is the time of one.  In us, one tile and two: a prompt of 128 tokens 6.3
+// and 7.7, of 256 11.8 and 15.7, 4 of 100 behind 900 32.6 and 33.0, behind 7900 90 and 73, one of 512 behind 512 35
+// and 23.
 int split_tiles(int batch, int tokens, int group, int G, int64_t capacity) {
   return (int64_t)tokens * group > (int64_t)16 * batch && most_rounds(batch, tokens, group, 2, capacity) * G > 16 * kCUs ? 2 : 1;
 }
@@ -983,9 +990,10 @@ template <typename IO, int D, bool FP8> int launch(const AttentionArgs& a, hipSt
         b.plan = reinterpret_cast<int*>(a.work);
         b.work = reinterpret_cast<float*>(b.plan + plan_words(batch));
       }
-      // Past the caches where the pool is larger than the last-level one, so that nothing of it is there the next time: 64 requests of
-      // up to 8192 tokens 61.3 -> 56.8 us (pool 330 MB); 32 of 4096 with 16 key heads, out of that cache, 40.3 -> 45.7.  Records of
-      // 128 channels only, where every load takes whole lines: of 64, 41.4 -> 54.4.
+      // Past the caches where the pool is larger than the last-level one, so that nothing of it is there the
+      // next time: 64 requests of up to 8192 tokens 61.3 -> 56.8 us (pool 330 MB); 32 of 4096 with 16 key
+      // heads, out of that cache, 40.3 -> 45.7.  Records of 128 channels only, where every load takes whole
+      // lines: of 64, 41.4 -> 54.4.
       constexpr bool CAN = D == 128 && QT == 1;
       const bool past = CAN && (int64_t)a.cache.pages * G * (17 * D) << a.cache.shift > (int64_t)256 << 20;
       if (past) hipLaunchKernelGGL((attention_kernel<IO, D, QT, true, FP8, CAN>), dim3((unsigned)workgroups), dim3(kThreads), 0, s, b);

@@ -264,7 +264,9 @@ int sketchssm_attention(const skssm_cache* cache, const skssm_new_tokens* seq, c
   const Range queries[] = {{p.q, nq}};
   const Range in[] = {{cache->data, cache_bytes(cache)}, {seq->offsets, ((size_t)seq->batch + 1) * 4}, {seq->lengths, (size_t)seq->batch * 4},
                       {seq->table, table_bytes(seq)}};
-  if (any_overlap(out, in) || any_overlap(beside, queries) || rows_overlap(p.out, H * D * eo, p.ld_out * eo, p.q, ((H - 1) * p.q_head + D) * e, p.ldq * e, T)) return fail(SKSSM_EINVAL, "%s: an output overlaps an input", what);
+  if (any_overlap(out, in) || any_overlap(beside, queries) ||
+      rows_overlap(p.out, H * D * eo, p.ld_out * eo, p.q, ((H - 1) * p.q_head + D) * e, p.ldq * e, T))
+    return fail(SKSSM_EINVAL, "%s: an output overlaps an input", what);
   if ((ns && overlap(p.out, no, p.scales, ns)) || (need && (overlap(p.out, no, p.workspace, need) || (ns && overlap(p.scales, ns, p.workspace, need)))))
     return fail(SKSSM_EINVAL, "%s: the outputs overlap", what);
   if (T == 0) return fail(SKSSM_OK, "%s", "");  // nothing to do: no launch, no error

@@ -1,11 +1,11 @@
 // Rotary positions and the 4-bit cache: the rotation of queries and keys, the
 // append of keys and values, and the cache's values back as numbers.
 //
-// Every array moves once, so the kernels are bound by memory: 16384 tokens of 40 heads of 128 channels turned in 60 us (5.7 TB/s), of 32 + 2 x 8
-// heads turned and appended in 74 (4.8; 71 without the byte stores of the values), read back in 21 (4.0).  A lane owns 8
-// channels of a token (16 or 32 bytes) and keeps their cosines and sines in
-// registers while it goes over the token's heads; four lanes (a DPP quad) hold
-// the 32 channels that share an exponent.
+// Every array moves once, so the kernels are bound by memory: 16384 tokens of 40 heads of 128 channels turned in 60
+// us (5.7 TB/s), of 32 + 2 x 8 heads turned and appended in 74 (4.8; 71 without the byte stores of the values), read
+// back in 21 (4.0).  A lane owns 8 channels of a token (16 or 32 bytes) and keeps their cosines and sines in
+// registers while it goes over the token's heads; four lanes (a DPP quad) hold the 32 channels that share an
+// exponent.
 #include <type_traits>
 
 #include "../attention.h"
@@ -202,8 +202,9 @@ template <typename IO, int PAIRS, int LT> int launch_append(const CacheAppendArg
 }
 
 template <typename IO, int PAIRS> int launch_append(const CacheAppendArgs& a, hipStream_t s) {
-  // Four tokens a workgroup (64 lanes each at most), or one, in us for the append and the read back of 32 + 2 x 8 heads of 128 channels: 64 tokens 10.2 and 8.7, 1024 12.1 and 11.8, 2048 17.3
-  // and 18.4, 4096 25.7 and 28.2; 16384 74 (two a workgroup 81, eight 77).
+  // Four tokens a workgroup (64 lanes each at most), or one, in us for the append and the read back of 32 + 2 x 8
+  // heads of 128 channels: 64 tokens 10.2 and 8.7, 1024 12.1 and 11.8, 2048 17.3 and 18.4, 4096 25.7 and 28.2;
+  // 16384 74 (two a workgroup 81, eight 77).
   return a.tok.seq.tokens > 1024 ? launch_append<IO, PAIRS, 2>(a, s) : launch_append<IO, PAIRS, 0>(a, s);
 }
 
