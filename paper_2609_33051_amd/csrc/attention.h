@@ -81,6 +81,7 @@ struct AttentionArgs {
   float* work;     // [share][key heads][2]: a tile's sums, maxima and sums of weights
   int* plan;       // at the workspace's start (NULL: no tile can be split)
   int share;       // workgroups of attention_kernel a key head
+  int most;        // rounds that a key head can have
   int span;        // pieces of 8 channels a workgroup of join_kernel
 };
 int run_attention(const AttentionArgs& a, int D, int io, bool fp8, void* stream);

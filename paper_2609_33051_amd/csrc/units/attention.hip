@@ -9,8 +9,9 @@
 // keys are summed is free, and the cache's records hold the values in the order it leaves).  Nothing passes
 // through LDS.  A row of ones beside V^T sums the weights as the products see them.
 //
-// The maximum that the weights are taken over moves only where the weights' sum has grown past 2^16; until then no score is compared with
-// another and nothing is rescaled (one prompt of 8192 tokens, with the registers that this frees: 2000 -> 607 us).
+// The maximum that the weights are taken over moves only where the weights' sum has grown past 2^16; until then no
+// score is compared with another and nothing is rescaled (one prompt of 8192 tokens, with the registers that this
+// frees: 2000 -> 607 us).
 //
 // Single tokens are bound by the cache's bytes: 64 over contexts of up to 8192, 32 heads on 8 of 128 channels, in 56
 // us (5.9 TB/s; the loads alone take as long), one over 131072 keys in 26 (5.5).  Prompts are bound by the vector
@@ -30,7 +31,8 @@ constexpr int kWaves = 4, kThreads = 64 * kWaves;
 constexpr int kStep = 32;         // keys a step
 constexpr float kMost = 65536.f;  // sum of weights from which on the maximum is taken again
 constexpr int kCUs = 256;
-constexpr int kApart = 8;
+constexpr int kApart = 8;         // rounds that a tile apart costs
+constexpr int kMostRounds = (1 << 30) - 1;
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
@@ -196,24 +198,26 @@ template <int ROWS> __device__ __forceinline__ Extent extent(const AttentionArgs
 }
 
 // Where a position among the sequences' weights lies: each thread sums the weights of a run of sequences, and
-// `upto` [kThreads] holds the sums up to and with each run.
+// `upto` [kThreads] holds the sums up to and with each run.  Sums end at kMostRounds, which none reaches whose offsets
+// rise: others may, and a sum that wrapped would lead out of the arrays.
+__device__ __forceinline__ int held(int x) { return x < kMostRounds ? x : kMostRounds; }
 template <typename F> __device__ __forceinline__ int lay_out(int batch, F weight, int* upto) {
   if (batch == 1) return weight(0);
   __shared__ int waves[kWaves];
   const int run = (batch + kThreads - 1) / kThreads, tid = threadIdx.x;
   int x = 0;
-  for (int b = tid * run; b < (tid + 1) * run && b < batch; ++b) x += weight(b);
+  for (int b = tid * run; b < (tid + 1) * run && b < batch; ++b) x = held(x + weight(b));
   for (int d = 1; d < 64; d *= 2) {
     const int y = __shfl_up(x, d);
-    x += (tid & 63) >= d ? y : 0;
+    x = held(x + ((tid & 63) >= d ? y : 0));
   }
   if ((tid & 63) == 63) waves[tid >> 6] = x;
   __syncthreads();
   int total = 0;
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) {
-    if (w < tid >> 6) x += waves[w];
-    total += waves[w];
+    if (w < tid >> 6) x = held(x + waves[w]);
+    total = held(total + waves[w]);
   }
   upto[tid] = x;
   __syncthreads();
@@ -244,16 +248,17 @@ template <typename F> __device__ __forceinline__ int seek(int batch, F weight, c
   return uniform(b);
 }
 
-// Split sequences.  The steps of a tile of rows are counted in rounds, one step of each wave, one round at least. A key head's rounds of all
-// sequences and tiles lie one after the other and are shared out evenly: workgroup u has rounds u each .. of them,
-// whatever tiles they are of.  A tile that one workgroup has whole is written by it; of others it leaves the sums
-// in one of its two slots, the second where the tile begins behind the workgroup's own first round.
-__device__ __forceinline__ int rounds(const Extent& e) { return e.steps <= kWaves ? 1 : (e.steps + kWaves - 1) / kWaves; }
+// Split sequences.  The steps of a tile of rows are counted in rounds, one step of each wave, one round at least. A
+// key head's rounds of all sequences and tiles lie one after the other and are shared out evenly: workgroup u has
+// rounds u each .. of them, whatever tiles they are of.  A tile that one workgroup has whole is written by it; of
+// others it leaves the sums in one of its two slots, the second where the tile begins behind the workgroup's own first
+// round.
 //
 // Where there are no more tiles than workgroups and the longest is not much longer than an even share, every tile is
 // one workgroup's: a share that ends inside a tile costs a second start and the join of its parts, some kApart rounds
 // (us, even shares and whole tiles: 256 requests of up to 1500 keys, 2 key heads of 256 channels 42.7 and 34.4, of up
 // to 1000, 128 channels 23.3 and 19.6; 64 of 1500, 8 key heads 24.0 and 22.1).
+__device__ __forceinline__ int rounds(const Extent& e) { return e.steps <= kWaves ? 1 : (e.steps + kWaves - 1) / kWaves; }
 template <int ROWS> struct Rounds {
   const AttentionArgs& a;
   __device__ __forceinline__ int operator()(int b) const {
@@ -322,6 +327,7 @@ template <typename IO, int D, int QT, bool FP8> struct Rows {
   bf16x8 q[QT][N][QP];
   floatx4 o[QT][2 * N], l[QT];  // of channels 16 j + 4 (lane / 16) .., and of the weights
   float m[QT];
+  bool unset = true;            // some row's maximum is -inf yet: it sees no keys so far, or its scores overflowed to that
   int lim[QT];                  // the last key that a lane's row sees
   __device__ __forceinline__ explicit Rows(float scale) : weight(scale) {}
 
@@ -356,10 +362,9 @@ template <typename IO, int D, int QT, bool FP8> struct Rows {
 
   // Keys first .. first + 31, of two records: keys(i, j) are channels 8 j .. (of a lane's quarter) of record i's,
   // values(g, lo, hi) block g of both records' values.  EDGE: some row does not see all of them; spoil() then has
-  // bit i of a lane's eight keys for values that are not finite.  fresh: these are the first keys.  used: called
-  // when keys have been read.
+  // bit i of a lane's eight keys for values that are not finite.  used: called when keys have been read.
   template <bool EDGE, typename K, typename U, typename S, typename V>
-  __device__ __forceinline__ void step(int first, int lane, bool fresh, K keys, U used, S spoil, V values) {
+  __device__ __forceinline__ void step(int first, int lane, K keys, U used, S spoil, V values) {
     const int kg = lane >> 4;
     floatx4 z[QT][2];
 #pragma unroll
@@ -408,13 +413,14 @@ template <typename IO, int D, int QT, bool FP8> struct Rows {
       return sum;
     };
     floatx4 sum[QT];
-    bool fine = !fresh;
+    bool fine = !unset;
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
       sum[t] = weigh(t);
       fine = fine && sum[t][0] <= kMost;
     }
     if (__builtin_amdgcn_ballot_w64(!fine)) {
+      unset = false;
 #pragma unroll
       for (int t = 0; t < QT; ++t) {
         float top = m[t];
@@ -423,6 +429,7 @@ template <typename IO, int D, int QT, bool FP8> struct Rows {
         top = across_rows_max(top);
         const float f = weight.from(m[t], top);
         m[t] = top;
+        unset = unset || __builtin_amdgcn_ballot_w64(top == -INFINITY);
         l[t] *= f;
 #pragma unroll
         for (int j = 0; j < 2 * N; ++j) o[t][j] *= f;
@@ -533,6 +540,7 @@ __global__ __launch_bounds__(kThreads, waves_held(sizeof(IO), D)) void attention
   bool entire = false;
   if constexpr (SPLIT) {
     total = lay_out(batch, weight_of, upto);
+    total = total < a.most ? total : a.most;
     each = (int)(((uint32_t)total + a.share - 1) / a.share);
     if (batch > 1 && batch <= a.share && longest<ROWS>(a) <= each + kApart) {  // as many tiles as there are rows for
       __syncthreads();
@@ -554,7 +562,7 @@ __global__ __launch_bounds__(kThreads, waves_held(sizeof(IO), D)) void attention
       int before = batch == 1 || threadIdx.x == 0 ? 0 : upto[threadIdx.x - 1];
       for (int i = threadIdx.x * run; i < (int)(threadIdx.x + 1) * run && i < batch; ++i) {
         a.plan[1 + i] = before;
-        before += weight_of(i);
+        before = held(before + weight_of(i));
       }
     }
     if (x >= total) return;
@@ -635,7 +643,7 @@ __global__ __launch_bounds__(kThreads, waves_held(sizeof(IO), D)) void attention
         const uint32_t lo = cleaned(x[0], kStep * s + 4 * kg, n);
         return lo | cleaned(x[1], kStep * s + 16 + 4 * kg, n) << 4;
       };
-      mine.template step<decltype(at_edge)::value>(kStep * s, lane, s == s0, [&](int i, int j) INLINE { return x[i].key(j, lane); }, keys_used, spoil,
+      mine.template step<decltype(at_edge)::value>(kStep * s, lane, [&](int i, int j) INLINE { return x[i].key(j, lane); }, keys_used, spoil,
                                                    [&](int g, bf16x8& lo, bf16x8& hi) INLINE { values(x[0], x[1], g, lo, hi); });
       values_used();
     };
@@ -831,7 +839,7 @@ template <typename IO, int D, int QT, bool FP8> __global__ __launch_bounds__(kTh
     for (int p = 0; p < kWaves / 2; ++p) {
       if (s * KEYS + 32 * p > mine_high) break;
       mine.template step<decltype(at_edge)::value>(
-          s * KEYS + 32 * p, lane, s == 0 && p == 0, [&](int i, int j) INLINE { return __builtin_bit_cast(bf16x8, from.k[2 * p + i][j][lane]); }, [] {},
+          s * KEYS + 32 * p, lane, [&](int i, int j) INLINE { return __builtin_bit_cast(bf16x8, from.k[2 * p + i][j][lane]); }, [] {},
           [&]() INLINE { return spoil[s & 1][2 * p][kg] | spoil[s & 1][2 * p + 1][kg] << 4; },
           [&](int g, bf16x8& lo, bf16x8& hi) INLINE {
             lo = __builtin_bit_cast(bf16x8, from.v[p][2 * g][lane]);
@@ -945,11 +953,6 @@ bool splits(int batch, int tokens, int group, int G, int64_t capacity) {
   const int64_t enough = capacity / 4 < kCUs / 2 ? kCUs / 2 : capacity / 4 < 2 * kCUs ? capacity / 4 : 2 * kCUs;
   return workgroups < enough;
 }
-// are workgroups for twice the CUs.
-bool splits(int batch, int tokens, int group, int G) {
-  const int64_t rows = (int64_t)tokens * group;
-  return rows < (int64_t)64 * batch || rows * G < (int64_t)128 * 2 * kCUs;
-}
 // Workgroups a key head's rounds are shared out to: as many as are at work at once (by the registers of
 // attention_kernel), and no more than there can be rounds.
 int64_t most_rounds(int batch, int tokens, int group, int QT, int64_t capacity) {
@@ -977,6 +980,7 @@ template <typename IO, int D, bool FP8> int launch(const AttentionArgs& a, hipSt
     auto run = [&](auto qt) {
       constexpr int QT = decltype(qt)::value;
       AttentionArgs b = a;
+      b.most = (int)most_rounds(batch, tokens, a.group, QT, capacity);
       b.share = shares(batch, tokens, a.group, G, D, QT, capacity);
       const int64_t workgroups = (int64_t)b.share * G;
       const bool join = capacity > kStep * kWaves && b.share > 1;  // a round is never split
@@ -985,7 +989,7 @@ template <typename IO, int D, bool FP8> int launch(const AttentionArgs& a, hipSt
       b.span = 16;
       while (b.span < 256 && b.span < pieces && (int64_t)tokens * G * ((pieces + b.span - 1) / b.span) > 4 * kCUs) b.span *= 2;
       const int64_t joins = (int64_t)tokens * G * ((pieces + b.span - 1) / b.span);
-      if (!fits(workgroups, kThreads) || !fits(joins, kThreads) || most_rounds(batch, tokens, a.group, QT, capacity) >= (int64_t)1 << 30) return -3;
+      if (!fits(workgroups, kThreads) || !fits(joins, kThreads) || most_rounds(batch, tokens, a.group, QT, capacity) >= kMostRounds) return -3;
       if (join) {
         b.plan = reinterpret_cast<int*>(a.work);
         b.work = reinterpret_cast<float*>(b.plan + plan_words(batch));

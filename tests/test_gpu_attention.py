@@ -487,3 +487,39 @@ def test_refused_before_any_launch():
               lambda: ops.rotary(q[:, :2], ang, out=q[:, 1:3]), lambda: ops.attention(cache, tab, ln, q, scale=float("inf")), lambda: ops.new_cache(4, 2, 24, 64), lambda: ops.new_cache(4, 2, 16, 80)):
         with pytest.raises(B.SketchSSMError):
             f()
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+@pytest.mark.parametrize("H,G,D,n,before", [(4, 2, 128, 1, 1100), (8, 2, 64, 3, 700), (32, 16, 128, 2100, 200), (16, 16, 256, 2100, 100)])
+def test_first_scores_that_overflow(io, H, G, D, n, before):
+    """Products of the first 64 keys and every query below -3.4e38 weigh nothing, and the others as without them."""
+    case("overflow", io, H, G, D, n, before)
+    dt, r = DT[io], rnd(before)
+    L = n + before
+    q = (r((n, H, D), torch.bfloat16).abs().clamp_min(0.25) * 1024).to(dt)  # without low parts, whose signs would differ
+    k, v = r((L, G, D), dt, 2.0 ** -10), r((L, G, D), dt)
+    k[:64] = -2.0 ** 124
+    tab, pool = R.table([L], 32)
+    cache = ops.new_cache(pool, G, 32, D)
+    ops.cache_append(cache, tab, i32([L]), k, v)
+    got, _ = ops.attention(cache, tab, i32([L]), q, offsets=R.offsets([n]))
+    o, mag, most = R.attention(q, R.held(k[64:]), R.held(v[64:]), n, D ** -0.5)
+    R.close(got, o, R.bound(o, mag, most, L, D, dt), "out")
+
+
+@pytest.mark.parametrize("B,T,H,G,D,length", [(16383, 65536, 8, 1, 64, 4096), (16381, 65536, 16, 2, 128, 3000), (5000, 20000, 4, 4, 64, 700), (40, 1500, 32, 8, 128, 900)])
+def test_offsets_that_do_not_rise(B, T, H, G, D, length):
+    """Nothing is written beside the outputs, whatever the offsets say (sums of rows and rounds past 2^31 among them), and the next call is right."""
+    case("wild offsets", B, T, H, G, D, length)
+    r = rnd(B)
+    cache, tab, ln, ks, vs = built(r, [length], G, D, 64, torch.bfloat16)
+    q = r((T, H, D), torch.bfloat16)
+    room = torch.full((T + 64, H, D), 7.0, dtype=torch.bfloat16, device="cuda")
+    want = ops.attention(cache, tab, ln, q[:1])[0]
+    off = torch.zeros(B + 1, dtype=torch.int32)
+    off[1::2] = 1 << 30
+    off[2::6] = -5
+    ops.attention(cache, tab.expand(B, -1).contiguous(), ln.expand(B).contiguous(), q, offsets=off.cuda(), out=room[32:32 + T])
+    torch.cuda.synchronize()
+    assert bool((room[:32] == 7).all()) and bool((room[32 + T:] == 7).all())
+    assert torch.equal(ops.attention(cache, tab, ln, q[:1])[0], want)
