@@ -756,13 +756,17 @@ __global__ __launch_bounds__(kThreads, waves_held(sizeof(IO), D)) void attention
   }
 }
 
-// Prompts: each of a workgroup's waves has a tile of rows, and all of them go over the keys together, 64 a step.  Each wave turns one
-// of the step's four records into the products' operands, which all read from LDS: alone, every wave would turn all four.
-// Two buffers: a step's operands are made while the one before is summed, a barrier a step.
+// Prompts: each of a workgroup's waves has a tile of rows, and all of them go over the keys together, 64 a step.  Each
+// wave turns one of the step's four records into the products' operands, which all read from LDS: alone, every wave
+// would turn all four.  Two buffers: a step's operands are made while the one before is summed, a barrier a step.  Past
+// 128 channels one (48 and 64 KB), between two barriers, so that a CU holds two workgroups, one of which sums while the
+// other turns (us, each wave for itself and this: 8192 tokens of 32 heads of 192 channels 816 -> 767, 2048 behind 14336
+// 820 -> 712; 16 heads of 256 channels, 4096 tokens 225 -> 204, 32 heads, 2048 behind 14336 1459 -> 1272.  Two buffers
+// and one workgroup a CU: 183 for the 158 of 4096 tokens of 16 heads of 192 channels, which take 166 with one).
 template <typename IO, int D, int QT, bool FP8> __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(AttentionArgs a) {
-  constexpr int N = D / 32, ROWS = 16 * QT, PITCH = D + 4, KEYS = 16 * kWaves;
+  constexpr int N = D / 32, ROWS = 16 * QT, PITCH = D + 4, KEYS = 16 * kWaves, BUFFERS = D > 128 ? 1 : 2;
   struct Operands { uint4 k[kWaves][N][64], v[kWaves / 2][2 * N][64]; };
-  __shared__ union { Operands x[2]; float so[kWaves * 16 * PITCH]; } shared;
+  __shared__ union { Operands x[BUFFERS]; float so[kWaves * 16 * PITCH]; } shared;
   __shared__ uint32_t spoil[2][kWaves][4];
   __shared__ int upto[kThreads];
   const int lane = threadIdx.x & 63, r = lane & 15, kg = lane >> 4;
@@ -812,7 +816,7 @@ template <typename IO, int D, int QT, bool FP8> __global__ __launch_bounds__(kTh
     x.load_values(rec, lane);
   };
   auto turn = [&](int s) INLINE {
-    Operands& to = shared.x[s & 1];
+    Operands& to = shared.x[s & (BUFFERS - 1)];
     if (s >= whole) {
       const uint32_t bad = cleaned(x, s * KEYS + wave * 16 + 4 * kg, n);
       if (r == 0) spoil[s & 1][wave][kg] = bad;
@@ -834,7 +838,7 @@ template <typename IO, int D, int QT, bool FP8> __global__ __launch_bounds__(kTh
     }
   };
   auto sum = [&](int s, auto at_edge) INLINE {
-    const Operands& from = shared.x[s & 1];
+    const Operands& from = shared.x[s & (BUFFERS - 1)];
 #pragma unroll
     for (int p = 0; p < kWaves / 2; ++p) {
       if (s * KEYS + 32 * p > mine_high) break;
@@ -855,11 +859,15 @@ template <typename IO, int D, int QT, bool FP8> __global__ __launch_bounds__(kTh
     lds_barrier();
     int s = 0;
     auto one = [&](auto at_edge) INLINE {
+      if constexpr (BUFFERS == 1) {
+        sum(s, at_edge);
+        lds_barrier();
+      }
       if (s + 1 < steps) {
         turn(s + 1);
         load(s + 2 < steps ? s + 2 : s + 1);
       }
-      sum(s, at_edge);
+      if constexpr (BUFFERS == 2) sum(s, at_edge);
       lds_barrier();
     };
     for (; s < whole && s < steps; ++s) one(std::false_type{});
@@ -1012,7 +1020,7 @@ template <typename IO, int D, bool FP8> int launch(const AttentionArgs& a, hipSt
   constexpr int QT = most_tiles_held(sizeof(IO), D, false);
   const int64_t workgroups = most_tiles(batch, tokens, a.group, 16 * QT * kWaves) * G;
   if (!fits(workgroups, kThreads)) return -3;
-  if constexpr (sizeof(IO) == 2 && D <= 128) hipLaunchKernelGGL((prompt_kernel<IO, D, QT, FP8>), dim3((unsigned)workgroups), dim3(kThreads), 0, s, a);
+  if constexpr (sizeof(IO) == 2) hipLaunchKernelGGL((prompt_kernel<IO, D, QT, FP8>), dim3((unsigned)workgroups), dim3(kThreads), 0, s, a);
   else hipLaunchKernelGGL((attention_kernel<IO, D, QT, false, FP8, false>), dim3((unsigned)workgroups), dim3(kThreads), 0, s, a);
   return 0;
 }
