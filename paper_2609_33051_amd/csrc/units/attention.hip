@@ -320,10 +320,14 @@ template <typename IO, bool FP8> __device__ __forceinline__ void put(const Atten
 // ---- the kernel
 
 // A wave's query rows: QT tiles of 16, with the sums over the keys so far.
-template <typename IO, int D, int QT, bool FP8> struct Rows {
-  // bf16 parts of a query and of a weight: what an fp32 result (the scales of an 8-bit output among them) has to keep
-  static constexpr int N = D / 32, QP = sizeof(IO) == 2 ? 1 : 3, WP = FP8 ? 3 : QP;
-  Weight<WP != 1> weight;
+template <typename IO, int D, int QT, bool SPLIT, bool FP8> struct Rows {
+  // bf16 parts of a query and of a weight.  Three keep what an fp32 result has to (the scales of an 8-bit output among
+  // them).  Under a bf16 result a weight's rounding to one is as large as the result's own: over many rows 1.2 to 1.35
+  // times its error, of a few rows, where weights may lie in one part of their binade, up to 1.6 times.  Few rows have
+  // two, and with them the result's own rounding alone (us, one part and two: 64 requests 60.8 and 62.2, 64 with 64
+  // channels 40.8 and 44.6, one of 131072 keys 31.6 and 32.4; 512 new tokens over 32768 keys 325 and 415).
+  static constexpr int N = D / 32, QP = sizeof(IO) == 2 ? 1 : 3, WP = FP8 || QP == 3 ? 3 : SPLIT && QT == 1 ? 2 : 1;
+  Weight<WP == 3> weight;
   bf16x8 q[QT][N][QP];
   floatx4 o[QT][2 * N], l[QT];  // of channels 16 j + 4 (lane / 16) .., and of the weights
   float m[QT];
@@ -593,7 +597,7 @@ __global__ __launch_bounds__(kThreads, waves_held(sizeof(IO), D)) void attention
       return place < most ? place : most;
     };
     const int low = limit(row0), high = limit(row0 + rows - 1);
-    Rows<IO, D, QT, FP8> mine(a.scale);
+    Rows<IO, D, QT, SPLIT, FP8> mine(a.scale);
     mine.start(a, e, h, row0, rows, lane, limit);
 
     const int stride = SPLIT ? kWaves : 1;
@@ -791,7 +795,7 @@ template <typename IO, int D, int QT, bool FP8> __global__ __launch_bounds__(kTh
   };
   const int low = limit(block0), high = limit(block0 + (left < ROWS * kWaves ? left : ROWS * kWaves) - 1);  // of the workgroup
   const int mine_high = rows > 0 ? limit(row0 + rows - 1) : -1;
-  Rows<IO, D, QT, FP8> mine(a.scale);
+  Rows<IO, D, QT, false, FP8> mine(a.scale);
   mine.start(a, e, h, row0, rows, lane, limit);
   const int n = e.length < most ? e.length : most + 1;  // keys there are
   const int steps = high < 0 ? 0 : high / KEYS + 1, whole = low < 0 ? 0 : (low + 1) / KEYS;

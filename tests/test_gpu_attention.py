@@ -523,3 +523,19 @@ def test_offsets_that_do_not_rise(B, T, H, G, D, length):
     torch.cuda.synchronize()
     assert bool((room[:32] == 7).all()) and bool((room[32 + T:] == 7).all())
     assert torch.equal(ops.attention(cache, tab, ln, q[:1])[0], want)
+
+
+@pytest.mark.parametrize("B,H,G,D,longest", [(1, 32, 8, 128, 9000), (5, 16, 1, 64, 700), (40, 8, 4, 256, 500), (3, 7, 1, 96, 3000), (70, 12, 6, 192, 200)])
+def test_single_tokens_keep_16_bits_of_a_weight(B, H, G, D, longest):
+    """A bf16 output of single tokens is off by its own rounding and 2^-16 of the weights: each is two bf16 parts, the second half a step (2^-8) of the first off by
+    2^-8 of itself; twice, for the sum of the weights."""
+    case("two parts", B, H, G, D, longest)
+    r = rnd(longest)
+    lengths = [longest - (b * 37) % (longest // 2) for b in range(B)]
+    cache, tab, ln, ks, vs = built(r, lengths, G, D, 64, torch.bfloat16)
+    q = r((B, H, D), torch.bfloat16)
+    got, _ = ops.attention(cache, tab, ln, q)
+    for b in range(B):
+        o, mag, most = R.attention(q[b:b + 1], ks[b], vs[b], 1, D ** -0.5)
+        fp32 = R.bound(o, mag, most, lengths[b], D, torch.float32)
+        R.close(got[b:b + 1], o, fp32 + 2 * 2.0 ** -16 * mag + (o.abs() + fp32 + 2.0 ** -15 * mag) * R.U16, f"sequence {b}")
