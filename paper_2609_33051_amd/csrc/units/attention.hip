@@ -13,9 +13,9 @@
 // score is compared with another and nothing is rescaled (one prompt of 8192 tokens, with the registers that this
 // frees: 2000 -> 607 us).
 //
-// Single tokens are bound by the cache's bytes: 64 over contexts of up to 8192, 32 heads on 8 of 128 channels, in 56
-// us (5.9 TB/s; the loads alone take as long), one over 131072 keys in 26 (5.5).  Prompts are bound by the vector
-// units (exponentials, the cache's conversion) and the matrix units, which hardly overlap: one of 8192 tokens in 526
+// Single tokens are bound by the cache's bytes: 64 over contexts of up to 8192, 32 heads on 8 of 128 channels, in 59
+// us (5.6 TB/s; with weights in one part 56, as long as the loads alone), one over 131072 keys in 27 (5.2).  Prompts are bound by the vector
+// units (exponentials, the cache's conversion) and the matrix units, which hardly overlap: one of 8192 tokens in 524
 // to 543 us, 1.0 PFLOP/s.
 #include <type_traits>
 
