@@ -106,15 +106,18 @@ def test_two_tiles_a_wave_split(io, D, H, G, page, new, lengths):
     check(io, H, G, D, page, new, lengths, seed=D)
 
 
-@pytest.mark.parametrize("io,H,G,D,new,lengths,kernel", [
+EIGHT = [
     ("bf16", 8, 2, 128, [1, 1, 1], [3, 40, 4000], "attention_kernel<t,128,1,1,1,0>"), ("bf16", 8, 2, 64, [1, 1], [1, 700], "attention_kernel<t,64,1,1,1,0>"),
     ("bf16", 8, 2, 128, [301, 77], [301, 12077], "attention_kernel<t,128,2,1,1,0>"), ("bf16", 8, 2, 64, [300], [8300], "attention_kernel<t,64,2,1,1,0>"),
     ("f32", 8, 2, 64, [300], [8300], "attention_kernel<f,64,2,1,1,0>"), ("bf16", 32, 8, 128, [1200, 900], [1200, 1000], "prompt_kernel<t,128,2,1>"),
     ("bf16", 64, 16, 64, [1100], [1111], "prompt_kernel<t,64,2,1>"), ("bf16", 16, 16, 256, [1100, 3000], [1200, 3000], "prompt_kernel<t,256,1,1>"),
-    ("f32", 32, 8, 128, [1200, 900], [1200, 1000], "attention_kernel<f,128,1,0,1,0>")])
+    ("f32", 32, 8, 128, [1200, 900], [1200, 1000], "attention_kernel<f,128,1,0,1,0>")]
+
+
+@pytest.mark.parametrize("io,H,G,D,new,lengths,kernel", EIGHT)
 def test_scales_of_8_bits(io, H, G, D, new, lengths, kernel):
     """An 8-bit output's scales are in 32 bits, whatever io is: off by what the fp32 form is, and at most 2^-16 of each weight (as two bf16 parts would be),
-    twice, for the sum of the weights.  A weight of one bf16 part, off by 2^-8, is past that."""
+    twice, for the sum of the weights."""
     case("scales", io, H, G, D, new, lengths)
     dt, r = DT[io], rnd(D)
     cache, tab, ln, ks, vs = built(r, lengths, G, D, 32, dt)
@@ -135,6 +138,39 @@ def test_scales_of_8_bits(io, H, G, D, new, lengths, kernel):
         # e4m3: 2^-4 of a value, 2^-10 of the scale where it is below the normal ones
         y = got[at:at + n].float().double().reshape(n, -1, 128) * s[..., None]
         R.close(y, o, bd + o.abs() * 2.0 ** -4 + s[..., None] * 2.0 ** -10 + 8 * R.U32 * o.abs(), f"sequence {b}")
+        at += n
+
+
+@pytest.mark.parametrize("io,H,G,D,new,lengths,kernel", [(*e[:5], [min(n, 9000) for n in e[5]], e[6]) for e in EIGHT])
+def test_weights_of_8_bits_are_not_bf16(io, H, G, D, new, lengths, kernel):
+    """Every other key weighs w = (1 + 0.98 2^-8) / 2, which bf16 would take to 1/2, 0.98 2^-8 of it off; the others weigh 1.  With values 1 and 0 the outputs are
+    a / (a + b w) of a keys and b, of which that rounding is w b / (a + b w) 0.98 2^-8, some 1/3 2^-8 and so 1.3e-3: more than the bound, which 16 bits of a weight keep."""
+    case("not bf16", io, H, G, D, new, lengths)
+    w = 0.5 * (1.0 + 0.98 * 2.0 ** -8)
+    scale = float(torch.tensor(-torch.log(torch.tensor(w, dtype=torch.float64)).item(), dtype=torch.float32))
+    T, dt = sum(lengths), DT[io]
+    k, v = torch.zeros((T, G, D), dtype=dt, device="cuda"), torch.zeros((T, G, D), dtype=dt, device="cuda")
+    at = 0
+    for n in lengths:
+        k[at + 1:at + n:2, :, 0] = -1.0
+        v[at:at + n:2] = 1.0
+        at += n
+    tab, pages = R.table(lengths, 32)
+    cache = ops.new_cache(pages, G, 32, D)
+    ops.cache_append(cache, tab, i32(lengths), k, v, offsets=R.offsets(lengths))
+    q = torch.zeros((sum(new), H, D), dtype=dt, device="cuda")
+    q[..., 0] = 1.0
+    _, scales = ops.attention(cache, tab, i32(lengths), q, offsets=R.offsets(new), scale=scale, out_dtype=F8)
+    at = 0
+    w = torch.exp(torch.tensor(-scale, dtype=torch.float64))
+    for n, length in zip(new, lengths):
+        seen = torch.arange(length - n + 1, length + 1, device="cuda", dtype=torch.float64)
+        b = (seen / 2).floor()
+        want = (seen - b) / (seen - b + b * w)
+        # one product a score, a handful of roundings of the exponent; the sums; 16 bits of a weight
+        bd = want * (2 * 32 * R.U32 + (length + 8) * R.U32 + 2 * 2.0 ** -16)
+        assert bool((bd < 1.3e-3 * 2 / 3 * want).all())
+        R.close(scales[:, at:at + n].t(), (want / 448.0)[:, None].expand(-1, H * D // 128), (bd + 4 * R.U32 * want)[:, None] / 448.0, "scales")
         at += n
 
 
