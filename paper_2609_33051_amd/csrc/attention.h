@@ -19,6 +19,11 @@ struct NewTokens {
   const int32_t* table;
   size_t ld_table;
   int columns;
+  // Place of sequence b's i-th of n new tokens.  Lengths below -2^30 count as that, so that no place wraps.
+  __device__ __forceinline__ int place(int b, int n, int i) const {
+    const int length = lengths[b];
+    return (length < -(1 << 30) ? -(1 << 30) : length) - n + i;
+  }
   // The page of a sequence's record `tile`, or -1 where there is none.
   __device__ __forceinline__ int page(const Cache& c, int b, int tile) const {
     const int j = tile >> c.shift;

@@ -124,7 +124,7 @@ __global__ __launch_bounds__(kThreads) void append_kernel(CacheAppendArgs a, int
     b = a.tok.seq.of(t);
     const int first = a.tok.seq.start(b), n = a.tok.seq.start(b + 1) - first;
     if (t < first || t >= first + n) return;  // behind the last sequence
-    place = a.tok.lengths[b] - n + (t - first);
+    place = a.tok.place(b, n, t - first);
   }
   Turn<IO, PAIRS> turn;
   const int half = a.rot.rotated >> 1;
@@ -223,7 +223,7 @@ template <typename IO> __global__ __launch_bounds__(kThreads) void read_kernel(R
   if (t >= a.tok.seq.tokens) return;
   const int b = a.tok.seq.of(t), first = a.tok.seq.start(b), n = a.tok.seq.start(b + 1) - first;
   if (t < first || t >= first + n) return;
-  const int place = a.tok.lengths[b] - n + (t - first), tile = place >> 4, r = place & 15;
+  const int place = a.tok.place(b, n, t - first), tile = place >> 4, r = place & 15;
   const int page = place < 0 ? 0 : a.tok.page(a.cache, b, tile);
   const uint8_t* rec = a.cache.data + ((((size_t)(page < 0 ? 0 : page) * G + h) << a.cache.shift) + (tile & ((1 << a.cache.shift) - 1))) * (17 * D);
   auto give = [&](void* out, int c0, uint32_t w, uint32_t e) {
