@@ -159,7 +159,7 @@ __device__ __forceinline__ float across_rows_max(float x) {
 }
 
 // Weights 2^(c (s - m)) of scores s under a maximum m, c = scale log2 e.  EXACT: to fp32's last places, with what c's own
-// rounding leaves out; otherwise the product c m is rounded, by the same for every weight of a row.
+// rounding leaves out; otherwise the product c m is rounded, by the same for every weight under m.
 template <bool EXACT> struct Weight {
   float c, low;
   __device__ __forceinline__ explicit Weight(float scale) {
@@ -175,8 +175,17 @@ template <bool EXACT> struct Weight {
       return __builtin_amdgcn_exp2f(fmaf(s, c, -under));
     }
   }
-  // What sums under the maximum m are multiplied by under a larger one.
-  __device__ __forceinline__ float from(float m, float to) const { return m == to ? 1.f : (*this)(m, under(to)); }
+  // What sums under the maximum m are multiplied by under a larger one: between the same rounded products that the weights are
+  // taken over (scores past 2^22 have them whole numbers: with m c itself sums of different maxima were 19 % apart).
+  __device__ __forceinline__ float from(float m, float to) const {
+#pragma clang fp contract(off)  // a fused m c would not be the rounded one
+    if constexpr (EXACT) {
+      return m == to ? 1.f : (*this)(m, under(to));
+    } else {
+      const float x = m * c - to * c;  // -inf of a maximum that is
+      return __builtin_amdgcn_exp2f(m == to ? 0.f : x);
+    }
+  }
 };
 
 // ---- what a workgroup takes

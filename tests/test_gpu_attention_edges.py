@@ -27,3 +27,37 @@ def test_the_smallest_lengths(io, length):
     assert not bool(a[2:7].any()) and not bool(b[2:7].any()) and same(b[7:], R.held(v[7:]))
     out, _ = ops.attention(cache, tab, lengths, got, offsets=off)
     assert not bool(out[2:7].any()) and bool(torch.isfinite(out).all()) and bool(out[[0, 1, 7, 8, 9]].any(-1).all())
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+@pytest.mark.parametrize("rising,D,H,G,new,lengths,last", [
+    (False, 128, 8, 2, [1, 1], [5000, 900], 1), (True, 128, 8, 2, [1, 1], [4362, 4300], 1), (False, 64, 8, 2, [300, 77], [8300, 12077], 300),
+    (True, 64, 8, 2, [300], [4500], 300), (True, 128, 32, 8, [4362], [4362], 200), (False, 256, 16, 16, [2100, 1000], [2100, 1000], 200)])
+def test_scores_far_from_zero(io, rising, D, H, G, new, lengths, last):
+    """Scores 1.5 2^22 + {0 .. 6}, whole in fp32, over maxima that differ from wave to wave or move on the way: their product with log2 e is
+    rounded to whole numbers, by the same for all that a row's sums are made of.  What counts is how far scores lie apart, 6."""
+    case("far scores", io, rising, D, H, G, new, lengths)
+    dt, T = DT[io], sum(lengths)
+    k, v = torch.zeros((T, G, D), dtype=dt, device="cuda"), torch.zeros((T, G, D), dtype=dt, device="cuda")
+    k[..., :32] = 192.0
+    grid = torch.tensor(R.GRID, device="cuda")
+    at = 0
+    for n in lengths:
+        j = torch.arange(n, device="cuda")
+        # rising: 4096 keys of 0, then 6, so that the weights' sum passes 2^16 some 150 keys later
+        f = torch.where(j < 4096, 0.0, 6.0) if rising else grid[j // 32 % 8]
+        k[at:at + n, :, 32] = f[:, None].to(dt)
+        v[at:at + n] = (torch.where(j < 4096 + 128, 1.0, -1.0) if rising else torch.where(j // 32 % 3 == 0, 1.0, -1.0))[:, None, None].to(dt)
+        at += n
+    tab, pages = R.table(lengths, 32)
+    cache = ops.new_cache(pages, G, 32, D)
+    ops.cache_append(cache, tab, i32(lengths), k, v, offsets=R.offsets(lengths))
+    q = torch.zeros((sum(new), H, D), dtype=dt, device="cuda")
+    q[..., :32], q[..., 32] = 1024.0, 1.0
+    got, _ = ops.attention(cache, tab, i32(lengths), q, offsets=R.offsets(new), scale=1.0)
+    a, t = 0, 0
+    for n, length in zip(new, lengths):
+        a, t = a + length, t + n
+        m = min(n, last)
+        o, mag, most = R.attention(q[t - m:t], k[a - length:a], v[a - length:a], m, 1.0)
+        R.close(got[t - m:t], o, R.bound(o, mag, torch.full_like(most, 6.0), length, D, dt), f"{length} keys")
