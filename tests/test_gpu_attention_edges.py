@@ -61,3 +61,37 @@ def test_scores_far_from_zero(io, rising, D, H, G, new, lengths, last):
         m = min(n, last)
         o, mag, most = R.attention(q[t - m:t], k[a - length:a], v[a - length:a], m, 1.0)
         R.close(got[t - m:t], o, R.bound(o, mag, torch.full_like(most, 6.0), length, D, dt), f"{length} keys")
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+@pytest.mark.parametrize("out", ["io", "f8"])
+@pytest.mark.parametrize("D,H,G,new,lengths", [(128, 8, 2, [1, 1], [9000, 700]), (64, 8, 2, [300], [8300]), (128, 32, 8, [1100, 900], [1200, 1000]), (256, 16, 16, [2100, 1000], [2100, 1000])])
+def test_the_largest_values(io, out, D, H, G, new, lengths):
+    """Values of up to 2^80 under scores that rise to ten (weights of up to 2^14 over a maximum that stays): sums stay in fp32's range."""
+    case("largest values", io, out, D, H, G, new, lengths)
+    dt, r, T = DT[io], rnd(D + len(new)), sum(lengths)
+    k, v = torch.zeros((T, G, D), dtype=dt, device="cuda"), r((T, G, D), torch.float32).clamp(-4, 4) * 2.0 ** 78
+    v = v.to(dt)
+    at = 0
+    for n in lengths:
+        k[at:at + n, :, :2] = (torch.arange(n, device="cuda") * (10.0 / n)).to(dt)[:, None, None]
+        at += n
+    tab, pages = R.table(lengths, 32)
+    cache = ops.new_cache(pages, G, 32, D)
+    ops.cache_append(cache, tab, i32(lengths), k, v, offsets=R.offsets(lengths))
+    q = torch.zeros((sum(new), H, D), dtype=dt, device="cuda")
+    q[..., 0] = 1.0
+    got, scales = ops.attention(cache, tab, i32(lengths), q, offsets=R.offsets(new), scale=1.0, out_dtype=torch.float8_e4m3fn if out == "f8" else None)
+    hk, hv = R.held(k), R.held(v)
+    a, t = 0, 0
+    for n, length in zip(new, lengths):
+        a, t = a + length, t + n
+        m = min(n, 200)
+        o, mag, most = R.attention(q[t - m:t], hk[a - length:a], hv[a - length:a], m, 1.0)
+        bd = R.bound(o, mag, most, length, D, dt)
+        if out == "io":
+            R.close(got[t - m:t], o, bd, f"{length} keys")
+            continue
+        s = scales[:, t - m:t].t()[..., None].double()
+        o, bd = o.reshape(m, -1, 128), bd.reshape(m, -1, 128)
+        R.close(got[t - m:t].float().double().reshape(m, -1, 128) * s, o, bd + o.abs() * 2.0 ** -4 + s * 2.0 ** -10 + 8 * R.U32 * o.abs(), f"{length} keys")
