@@ -79,7 +79,7 @@ typedef struct {
   int32_t places, rotated, interleaved;
 } skssm_rotation;
 
-/* sketchssm_rotary -- y = x rotated, x and y [T][heads][dim] io (dim a multiple of 16 bytes).  y may be x (with its strides). */
+/* sketchssm_rotary -- y = x rotated, x and y [T][heads][dim] io (dim a multiple of 8, up to 512).  y may be x (with its strides). */
 int sketchssm_rotary(int32_t io_dtype, int64_t tokens, int32_t heads, int32_t dim, const skssm_rotation* rotation,
                      const void* x, int64_t ldx, int64_t x_head, void* y, int64_t ldy, int64_t y_head, void* stream);
 

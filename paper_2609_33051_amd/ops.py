@@ -324,7 +324,7 @@ def _rotation(angles: Tensor, positions: Tensor | None, interleaved: bool, token
 
 
 def rotary(x: Tensor, rotation: Tensor, positions: Tensor | None = None, *, interleaved: bool = False, out: Tensor | None = None) -> Tensor:
-    """x [T][heads][dim] io with the leading channels of every head rotated in
+    """x [T][heads][dim] io (dim a multiple of 8, up to 512) with the leading channels of every head rotated in
     pairs: (i, i + R / 2), or (2 i, 2 i + 1) if interleaved.  rotation
     [places][R] holds each place's cosines and then its sines
     (`attention.rotary_angles` makes one); positions [T] int32 names each
