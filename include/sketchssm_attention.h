@@ -87,7 +87,7 @@ int sketchssm_rotary(int32_t io_dtype, int64_t tokens, int32_t heads, int32_t di
  * sketchssm_cache_append -- the new tokens' keys, rotated, and values into the
  * cache; rotates their queries in the same launch where q is given (q_out may be q).
  * k, v [T][kv_heads][dim], q [T][heads][dim] io.  Keys are rounded to 4 bits
- * from fp32.  Two sequences of a call may not share a page that is written.
+ * from fp32.  A page that is written is one sequence's, and stands in its row of the table once.
  */
 typedef struct {
   int32_t io_dtype, heads;
@@ -117,10 +117,20 @@ int sketchssm_cache_read(const skssm_cache* cache, const skssm_new_tokens* seq, 
  * apart) = max(largest |out| of a row's 128 columns / 448, 2^-64): what
  * sketchssm_matmul_fp8 reads (dim 64 with an even number of heads a key head, 128 or 256).
  * A padding row is 0.  Rows of `out` past the last sequence keep their values.
- * Scores, softmax statistics and sums are fp32.  Keys and values enter the products as they
- * are; with bf16 io the weights e^(s - max) are rounded to bf16 (their sum is that of the
- * rounded ones), with F32 io queries and weights keep 24 bits.
- * scale is from 2^-96 to 2^96.  A NaN reaches only outputs of its head whose token sees it.
+ * Scores, softmax statistics and sums are fp32; keys and values enter the products as they are, and with F32 io queries with 24 bits.
+ * Weights e^(s - m) are taken over a maximum m that may be an earlier one of the row's (they are up to 2^16 then) and keep
+ *     24 bits with F32 io,
+ *     at least 16 bits with bf16 io where out is E4M3 (scales are fp32), or where the call's sequences have at most 16 rows
+ *         (new tokens times heads a key head) on average: single tokens of up to 16 heads a key head,
+ *     8 bits at least, bf16's, otherwise: prompts with bf16 io and out;
+ * their sum is that of the rounded ones.  scale is from 2^-96 to 2^96.  Scores and scale times them are in fp32's range, up to 2^126,
+ * but for scores that fall below it, which weigh nothing; values up to 2^80 leave the sums in it whatever the number of
+ * keys.  A NaN reaches only outputs of its head whose token sees it.
+ *
+ * Equal calls give equal bits.  A token's may differ in their last places with the sequences beside it: keys are split elsewhere.
+ * The form is one for the whole call, by the rows that a sequence has on average, and long contexts are split over workgroups only
+ * in that of few rows: prompts and single tokens over long contexts are faster as two calls (a prompt of 4096 tokens and one
+ * token over 131072 keys, 32 heads on 8 of 128 channels: 175 and 35 us, as one call 4.1 ms).
  *
  * workspace: sketchssm_attention_workspace bytes (may be 0), where a sequence
  * is split over workgroups; its contents need not be kept, and calls that may run at the same time need one each.

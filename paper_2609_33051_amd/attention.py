@@ -100,7 +100,8 @@ class Attention:
         """Packed new tokens x [T][hidden] of every sequence (rows offsets[b] ..
         offsets[b+1]-1; None: T / batch each) behind what the cache holds of it,
         with the residual stream: (out [T][hidden], the residual stream with x
-        added)."""
+        added).  Single tokens over long contexts are faster in a `step` of
+        their own than in a call with prompts."""
         H, G, D = self.heads, self.kv_heads, self.dim
         u, s, residual = ops.norm(x, self.norm, self.eps, residual=residual, out_dtype=ops.F8)
         qkv = ops.matmul_fp8(u, s, self.qkv_proj, self.qkv_scale, out_dtype=self.dtype).view(-1, H + 2 * G, D)

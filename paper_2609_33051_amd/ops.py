@@ -383,7 +383,8 @@ def cache_append(cache: Tensor, table: Tensor, lengths: Tensor, k: Tensor, v: Te
     page (j + 1) - 1 are in page table[b][j] of the cache.  lengths, table and
     offsets are int32.  A token whose place is below 0 (lengths[b] less than
     its new tokens) is a padding row and not appended; one whose page is not
-    in the cache is not written.  Sequences may not share a page that is written."""
+    in the cache is not written.  A page that is written is one sequence's, and
+    stands in its row of the table once."""
     dev = _device(k)
     io = _io(k)
     c = _cache(cache, dev)
@@ -448,7 +449,12 @@ def attention(cache: Tensor, table: Tensor, lengths: Tensor, q: Tensor, *, offse
     cache_append, which comes first): (out [T][heads][dim], scales).  heads /
     kv_heads consecutive heads share a key head; scale is dim^-1/2 unless given.
     out_dtype None: the io type; F8: blocks of 128 columns over their scale,
-    scales [heads dim / 128][T] (what matmul_fp8 reads).  Padding rows are 0."""
+    scales [heads dim / 128][T] (what matmul_fp8 reads).  Padding rows are 0.
+
+    One form is taken for the whole call, by the new tokens a sequence has on
+    average: prompts and single tokens over long contexts are faster as two
+    calls.  Weights keep 24 bits in float32; in bfloat16 at least 16 for F8 and
+    for single tokens (of up to 16 heads a key head), 8 for prompts."""
     dev = _device(q)
     io = _io(q)
     c = _cache(cache, dev)
