@@ -6,12 +6,14 @@
 // Both products take the cache as their left operand, so that a query row is one column, one lane in each of
 // the wave's four rows of lanes: the running maximum and every weight are a lane's own, and P^T comes out of
 // the first product in the registers in which the second one takes it (the order in which the 32
-// keys are summed is free, and the cache's records hold the values in the order it leaves).  Nothing passes
-// through LDS.  A row of ones beside V^T sums the weights as the products see them.
+// keys are summed is free, and the cache's records hold the values in the order it leaves).  The weights never pass
+// through LDS; the cache's operands do where a workgroup's waves share them (prompt_kernel).  A row of ones beside V^T
+// sums the weights as the products see them.
 //
 // The maximum that the weights are taken over moves only where the weights' sum has grown past 2^16; until then no
 // score is compared with another and nothing is rescaled (one prompt of 8192 tokens, with the registers that this
-// frees: 2000 -> 607 us).
+// frees: 2000 -> 607 us).  The limit is one for any number of keys: a wave whose sum is past it with scores that do not
+// grow takes the maximum every step (2100 tokens over 130000 keys of equal scores 8.98 ms, of random ones 7.67).
 //
 // Single tokens are bound by the cache's bytes: 64 over contexts of up to 8192, 32 heads on 8 of 128 channels, in 59
 // us (5.6 TB/s; with weights in one part 56, as long as the loads alone), one over 131072 keys in 27 (5.2).  Prompts are bound by the vector
@@ -1015,10 +1017,12 @@ template <typename IO, int D, bool FP8> int launch(const AttentionArgs& a, hipSt
         b.plan = reinterpret_cast<int*>(a.work);
         b.work = reinterpret_cast<float*>(b.plan + plan_words(batch));
       }
-      // Past the caches where the pool is larger than the last-level one, so that nothing of it is there the
-      // next time: 64 requests of up to 8192 tokens 61.3 -> 56.8 us (pool 330 MB); 32 of 4096 with 16 key
-      // heads, out of that cache, 40.3 -> 45.7.  Records of 128 channels only, where every load takes whole
-      // lines: of 64, 41.4 -> 54.4.
+      // Past the caches where the pool is larger than the last-level one.  One layer's cache read over and over: 64
+      // requests of up to 8192 tokens 61.3 -> 56.8 us (pool 330 MB); 32 of 4096 with 16 key heads, out of that cache, 40.3
+      // -> 45.7.  It is the pool that counts and not the part of it that a call can reach: a large pool is that of a model
+      // whose layers pass in turn (eight of 1.1 GB, without and with: 32 of 4096 39.6 and 36.6 us a layer, 64 of 2000 34.7
+      // and 31.0, 64 of 3500 56.8 and 50.6, one of 16384 14.5 and 14.8; one layer alone 34.4 and 35.6, 30.2 and 30.2, 48.0
+      // and 50.4, 14.1 and 14.5).  Records of 128 channels only, where every load takes whole lines: of 64, 41.4 -> 54.4.
       constexpr bool CAN = D == 128 && QT == 1;
       const bool past = CAN && (int64_t)a.cache.pages * G * (17 * D) << a.cache.shift > (int64_t)256 << 20;
       if (past) hipLaunchKernelGGL((attention_kernel<IO, D, QT, true, FP8, CAN>), dim3((unsigned)workgroups), dim3(kThreads), 0, s, b);
